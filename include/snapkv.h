@@ -354,6 +354,97 @@ int snapkv_decode_attention(int dtype, const void* q, const void* k_cache, const
                             float* out, float* out_lse, void* stream);
 
 /*
+ * Appends new tokens' keys and values to a paged cache, keys (and the tokens' queries) rotated by their positions on the
+ * way: what fills the pages that snapkv_compress_paged and snapkv_decode_attention_paged read.  The rows of a compressed
+ * prompt are fewer than its tokens (Sec. 4.1), so the row that a token is stored in and its position are separate
+ * arguments; with rot_dim = 0 the call also moves rows that are rotated already, such as the kept rows out_k and out_v of a
+ * compress call, into pages.
+ *
+ * The T tokens of B sequences lie packed: sequence b's are the tokens cu_seqlens[b] .. cu_seqlens[b + 1] - 1.  Token t of
+ * sequence b goes to logical row r = starts[b] + t - cu_seqlens[b] of its sequence, which is row r % page_size of page
+ * block_table[b][r / page_size].  Rotation by position p of the first rot_dim elements x of a row:
+ *     (x[i], x[j]) -> (x[i] cos[p][m] - x[j] sin[p][m], x[j] cos[p][m] + x[i] sin[p][m]),  m < rot_dim / 2,
+ * with (i, j) = (m, m + rot_dim / 2), or (2m, 2m + 1) when interleaved; in float32, rounded once.  The elements from rot_dim on
+ * stay as they are.
+ *
+ *   dtype   SNAPKV_DTYPE_* of q, k, v, the pages and the outputs
+ *   q       [T, Hq, D] device, or NULL with Hq = 0;  k, v [T, Hkv, D] device: the new tokens; row t of head h starts
+ *           row_stride * t + head_stride * h ELEMENTS after the pointer (row_stride >= D, head_stride >= 0, every row
+ *           16-byte aligned); Hq % Hkv == 0, D in {64, 128}
+ *   cu_seqlens [B + 1] device int32, ascending, or NULL: one token per sequence (T == B).  Tokens before the first
+ *           sequence and behind the last are left alone: nothing is read or written for them
+ *   starts  [B] device int32: rows that each sequence has already
+ *   positions [T] device int32, or NULL: every token's position is its row.  Clamped to [0, n_positions)
+ *   cos, sin [n_positions, rot_dim / 2] device float32, 16-byte aligned (NULL allowed with rot_dim = 0)
+ *   rot_dim 0, or a multiple of 16 (float32: 8) up to D
+ *   k_pages, v_pages [num_pages, page_size, Hkv, D] device;  block_table [B, table_columns] device int32
+ *   q_out   [T, Hq, D] device, the rotated queries (NULL with Hq = 0);  k_out [T, Hkv, D] device or NULL: the rotated keys
+ *           once more, for the attention over the prompt; strides as for the inputs
+ *
+ * Rows that the table has no column for (or before the first) and table entries outside [0, num_pages) are not
+ * written to pages.  Distinct tokens must not meet in one row of one page.  T = 0 or B = 0 does nothing.  No scratch; calls are independent and
+ * may be captured.  Returns SNAPKV_OK or a negative SNAPKV_ERR_* code.
+ */
+int snapkv_append_paged(int dtype, const void* q, const void* k, const void* v, const int32_t* cu_seqlens,
+                        const int32_t* starts, const int32_t* positions, int64_t T, int B, int Hq, int Hkv, int D,
+                        int64_t q_row_stride, int64_t q_head_stride, int64_t k_row_stride, int64_t k_head_stride,
+                        int64_t v_row_stride, int64_t v_head_stride, const float* cos, const float* sin,
+                        int64_t n_positions, int rot_dim, int interleaved, void* k_pages, void* v_pages,
+                        const int32_t* block_table, int64_t table_columns, int64_t num_pages, int page_size, void* q_out,
+                        int64_t q_out_row_stride, int64_t q_out_head_stride, void* k_out, int64_t k_out_row_stride,
+                        int64_t k_out_head_stride, void* stream);
+
+/*
+ * Causal attention over whole prompts packed one behind the other: the step before the compression (Sec. 4.1 runs it at
+ * the end of prompt encoding).  For token i of a prompt and query head h (reading KV head h / g):
+ *     out[i, h, :]   = sum_{j <= i} softmax_j(q[i, h] . k[j, h/g] / sqrt(D)) v[j, h/g],
+ *     out_lse[h, i]  = log sum_{j <= i} exp(q[i, h] . k[j, h/g] / sqrt(D))   (natural logarithm),
+ * j over the tokens of the same prompt.  The last W columns of a prompt in out_lse are the lse that snapkv_compress_lse takes.
+ *
+ *   dtype   SNAPKV_DTYPE_BF16 or SNAPKV_DTYPE_F16 (float32 storage: SNAPKV_ERR_UNSUPPORTED)
+ *   q [T, Hq, D], k and v [T, Hkv, D] device, dtype: row t of head h starts row_stride * t + head_stride * h ELEMENTS after the
+ *           pointer (row_stride >= D, head_stride >= 0, every row 16-byte aligned), e.g. columns of one projection's
+ *           output or head-major storage; finite values; Hq % Hkv == 0, D in {64, 128}
+ *   cu_seqlens [B + 1] device int32, ascending: prompt b is the tokens cu_seqlens[b] .. cu_seqlens[b + 1] - 1 (none: an
+ *           empty prompt).  Values are clamped to [0, T]
+ *   out     [T, Hq, D] device, dtype, contiguous;  out_lse [Hq, T] device float32 or NULL.  Rows that belong to no prompt
+ *           are left as they were
+ *
+ * The probabilities are rounded to dtype before the product with v; sums and statistics are float32.  T = 0 or B = 0
+ * does nothing.  No scratch; calls are independent, repeat bit for bit and may be captured.  Returns SNAPKV_OK or a negative SNAPKV_ERR_*
+ * code.
+ */
+int snapkv_prompt_attention(int dtype, const void* q, const void* k, const void* v, const int32_t* cu_seqlens, int B,
+                            int64_t T, int Hq, int Hkv, int D, int64_t q_row_stride, int64_t q_head_stride,
+                            int64_t k_row_stride, int64_t k_head_stride, int64_t v_row_stride, int64_t v_head_stride,
+                            void* out, float* out_lse, void* stream);
+
+/*
+ * snapkv_decode_attention over a paged cache: attention of one new token per sequence over the rows that its block table
+ * names (prompts of at most C tokens, which the compression leaves as they are, and kept rows moved into pages).
+ *
+ *   dtype   SNAPKV_DTYPE_BF16 or SNAPKV_DTYPE_F16 (float32 storage: SNAPKV_ERR_UNSUPPORTED)
+ *   q       [B, Hq, D] device, dtype;  k_pages, v_pages [num_pages, page_size, Hkv, D] device, dtype, finite values in the
+ *           rows below lens (the others are not read)
+ *   block_table [B, table_columns] device int32; entries outside [0, num_pages) are clamped to that range
+ *   lens    [B] device int32 rows per sequence, clamped to [0, max_len]; a sequence with no rows gets out = 0 and out_lse = -inf
+ *   max_len 1 <= max_len <= table_columns * page_size, at most 2^30: no sequence is longer (it fixes how the keys are split)
+ *   Hq % Hkv == 0, Hq / Hkv <= 16, D in {64, 128}
+ *   out     [B, Hq, D] device, dtype (rounded once from float32);  out_lse [B, Hq] device float32 or NULL
+ *   workspace device memory, 256-byte aligned, of at least snapkv_decode_paged_workspace_bytes(B, Hq, Hkv, D, max_len) bytes
+ *           (which depends on the compute units of the CURRENT device, and is 0 for steps that are not split: then it may be
+ *           NULL), owned by the caller and free to reuse once the enqueued work has finished; its contents do not matter
+ *
+ * Steps with distinct workspaces are independent, and a step may be captured.  Returns SNAPKV_OK or a negative
+ * SNAPKV_ERR_* code.
+ */
+int snapkv_decode_attention_paged(int dtype, const void* q, const void* k_pages, const void* v_pages,
+                                  const int32_t* block_table, int64_t table_columns, int64_t num_pages, int page_size,
+                                  const int32_t* lens, int64_t max_len, int B, int Hq, int Hkv, int D, void* out,
+                                  float* out_lse, void* workspace, size_t workspace_bytes, void* stream);
+size_t snapkv_decode_paged_workspace_bytes(int B, int Hq, int Hkv, int D, int64_t max_len);
+
+/*
  * Top-(kcount) selection alone (Eq. 2), exposed for testing the selector on arbitrary scores:
  *   scores [H, n] device float32, all values >= +0 (their bit patterns are compared as unsigned
  *   integers); out_idx [H, kcount] device int32: the kcount best positions per row under

@@ -27,7 +27,8 @@ SYMBOLS = ("snapkv_version", "snapkv_strerror", "snapkv_compress", "snapkv_compr
            "snapkv_decode_attention", "snapkv_compress_per_query_head",
            "snapkv_capacity_for_rate", "snapkv_hit_rate", "snapkv_compress_paged",
            "snapkv_compress_varlen", "snapkv_compress_layers", "snapkv_compress_static",
-           "snapkv_compress_ws_status", "snapkv_debug_set_wait_limit")
+           "snapkv_compress_ws_status", "snapkv_debug_set_wait_limit", "snapkv_append_paged",
+           "snapkv_prompt_attention", "snapkv_decode_attention_paged", "snapkv_decode_paged_workspace_bytes")
 
 _lib = None
 
@@ -96,6 +97,15 @@ def load():
     L.snapkv_hit_rate.argtypes = [i32, vp, vp, i64, i64, i32, i32, i32, vp, i32, i64, i64, ctypes.c_float, vp, vp]
     L.snapkv_decode_attention.restype = i32
     L.snapkv_decode_attention.argtypes = [i32, vp, vp, vp, vp, i32, i32, i32, i32, i64, i64, vp, vp, vp]
+    L.snapkv_append_paged.restype = i32
+    L.snapkv_append_paged.argtypes = [i32, vp, vp, vp, vp, vp, vp, i64, i32, i32, i32, i32, i64, i64, i64, i64, i64, i64,
+                                      vp, vp, i64, i32, i32, vp, vp, vp, i64, i64, i32, vp, i64, i64, vp, i64, i64, vp]
+    L.snapkv_prompt_attention.restype = i32
+    L.snapkv_prompt_attention.argtypes = [i32, vp, vp, vp, vp, i32, i64, i32, i32, i32, i64, i64, i64, i64, i64, i64, vp, vp, vp]
+    L.snapkv_decode_paged_workspace_bytes.restype = sz
+    L.snapkv_decode_paged_workspace_bytes.argtypes = [i32, i32, i32, i32, i64]
+    L.snapkv_decode_attention_paged.restype = i32
+    L.snapkv_decode_attention_paged.argtypes = [i32, vp, vp, vp, vp, i64, i64, i32, vp, i64, i32, i32, i32, i32, vp, vp, vp, sz, vp]
     L.snapkv_release.restype = None
     L.snapkv_release.argtypes = []
     L.snapkv_profile_start.restype = i32
@@ -492,6 +502,126 @@ def snapkv_decode_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: tor
         _dev(lens, "lens", torch.int32) if lens is not None else None, B, Hq, Hkv, D, int(S), cap,
         _dev(out, "out", torch.float32), _dev(out_lse, "out_lse", torch.float32) if out_lse is not None else None,
         _stream(stream)))
+
+
+def _rows(t: torch.Tensor, name: str, dtype):
+    """Address and (row, head) strides of a [T, heads, D] view with contiguous rows; the stride of a dimension of one
+    does not matter."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
+    T, H, D = t.shape
+    if D > 1 and t.stride(2) != 1:
+        raise ValueError(f"the rows of {name} must be contiguous")
+    return t.data_ptr(), t.stride(0) if T > 1 else D, t.stride(1) if H > 1 else 0
+
+
+def _on_current_device(*tensors) -> None:
+    """A call runs on the current device, on a stream of it: tensors of another one are refused."""
+    for t in tensors:
+        if t is not None and t.is_cuda and t.get_device() != torch.cuda.current_device():
+            raise ValueError(f"tensors are on cuda:{t.get_device()}, the current device is cuda:{torch.cuda.current_device()}")
+
+
+def snapkv_append_paged(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
+                        block_table: torch.Tensor, starts: torch.Tensor, cu_seqlens: Optional[torch.Tensor] = None,
+                        positions: Optional[torch.Tensor] = None, cos: Optional[torch.Tensor] = None,
+                        sin: Optional[torch.Tensor] = None, interleaved: bool = False, q: Optional[torch.Tensor] = None,
+                        q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, stream=None) -> None:
+    """k, v [T,Hkv,D] (views with contiguous rows) go into k_pages/v_pages [num_pages, page_size, Hkv, D] behind
+    block_table [B, columns] int32, sequence b's from row starts[b] on; cu_seqlens [B+1] int32, or None: a token per
+    sequence.  With cos/sin [positions, rot_dim/2] float32 the keys, and q [T,Hq,D] -> q_out, are rotated by positions [T]
+    int32 (None: the rows); k_out [T,Hkv,D]: the rotated keys once more."""
+    lib = load()
+    T, Hkv, D = k.shape
+    num_pages, page_size, Hp, Dp = k_pages.shape
+    if tuple(v.shape) != (T, Hkv, D) or (Hp, Dp) != (Hkv, D) or v_pages.shape != k_pages.shape:
+        raise ValueError("k, v, k_pages and v_pages disagree on their shapes")
+    if block_table.dim() != 2 or tuple(starts.shape) != (block_table.shape[0],):
+        raise ValueError("block_table must be [B, columns] and starts [B]")
+    B = block_table.shape[0]
+    if cu_seqlens is not None and tuple(cu_seqlens.shape) != (B + 1,):
+        raise ValueError("cu_seqlens must be [B + 1]")
+    if positions is not None and tuple(positions.shape) != (T,):
+        raise ValueError("positions must be [T]")
+    if (cos is None) != (sin is None) or (cos is not None and (cos.dim() != 2 or cos.shape != sin.shape)):
+        raise ValueError("cos and sin must both be [positions, rot_dim / 2]")
+    if (q is None) != (q_out is None) or (q is not None and (q.dim() != 3 or q.shape != q_out.shape or q.shape[0] != T or q.shape[2] != D)):
+        raise ValueError("q and q_out must both be [T, Hq, D]")
+    if k_out is not None and k_out.shape != k.shape:
+        raise ValueError("k_out must be [T, Hkv, D]")
+    _on_current_device(k, v, k_pages, v_pages, block_table, starts, cu_seqlens, positions, cos, sin, q, q_out, k_out)
+    code, dt, none = _dtype_code(k), k.dtype, (None, 0, 0)
+    int_of = lambda t, name: _dev(t, name, torch.int32) if t is not None else None
+    qp, qr, qh = _rows(q, "q", dt) if q is not None else none
+    op, orow, oh = _rows(q_out, "q_out", dt) if q_out is not None else none
+    cp, cr, ch = _rows(k_out, "k_out", dt) if k_out is not None else none
+    kp, kr, kh = _rows(k, "k", dt)
+    vp, vr, vh = _rows(v, "v", dt)
+    _check(lib.snapkv_append_paged(
+        code, qp, kp, vp, int_of(cu_seqlens, "cu_seqlens"), int_of(starts, "starts"), int_of(positions, "positions"), T, B,
+        q.shape[1] if q is not None else 0, Hkv, D, qr, qh, kr, kh, vr, vh,
+        _dev(cos, "cos", torch.float32) if cos is not None else None, _dev(sin, "sin", torch.float32) if sin is not None else None,
+        cos.shape[0] if cos is not None else 0, 2 * cos.shape[1] if cos is not None else 0, int(bool(interleaved)),
+        _dev(k_pages, "k_pages", dt), _dev(v_pages, "v_pages", dt), _dev(block_table, "block_table", torch.int32),
+        block_table.shape[1], num_pages, page_size, op, orow, oh, cp, cr, ch, _stream(stream)))
+
+
+def snapkv_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqlens: torch.Tensor, out: torch.Tensor,
+                            out_lse: Optional[torch.Tensor] = None, stream=None) -> None:
+    """q [T,Hq,D], k/v [T,Hkv,D] (bf16 or fp16 views with contiguous rows), the prompts packed by cu_seqlens [B+1] int32 ->
+    out [T,Hq,D] of q's dtype and, if given, out_lse [Hq,T] float32."""
+    lib = load()
+    T, Hq, D = q.shape
+    Tk, Hkv, Dk = k.shape
+    if (Tk, Dk) != (T, D) or v.shape != k.shape:
+        raise ValueError("q, k and v disagree on their shapes")
+    if out.shape != q.shape or (out_lse is not None and tuple(out_lse.shape) != (Hq, T)):
+        raise ValueError("out must be [T, Hq, D] and out_lse [Hq, T]")
+    if cu_seqlens.dim() != 1 or cu_seqlens.numel() < 1:
+        raise ValueError("cu_seqlens must be [B + 1]")
+    _on_current_device(q, k, v, cu_seqlens, out, out_lse)
+    code, dt = _dtype_code(q), q.dtype
+    qp, qr, qh = _rows(q, "q", dt)
+    kp, kr, kh = _rows(k, "k", dt)
+    vp, vr, vh = _rows(v, "v", dt)
+    _check(lib.snapkv_prompt_attention(
+        code, qp, kp, vp, _dev(cu_seqlens, "cu_seqlens", torch.int32), cu_seqlens.numel() - 1, T, Hq, Hkv, D, qr, qh, kr, kh,
+        vr, vh, _dev(out, "out", dt), _dev(out_lse, "out_lse", torch.float32) if out_lse is not None else None, _stream(stream)))
+
+
+def snapkv_decode_paged_workspace_bytes(B: int, Hq: int, Hkv: int, D: int, max_len: int) -> int:
+    return int(load().snapkv_decode_paged_workspace_bytes(B, Hq, Hkv, D, max_len))
+
+
+def snapkv_decode_attention_paged(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, block_table: torch.Tensor,
+                                  lens: torch.Tensor, max_len: int, out: torch.Tensor, out_lse: Optional[torch.Tensor] = None,
+                                  workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """q [B,Hq,D], k_pages/v_pages [num_pages, page_size, Hkv, D] (bf16 or fp16), block_table [B, columns] int32, lens [B]
+    int32 (at most max_len rows) -> out [B,Hq,D] of q's dtype and, if given, out_lse [B,Hq] float32.  `workspace`: a uint8
+    GPU tensor of snapkv_decode_paged_workspace_bytes; None: allocated by torch for this call, on the current stream."""
+    lib = load()
+    B, Hq, D = q.shape
+    num_pages, page_size, Hkv, Dk = k_pages.shape
+    if Dk != D or v_pages.shape != k_pages.shape:
+        raise ValueError("q, k_pages and v_pages disagree on their shapes")
+    if block_table.dim() != 2 or block_table.shape[0] != B or tuple(lens.shape) != (B,):
+        raise ValueError("block_table must be [B, columns] and lens [B]")
+    if out.shape != q.shape or (out_lse is not None and tuple(out_lse.shape) != (B, Hq)):
+        raise ValueError("out must be [B, Hq, D] and out_lse [B, Hq]")
+    _on_current_device(q, k_pages, v_pages, block_table, lens, out, out_lse, workspace)
+    ins = (_dev(q, "q"), _dev(k_pages, "k_pages", q.dtype), _dev(v_pages, "v_pages", q.dtype),
+           _dev(block_table, "block_table", torch.int32), block_table.shape[1], num_pages, page_size, _dev(lens, "lens", torch.int32))
+    outs = (_dev(out, "out", q.dtype), _dev(out_lse, "out_lse", torch.float32) if out_lse is not None else None)
+    st = _stream(stream)
+    if workspace is None:
+        if stream is not None and st != _stream(None):
+            raise ValueError("a step on another stream than the current one needs a workspace of the caller's")
+        need = lib.snapkv_decode_paged_workspace_bytes(B, Hq, Hkv, D, int(max_len))
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+    _check(lib.snapkv_decode_attention_paged(_dtype_code(q), *ins, int(max_len), B, Hq, Hkv, D, *outs,
+                                             _dev(workspace, "workspace", torch.uint8), workspace.numel(), st))
 
 
 def compress(q_win, k, v, pool_kind: int, p: int, C: int, stream=None

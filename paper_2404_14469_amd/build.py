@@ -9,7 +9,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libsnapkv.so")
 SOURCES = ["snapkv_api.hip", "snapkv_geom.hip", "snapkv_fused.hip", "snapkv_wide.hip", "snapkv_select.hip", "snapkv_topk.hip",
-           "snapkv_decode.hip", "snapkv_hitrate.hip"]
+           "snapkv_decode.hip", "snapkv_hitrate.hip", "snapkv_append.hip", "snapkv_prompt.hip", "snapkv_paged.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 # Packed-fp32 instruction selection is switched off for all device code.
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",

@@ -118,6 +118,13 @@ int elem_bytes(int dtype) { return dtype == SNAPKV_DTYPE_F32 ? 4 : 2; }
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+// A tensor of rows of D contiguous elements behind (row, head) strides in elements: every row 16-byte aligned.
+int check_rows(const void* p, int64_t row_stride, int64_t head_stride, int D, int e) {
+    if (row_stride < D || head_stride < 0 || row_stride > ((int64_t)1 << 40) || head_stride > ((int64_t)1 << 40)) return SNAPKV_ERR_INVALID_ARG;
+    if (!aligned16(p) || row_stride * e % 16 != 0 || head_stride * e % 16 != 0) return SNAPKV_ERR_MISALIGNED;
+    return SNAPKV_OK;
+}
+
 // Shape checks shared by every entry point that scores (steps 1-3).
 int check_score_args(const void* q_win, const void* k, int64_t L, int Hq, int Hkv, int D, int W,
                      int pool_kind, int p) {
@@ -1233,6 +1240,161 @@ int snapkv_hit_rate(int dtype, const void* q_cur, const void* k, int64_t Lk, int
                            static_cast<hipStream_t>(stream)) == hipSuccess
                ? SNAPKV_OK
                : SNAPKV_ERR_HIP;
+}
+
+int snapkv_append_paged(int dtype, const void* q, const void* k, const void* v, const int32_t* cu_seqlens,
+                        const int32_t* starts, const int32_t* positions, int64_t T, int B, int Hq, int Hkv, int D,
+                        int64_t q_row_stride, int64_t q_head_stride, int64_t k_row_stride, int64_t k_head_stride,
+                        int64_t v_row_stride, int64_t v_head_stride, const float* cos, const float* sin,
+                        int64_t n_positions, int rot_dim, int interleaved, void* k_pages, void* v_pages,
+                        const int32_t* block_table, int64_t table_columns, int64_t num_pages, int page_size, void* q_out,
+                        int64_t q_out_row_stride, int64_t q_out_head_stride, void* k_out, int64_t k_out_row_stride,
+                        int64_t k_out_head_stride, void* stream) {
+    if (!valid_dtype(dtype)) return SNAPKV_ERR_INVALID_ARG;
+    if (T < 0 || B < 0 || Hq < 0 || Hkv < 1) return SNAPKV_ERR_INVALID_ARG;
+    if (T == 0 || B == 0) return SNAPKV_OK;
+    if (!k || !v || !starts || !k_pages || !v_pages || !block_table) return SNAPKV_ERR_INVALID_ARG;
+    if ((Hq > 0) != (q != nullptr) || (Hq > 0) != (q_out != nullptr) || Hq % Hkv != 0) return SNAPKV_ERR_INVALID_ARG;
+    if (!cu_seqlens && T != B) return SNAPKV_ERR_INVALID_ARG;
+    if (num_pages < 1 || page_size < 1 || table_columns < 1) return SNAPKV_ERR_INVALID_ARG;
+    if (rot_dim < 0 || rot_dim > D || (interleaved != 0 && interleaved != 1)) return SNAPKV_ERR_INVALID_ARG;
+    if (rot_dim > 0 && (!cos || !sin || n_positions < 1)) return SNAPKV_ERR_INVALID_ARG;
+    if (D != 64 && D != 128) return SNAPKV_ERR_UNSUPPORTED;
+    const int e = elem_bytes(dtype);
+    if (rot_dim % (32 / e) != 0) return SNAPKV_ERR_UNSUPPORTED;
+    if (T >= (int64_t)1 << 31 || B >= 1 << 24 || Hq + 2 * (int64_t)Hkv > 65535 || num_pages > ((int64_t)1 << 31) ||
+        table_columns > ((int64_t)1 << 31) || n_positions > ((int64_t)1 << 31))
+        return SNAPKV_ERR_UNSUPPORTED;
+    struct { const void* p; int64_t rows, heads; } const t[] = {
+        {k, k_row_stride, k_head_stride}, {v, v_row_stride, v_head_stride}, {q, q_row_stride, q_head_stride},
+        {q_out, q_out_row_stride, q_out_head_stride}, {k_out, k_out_row_stride, k_out_head_stride}};
+    for (const auto& x : t) {
+        if (!x.p) continue;
+        const int rc = check_rows(x.p, x.rows, x.heads, D, e);
+        if (rc != SNAPKV_OK) return rc;
+    }
+    if (!aligned16(k_pages) || !aligned16(v_pages) || !aligned16(cos) || !aligned16(sin)) return SNAPKV_ERR_MISALIGNED;
+    for (const int32_t* x : {cu_seqlens, starts, positions, block_table})
+        if ((reinterpret_cast<uintptr_t>(x) & 3u) != 0) return SNAPKV_ERR_MISALIGNED;
+    AppendArgs A{};
+    A.q = static_cast<const char*>(q);
+    A.k = static_cast<const char*>(k);
+    A.v = static_cast<const char*>(v);
+    A.q_rs = q_row_stride * e;
+    A.q_hs = q_head_stride * e;
+    A.k_rs = k_row_stride * e;
+    A.k_hs = k_head_stride * e;
+    A.v_rs = v_row_stride * e;
+    A.v_hs = v_head_stride * e;
+    A.q_out = static_cast<char*>(q_out);
+    A.k_out = static_cast<char*>(k_out);
+    A.qo_rs = q_out_row_stride * e;
+    A.qo_hs = q_out_head_stride * e;
+    A.ko_rs = k_out_row_stride * e;
+    A.ko_hs = k_out_head_stride * e;
+    A.k_pages = static_cast<char*>(k_pages);
+    A.v_pages = static_cast<char*>(v_pages);
+    A.table = block_table;
+    A.table_stride = table_columns;
+    A.table_rows = table_columns * page_size;
+    A.pages = num_pages;
+    A.starts = starts;
+    A.cu = cu_seqlens;
+    A.positions = positions;
+    A.cos = cos;
+    A.sin = sin;
+    A.npos = n_positions;
+    A.T = T;
+    A.B = B;
+    A.Hq = Hq;
+    A.Hkv = Hkv;
+    A.page = page_size;
+    A.rot = rot_dim;
+    return launch_append(dtype, D, interleaved != 0, A, static_cast<hipStream_t>(stream)) == hipSuccess ? SNAPKV_OK
+                                                                                                    : SNAPKV_ERR_HIP;
+}
+
+int snapkv_prompt_attention(int dtype, const void* q, const void* k, const void* v, const int32_t* cu_seqlens, int B,
+                            int64_t T, int Hq, int Hkv, int D, int64_t q_row_stride, int64_t q_head_stride,
+                            int64_t k_row_stride, int64_t k_head_stride, int64_t v_row_stride, int64_t v_head_stride,
+                            void* out, float* out_lse, void* stream) {
+    if (!valid_dtype(dtype)) return SNAPKV_ERR_INVALID_ARG;
+    if (T < 0 || B < 0 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0) return SNAPKV_ERR_INVALID_ARG;
+    if (T == 0 || B == 0) return SNAPKV_OK;
+    if (!q || !k || !v || !cu_seqlens || !out) return SNAPKV_ERR_INVALID_ARG;
+    if (dtype == SNAPKV_DTYPE_F32 || (D != 64 && D != 128)) return SNAPKV_ERR_UNSUPPORTED;
+    if (T >= (int64_t)1 << 30 || B >= 1 << 24 || Hq > 65535 || (T / 64 + B) * Hq >= (int64_t)1 << 31) return SNAPKV_ERR_UNSUPPORTED;
+    struct { const void* p; int64_t rows, heads; } const t[] = {
+        {q, q_row_stride, q_head_stride}, {k, k_row_stride, k_head_stride}, {v, v_row_stride, v_head_stride}};
+    for (const auto& x : t) {
+        const int rc = check_rows(x.p, x.rows, x.heads, D, 2);
+        if (rc != SNAPKV_OK) return rc;
+    }
+    if (!aligned16(out) || (reinterpret_cast<uintptr_t>(out_lse) & 3u) != 0 || (reinterpret_cast<uintptr_t>(cu_seqlens) & 3u) != 0)
+        return SNAPKV_ERR_MISALIGNED;
+    PromptArgs A{};
+    A.q = static_cast<const char*>(q);
+    A.k = static_cast<const char*>(k);
+    A.v = static_cast<const char*>(v);
+    A.q_rs = q_row_stride * 2;
+    A.q_hs = q_head_stride * 2;
+    A.k_rs = k_row_stride * 2;
+    A.k_hs = k_head_stride * 2;
+    A.v_rs = v_row_stride * 2;
+    A.v_hs = v_head_stride * 2;
+    A.out = static_cast<char*>(out);
+    A.lse = out_lse;
+    A.cu = cu_seqlens;
+    A.T = T;
+    A.B = B;
+    A.Hq = Hq;
+    A.Hkv = Hkv;
+    A.g = Hq / Hkv;
+    return launch_prompt(dtype, D, A, static_cast<hipStream_t>(stream)) == hipSuccess ? SNAPKV_OK : SNAPKV_ERR_HIP;
+}
+
+size_t snapkv_decode_paged_workspace_bytes(int B, int Hq, int Hkv, int D, int64_t max_len) {
+    if (B < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || max_len < 1 || max_len > (int64_t)1 << 30) return 0;
+    if (D != 64 && D != 128) return 0;
+    return paged_plan(B, Hq, Hkv, D, max_len).bytes;
+}
+
+int snapkv_decode_attention_paged(int dtype, const void* q, const void* k_pages, const void* v_pages,
+                                  const int32_t* block_table, int64_t table_columns, int64_t num_pages, int page_size,
+                                  const int32_t* lens, int64_t max_len, int B, int Hq, int Hkv, int D, void* out,
+                                  float* out_lse, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!valid_dtype(dtype)) return SNAPKV_ERR_INVALID_ARG;
+    if (!q || !k_pages || !v_pages || !block_table || !lens || !out) return SNAPKV_ERR_INVALID_ARG;
+    if (B < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || num_pages < 1 || page_size < 1 || table_columns < 1 || max_len < 1)
+        return SNAPKV_ERR_INVALID_ARG;
+    if (dtype == SNAPKV_DTYPE_F32 || (D != 64 && D != 128)) return SNAPKV_ERR_UNSUPPORTED;
+    if (Hq / Hkv > 16 || Hkv > 65535 || B > 65535 || max_len > (int64_t)1 << 30 || num_pages > ((int64_t)1 << 31) ||
+        table_columns > ((int64_t)1 << 31))
+        return SNAPKV_ERR_UNSUPPORTED;
+    if (max_len > table_columns * page_size) return SNAPKV_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(out)) return SNAPKV_ERR_MISALIGNED;
+    for (const void* x : {(const void*)out_lse, (const void*)lens, (const void*)block_table})
+        if ((reinterpret_cast<uintptr_t>(x) & 3u) != 0) return SNAPKV_ERR_MISALIGNED;
+    const size_t need = paged_plan(B, Hq, Hkv, D, max_len).bytes;
+    if (need > 0 && (!workspace || workspace_bytes < need)) return SNAPKV_ERR_WORKSPACE;
+    if (need > 0 && (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return SNAPKV_ERR_MISALIGNED;
+    PagedArgs A{};
+    A.q = static_cast<const char*>(q);
+    A.k = static_cast<const char*>(k_pages);
+    A.v = static_cast<const char*>(v_pages);
+    A.table = block_table;
+    A.lens = lens;
+    A.table_stride = table_columns;
+    A.pages = num_pages;
+    A.max_len = max_len;
+    A.B = B;
+    A.Hq = Hq;
+    A.Hkv = Hkv;
+    A.g = Hq / Hkv;
+    A.page = page_size;
+    A.out = static_cast<char*>(out);
+    A.lse = out_lse;
+    return launch_paged(dtype, D, A, workspace, static_cast<hipStream_t>(stream)) == hipSuccess ? SNAPKV_OK : SNAPKV_ERR_HIP;
 }
 
 void snapkv_release(void) {

@@ -1,0 +1,282 @@
+// Attention of one new token per sequence over a paged cache of [pages, page, Hkv, D] rows.
+//
+//   out[b, h] = sum_j softmax_j(q[b, h] . k_j / sqrt(D)) v_j,   lse[b, h] = log sum_j exp(q[b, h] . k_j / sqrt(D)),
+//
+// j over the lens[b] rows of sequence b: one pass with the running maximum and sum.  Every row is read once, so HBM bounds
+// the step, and one short sequence the latency of its few loads.  The arithmetic is that of the step over compacted
+// caches (snapkv_decode.hip): 16x16x32 products with the g query heads of a KV head as the 16 columns, probabilities in two
+// parts of the storage type, value tiles transposed by a 0/1 product.
+//
+// Work split: a workgroup of four waves takes `chunk` keys of one (sequence, KV head), the same number in every sequence, so
+// a long sequence among short ones is shared out as finely as one by itself; workgroups beyond a sequence's end return
+// at once.  Sequences of one chunk are finished by their workgroup; the partial (max, sum, output) of longer
+// ones are joined by a second kernel.  Rows behind a sequence's end are never read: their lanes read the last row again.
+#include "snapkv_attn.h"
+#include "snapkv_internal.h"
+
+#include <algorithm>
+#include <cmath>
+
+namespace snapkv {
+namespace {
+
+constexpr int kWaves = 4;
+
+template <typename T> struct store_type;
+template <> struct store_type<dec_bf16> { typedef __bf16 type; };
+template <> struct store_type<dec_f16> { typedef _Float16 type; };
+
+template <typename T, int D>
+__global__ __launch_bounds__(kWaves * 64) void paged_attn(const PagedArgs A) {
+    typedef typename store_type<T>::type elem;
+    constexpr int NP = D / 32;        // 16-byte pieces per lane and row
+    constexpr int NB = D / 16;        // 16-column blocks of the output
+    constexpr int ROW = D * 2;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int n16 = lane & 15, kg = lane >> 4;
+    const int chunk = blockIdx.x, kvh = blockIdx.y, b = blockIdx.z;
+    int64_t len = A.lens[b];
+    const int S = (int)(len < 0 ? 0 : (len > A.max_len ? A.max_len : len));
+    const int begin = chunk * A.chunk;
+    if (begin >= S && chunk > 0) return;
+    const int end = begin + A.chunk < S ? begin + A.chunk : S;     // keys begin .. end - 1
+    const int32_t* table = A.table + (int64_t)b * A.table_stride;
+    const int64_t token = (int64_t)A.Hkv * ROW;                    // bytes between the rows of a page
+    const char* kbase = A.k + (int64_t)kvh * ROW;
+    const char* vbase = A.v + (int64_t)kvh * ROW;
+
+    uint4 qf[NP];
+#pragma unroll
+    for (int c = 0; c < NP; ++c) qf[c] = make_uint4(0, 0, 0, 0);
+    if (n16 < A.g) {
+        const char* qrow = A.q + ((int64_t)b * A.Hq + (int64_t)kvh * A.g + n16) * ROW;
+#pragma unroll
+        for (int c = 0; c < NP; ++c) qf[c] = *reinterpret_cast<const uint4*>(qrow + (4 * c + kg) * 16);
+    }
+    const uint4 sel0 = selector<T>(lane, 0), sel1 = selector<T>(lane, 1);
+
+    float m = -INFINITY, lsum = 0.f;
+    dfx4 acc[NB];
+#pragma unroll
+    for (int i = 0; i < NB; ++i) acc[i] = dfx4{0.f, 0.f, 0.f, 0.f};
+
+    auto offset_of = [&](int key) {                    // byte offset of the row of a key, 64 bits
+        const int r = key < end ? key : end - 1;
+        const int pg = (int)(((uint64_t)(unsigned)r * A.page_magic) >> A.page_shift);
+        int64_t at = table[pg];
+        at = at < 0 ? 0 : (at >= A.pages ? A.pages - 1 : at);
+        return (at * A.page + (r - pg * A.page)) * token;
+    };
+    struct PairRegs {
+        uint4 kx[NP], ky[NP], vx[NP], vy[NP];
+    };
+    auto request = [&](PairRegs& P, int key0) {
+        const int64_t rx = offset_of(key0 + n16), ry = offset_of(key0 + 16 + n16);
+#pragma unroll
+        for (int c = 0; c < NP; ++c) {
+            P.kx[c] = *reinterpret_cast<const uint4*>(kbase + rx + (4 * c + kg) * 16);
+            P.ky[c] = *reinterpret_cast<const uint4*>(kbase + ry + (4 * c + kg) * 16);
+        }
+#pragma unroll
+        for (int c = 0; c < NP; ++c) {
+            P.vx[c] = *reinterpret_cast<const uint4*>(vbase + rx + (4 * c + kg) * 16);
+            P.vy[c] = *reinterpret_cast<const uint4*>(vbase + ry + (4 * c + kg) * 16);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto process = [&](const PairRegs& P, int key0) {
+        dfx4 sx = {0.f, 0.f, 0.f, 0.f}, sy = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < NP; ++c) {
+            sx = mma(T{}, P.kx[c], qf[c], sx);
+            sy = mma(T{}, P.ky[c], qf[c], sy);
+        }
+        const int k0 = key0 + 4 * kg;
+        float e[8];
+        float tmax = -INFINITY;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            e[r] = k0 + r < end ? sx[r] * A.scale2 : -INFINITY;
+            e[4 + r] = k0 + 16 + r < end ? sy[r] * A.scale2 : -INFINITY;
+            tmax = fmaxf(tmax, fmaxf(e[r], e[4 + r]));
+        }
+        tmax = fmaxf(tmax, __shfl_xor(tmax, 16));
+        tmax = fmaxf(tmax, __shfl_xor(tmax, 32));
+        const float mn = fmaxf(m, tmax);
+        const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+        m = mn;
+        float psum = 0.f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            e[j] = __builtin_amdgcn_exp2f(e[j] - mn);
+            psum += e[j];
+        }
+        lsum = lsum * alpha + psum;
+        uint4 ph, pl;
+        split2(T{}, e[0], e[1], ph.x, pl.x);
+        split2(T{}, e[2], e[3], ph.y, pl.y);
+        split2(T{}, e[4], e[5], ph.z, pl.z);
+        split2(T{}, e[6], e[7], ph.w, pl.w);
+#pragma unroll
+        for (int i = 0; i < NB; ++i) acc[i] *= alpha;
+#pragma unroll
+        for (int c = 0; c < NP; ++c) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+                const dfx4 z = {0.f, 0.f, 0.f, 0.f};
+                const dfx4 tx = mma(T{}, P.vx[c], half ? sel1 : sel0, z);
+                const dfx4 ty = mma(T{}, P.vy[c], half ? sel1 : sel0, z);
+                uint4 vt;
+                vt.x = pack_exact(T{}, tx[0], tx[1]);
+                vt.y = pack_exact(T{}, tx[2], tx[3]);
+                vt.z = pack_exact(T{}, ty[0], ty[1]);
+                vt.w = pack_exact(T{}, ty[2], ty[3]);
+                dfx4 o = acc[2 * c + half];
+                o = mma(T{}, vt, ph, o);
+                o = mma(T{}, vt, pl, o);
+                acc[2 * c + half] = o;
+            }
+        }
+    };
+    constexpr int STEP = 32 * kWaves;
+    PairRegs R0, R1;
+    int key = begin + 32 * wave;
+    if (key < end) {
+        request(R0, key);
+        for (;;) {
+            request(R1, key + STEP < end ? key + STEP : key);
+            process(R0, key);
+            key += STEP;
+            if (key >= end) break;
+            request(R0, key + STEP < end ? key + STEP : key);
+            process(R1, key);
+            key += STEP;
+            if (key >= end) break;
+        }
+    }
+    lsum += __shfl_xor(lsum, 16);
+    lsum += __shfl_xor(lsum, 32);
+
+    __shared__ float s_acc[kWaves][16][D + 4];
+    __shared__ float s_m[kWaves][16], s_l[kWaves][16];
+#pragma unroll
+    for (int i = 0; i < NB; ++i)
+        *reinterpret_cast<float4*>(&s_acc[wave][n16][16 * i + 4 * kg]) = make_float4(acc[i][0], acc[i][1], acc[i][2], acc[i][3]);
+    if (kg == 0) {
+        s_m[wave][n16] = m;
+        s_l[wave][n16] = lsum;
+    }
+    __syncthreads();
+    constexpr int DT = D / 16;
+    const int qi = tid >> 4, d0 = (tid & 15) * DT;
+    if (qi < A.g) {
+        float M = -INFINITY;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s_m[w][qi]);
+        float Lq = 0.f, o[DT];
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[d] = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const float mw = s_m[w][qi];
+            const float f = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw - M);
+            Lq += s_l[w][qi] * f;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[d] += s_acc[w][qi][d0 + d] * f;
+        }
+        const int64_t hq = (int64_t)b * A.Hq + (int64_t)kvh * A.g + qi;
+        if (S <= A.chunk) {
+            const float inv = Lq > 0.f ? 1.f / Lq : 0.f;
+            elem* out = reinterpret_cast<elem*>(A.out) + hq * D + d0;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) out[d] = (elem)(o[d] * inv);
+            if (A.lse && (tid & 15) == 0)
+                A.lse[hq] = Lq > 0.f ? (M + __builtin_amdgcn_logf(Lq)) * 0.6931471805599453f : -INFINITY;
+        } else {
+            float* pa = A.part_acc + (hq * A.nchunk + chunk) * D;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) pa[d0 + d] = o[d];
+            if ((tid & 15) == 0) A.part_ml[hq * A.nchunk + chunk] = make_float2(M, Lq);
+        }
+    }
+}
+
+// Joins the partials of the sequences of more than one chunk: a wave per query head.
+template <typename T, int D>
+__global__ __launch_bounds__(64) void paged_join(const PagedArgs A) {
+    typedef typename store_type<T>::type elem;
+    constexpr int E = D / 64;
+    const int64_t hq = blockIdx.x;
+    const int lane = threadIdx.x, b = (int)(hq / A.Hq);
+    int64_t len = A.lens[b];
+    const int S = (int)(len < 0 ? 0 : (len > A.max_len ? A.max_len : len));
+    if (S <= A.chunk) return;
+    const int n = (S + A.chunk - 1) / A.chunk;
+    const float2* ml = A.part_ml + hq * A.nchunk;
+    float M = -INFINITY;
+    for (int i = lane; i < n; i += 64) M = fmaxf(M, ml[i].x);
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) M = fmaxf(M, __shfl_xor(M, d));
+    float Lq = 0.f, o[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = 0.f;
+    const float* pa = A.part_acc + hq * A.nchunk * D + lane * E;
+    for (int i = 0; i < n; ++i) {
+        const float2 p = ml[i];
+        const float f = __builtin_amdgcn_exp2f(p.x - M);
+        Lq += p.y * f;
+#pragma unroll
+        for (int e = 0; e < E; ++e) o[e] += pa[(int64_t)i * D + e] * f;
+    }
+    elem* out = reinterpret_cast<elem*>(A.out) + hq * D + lane * E;
+#pragma unroll
+    for (int e = 0; e < E; ++e) out[e] = (elem)(Lq > 0.f ? o[e] / Lq : 0.f);
+    if (A.lse && lane == 0) A.lse[hq] = Lq > 0.f ? (M + __builtin_amdgcn_logf(Lq)) * 0.6931471805599453f : -INFINITY;
+}
+
+}  // namespace
+
+PagedPlan paged_plan(int B, int Hq, int Hkv, int D, int64_t max_len) {
+    const int64_t pairs = (int64_t)B * Hkv, keys = pairs * max_len;
+    int64_t chunk = (keys / 768 + 127) / 128 * 128;
+    chunk = std::max<int64_t>(256, std::min<int64_t>(chunk, 4096));
+    if (max_len <= 512) chunk = 512;
+    PagedPlan P;
+    P.chunk = (int)chunk;
+    P.nchunk = (int)((max_len + chunk - 1) / chunk);
+    const size_t heads = (size_t)B * Hq;
+    P.bytes = P.nchunk <= 1 ? 0 : ((heads * P.nchunk * D * sizeof(float) + 255) & ~(size_t)255) + heads * P.nchunk * sizeof(float2);
+    return P;
+}
+
+hipError_t launch_paged(int dtype, int D, PagedArgs A, void* workspace, hipStream_t st) {
+    const PagedPlan P = paged_plan(A.B, A.Hq, A.Hkv, D, A.max_len);
+    A.chunk = P.chunk;
+    A.nchunk = P.nchunk;
+    // r / page for 0 <= r < 2^31: with 2^(l-1) < page <= 2^l, ceil(2^(31+l) / page) fits 32 bits and its product's error stays
+    // below one part in r (page 1: 2^31 and a shift by 31)
+    int l = 0;
+    while (l < 31 && (1ll << l) < A.page) ++l;
+    A.page_magic = (unsigned)(((1ull << (31 + l)) + A.page - 1) / A.page);
+    A.page_shift = 31 + l;
+    A.scale2 = (float)(1.4426950408889634 / std::sqrt((double)D));
+    A.part_acc = nullptr;
+    A.part_ml = nullptr;
+    const size_t heads = (size_t)A.B * A.Hq;
+    if (P.nchunk > 1) {
+        A.part_acc = static_cast<float*>(workspace);
+        A.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + ((heads * P.nchunk * D * sizeof(float) + 255) & ~(size_t)255));
+    }
+    auto launch = [&](auto step, auto join) {
+        hipLaunchKernelGGL(step, dim3(P.nchunk, A.Hkv, A.B), dim3(kWaves * 64), 0, st, A);
+        if (P.nchunk > 1) hipLaunchKernelGGL(join, dim3((unsigned)heads), dim3(64), 0, st, A);
+    };
+    if (dtype == 0 && D == 128) launch(paged_attn<dec_bf16, 128>, paged_join<dec_bf16, 128>);
+    else if (dtype == 0 && D == 64) launch(paged_attn<dec_bf16, 64>, paged_join<dec_bf16, 64>);
+    else if (dtype == 2 && D == 128) launch(paged_attn<dec_f16, 128>, paged_join<dec_f16, 128>);
+    else if (dtype == 2 && D == 64) launch(paged_attn<dec_f16, 64>, paged_join<dec_f16, 64>);
+    else return hipErrorInvalidValue;
+    return hipGetLastError();
+}
+
+}  // namespace snapkv
