@@ -43,7 +43,7 @@ struct p_bf16 {
 struct p_f16 {
     typedef _Float16 elem;
     typedef pf16x8 frag;
-    static constexpr float kShift = 8.f;
+    static constexpr float kShift = 7.f;
 };
 __device__ __forceinline__ pfx16 mma32(pbf16x8 a, pbf16x8 b, pfx16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ pfx16 mma32(pf16x8 a, pf16x8 b, pfx16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
@@ -126,15 +126,20 @@ __device__ bool locate(const PromptArgs& A, int rank, int lane, int& seq, int& t
     return false;
 }
 
+// The other half of the wave: lane l gets lane l ^ 32's value.
+__device__ __forceinline__ float other_half(float x) {
+    const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float((threadIdx.x & 32) ? y[0] : y[1]);
+}
+
 template <typename T, int D, int WAVES>
-__global__ __launch_bounds__(WAVES * 64) void prompt_attn(const PromptArgs A) {
+__global__ __launch_bounds__(WAVES * 64, 2) void prompt_attn(const PromptArgs A) {
     typedef typename T::elem elem;
     typedef typename T::frag frag;
     constexpr int ROWS = WAVES * 32;            // query rows of a workgroup
     constexpr int ROW = D * 2, PIECES = D / 8;  // bytes and 16-byte pieces of a row
     constexpr int NC = D / 16, ND = D / 32;     // contraction steps of a logit; 32-column blocks of the output
-    __shared__ __align__(16) char s_k[kKeys * ROW];
-    __shared__ __align__(16) char s_v[kKeys * ROW];
+    __shared__ __align__(16) char s_k0[kKeys * ROW], s_v0[kKeys * ROW], s_k1[kKeys * ROW], s_v1[kKeys * ROW];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n32 = lane & 31, h2 = lane >> 5;
@@ -169,18 +174,18 @@ __global__ __launch_bounds__(WAVES * 64) void prompt_attn(const PromptArgs A) {
     const int last = min(len, (tile + 1) * ROWS) - 1;        // the last key any of the tile's rows sees
     const int ntiles = last / kKeys + 1;
     constexpr int PER = kKeys * PIECES / 64;                 // 1 KB loads of a tile
-    for (int kt = 0; kt < ntiles; ++kt) {
-        __syncthreads();                                     // the last tile has been read
+    auto load = [&](int kt, char* dk, char* dv) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < PER / WAVES; ++i) {
             const int at = (i * WAVES + wave) * 64;
             const int r = (at + lane) / PIECES, s = (at + lane) % PIECES;
             const int key = min(kt * kKeys + r, len - 1);
-            __builtin_amdgcn_global_load_lds((global_ptr)(kh + (int64_t)key * A.k_rs + k_slot<D>(r, s) * 16), (lds_ptr)(s_k + at * 16), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((global_ptr)(vh + (int64_t)key * A.v_rs + v_slot<D>(r, s) * 16), (lds_ptr)(s_v + at * 16), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((global_ptr)(kh + (int64_t)key * A.k_rs + k_slot<D>(r, s) * 16), (lds_ptr)(dk + at * 16), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((global_ptr)(vh + (int64_t)key * A.v_rs + v_slot<D>(r, s) * 16), (lds_ptr)(dv + at * 16), 16, 0, 0);
         }
-        __syncthreads();
-        if (kt * kKeys > row0 + 31) continue;                // all of it lies behind the wave's rows
+    };
+    auto step = [&](int kt, const char* s_k, const char* s_v) __attribute__((always_inline)) {
+        if (kt * kKeys > row0 + 31) return;                  // all of it lies behind the wave's rows
         pfx16 x[2];
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb) {
@@ -203,25 +208,30 @@ __global__ __launch_bounds__(WAVES * 64) void prompt_attn(const PromptArgs A) {
         float top = x[0][0];
 #pragma unroll
         for (int r = 1; r < 32; ++r) top = fmaxf(top, x[r / 16][r % 16]);
-        top = fmaxf(top, __shfl_xor(top, 32));
-        const float mn = fmaxf(m, top * A.scale2);           // finite: key 0 of the prompt is in the first tile
-        const float alpha = __builtin_amdgcn_exp2f(m - mn);
-        m = mn;
+        top = fmaxf(top, other_half(top)) * A.scale2;        // finite in the first tile: it holds the prompt's key 0
+        // The shift of the exponentials need not be the maximum itself: it is moved, and sums and outputs rescaled, only
+        // when some row of the wave has outgrown it by 2^8
+        if (__any(top > m + 8.f)) {
+            const float mn = fmaxf(m, top);
+            const float alpha = __builtin_amdgcn_exp2f(m - mn);
+            m = mn;
+            lsum *= alpha;
+#pragma unroll
+            for (int i = 0; i < ND; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[i][r] *= alpha;
+        }
         float sum = 0.f;
         frag pf[4];
 #pragma unroll
         for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[kb][r], A.scale2, T::kShift - mn));
+                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[kb][r], A.scale2, T::kShift - m));
                 sum += p;
                 pf[2 * kb + r / 8][r % 8] = (elem)p;
             }
-        lsum = lsum * alpha + sum;
-#pragma unroll
-        for (int i = 0; i < ND; ++i)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) acc[i][r] *= alpha;
+        lsum += sum;
 #pragma unroll
         for (int j = 0; j < 4; ++j) {                        // 16 keys
             const int kr = 16 * j + 4 * h2 + (lane & 15) / 4;
@@ -236,8 +246,19 @@ __global__ __launch_bounds__(WAVES * 64) void prompt_attn(const PromptArgs A) {
                 acc[i] = mma32(vf, pf[j], acc[i]);
             }
         }
+    };
+    load(0, s_k0, s_v0);
+    for (int kt = 0;;) {
+        __syncthreads();                                     // this tile has arrived, the other buffer has been read
+        if (kt + 1 < ntiles) load(kt + 1, s_k1, s_v1);
+        step(kt, s_k0, s_v0);
+        if (++kt >= ntiles) break;
+        __syncthreads();
+        if (kt + 1 < ntiles) load(kt + 1, s_k0, s_v0);
+        step(kt, s_k1, s_v1);
+        if (++kt >= ntiles) break;
     }
-    lsum += __shfl_xor(lsum, 32);
+    lsum += other_half(lsum);
     if (row < len) {
         const float inv = 1.f / lsum;
         elem* o = reinterpret_cast<elem*>(A.out) + ((int64_t)(begin + row) * A.Hq + hq) * D + 4 * h2;
