@@ -1332,6 +1332,7 @@ int snapkv_prompt_attention(int dtype, const void* q, const void* k, const void*
     }
     if (!aligned16(out) || (reinterpret_cast<uintptr_t>(out_lse) & 3u) != 0 || (reinterpret_cast<uintptr_t>(cu_seqlens) & 3u) != 0)
         return SNAPKV_ERR_MISALIGNED;
+    if (k_row_stride > 1 << 24 || v_row_stride > 1 << 24) return SNAPKV_ERR_UNSUPPORTED;   // offsets within a tile of 64 rows have 31 bits
     PromptArgs A{};
     A.q = static_cast<const char*>(q);
     A.k = static_cast<const char*>(k);

@@ -52,6 +52,7 @@ constexpr int kKeys = 64;      // keys of a tile
 
 typedef const __attribute__((address_space(1))) void* global_ptr;
 typedef __attribute__((address_space(3))) void* lds_ptr;
+typedef __attribute__((address_space(3))) char* lds_char;
 typedef __attribute__((address_space(3))) ps16x4* lds_s16x4;
 
 // Which 16-byte piece of its row an LDS slot of a tile holds: the pieces of a row are permuted so that the lanes of a read,
@@ -59,64 +60,53 @@ typedef __attribute__((address_space(3))) ps16x4* lds_s16x4;
 template <int D> __device__ __forceinline__ int k_slot(int row, int piece) { return piece ^ (row & (D / 8 - 1)); }
 template <int D> __device__ __forceinline__ int v_slot(int row, int piece) { return piece ^ ((row & (D / 32 - 1)) << 2); }
 
-// The tile of rank `rank` in descending order of its number of visible keys: sequence and row tile, or false.  A sequence
-// of n row tiles has one of each cost 1 .. n; F(c) counts the tiles of cost c and more.
+// The row tile of rank `rank` when all are in descending order of their number of visible keys, so that the long ones start
+// first: its sequence's first token and length, and which tile of it; false behind the last.  A sequence of n tiles has one of
+// each cost 1 .. n, so F(c) = sum over sequences of max(0, n - c + 1) tiles cost c or more, and the tile's cost is the largest
+// c with F(c) > rank.  Every lane counts another c, 63 of them and one beyond the range at a time, over the sequences one by one.
 template <int ROWS>
-__device__ bool locate(const PromptArgs& A, int rank, int lane, int& seq, int& tile, int& begin, int& len) {
-    auto span = [&](int b, int& s0, int& n) {
-        s0 = 0;
-        n = 0;
+__device__ __forceinline__ bool locate(const PromptArgs& A, int rank, int lane, int& begin, int& len, int& tile) {
+    int from, n;
+    auto span = [&](int b) __attribute__((always_inline)) {          // of the lane's sequence: first token, tokens; returns tiles
+        from = n = 0;
         if (b < A.B) {
-            const int a = A.cu[b], e = A.cu[b + 1];
-            s0 = a < 0 ? 0 : a;
-            const int e1 = e > A.T ? (int)A.T : e;
-            n = e1 > s0 ? e1 - s0 : 0;
+            from = max(A.cu[b], 0);
+            n = max((int)min((int64_t)A.cu[b + 1], A.T) - from, 0);
         }
+        return (n + ROWS - 1) / ROWS;
     };
     int most = 0, total = 0;
     for (int b0 = 0; b0 < A.B; b0 += 64) {
-        int s0, n;
-        span(b0 + lane, s0, n);
-        const int nt = (n + ROWS - 1) / ROWS;
-        int x = nt, t = nt;
-#pragma unroll
-        for (int d = 32; d >= 1; d >>= 1) {
-            x = max(x, __shfl_xor(x, d));
-            t += __shfl_xor(t, d);
+        const int nt = span(b0 + lane);
+        for (int i = 0; i < min(64, A.B - b0); ++i) {
+            const int x = __builtin_amdgcn_readlane(nt, i);
+            most = max(most, x);
+            total += x;
         }
-        most = max(most, x);
-        total += t;
     }
     if (rank >= total) return false;
-    auto count = [&](int c) {                              // F(c)
-        int t = 0;
+    int lo = 1, width = most, after = 0;                             // F(lo) > rank >= F(lo + width); after = F(lo + 1) at the end
+    for (bool more = true; more;) {
+        const int w = (width + 62) / 63, c = lo + lane * w;
+        int f = 0;
         for (int b0 = 0; b0 < A.B; b0 += 64) {
-            int s0, n;
-            span(b0 + lane, s0, n);
-            const int nt = (n + ROWS - 1) / ROWS;
-            t += max(0, nt - c + 1);
+            const int nt = span(b0 + lane);
+            for (int i = 0; i < min(64, A.B - b0); ++i) f += max(__builtin_amdgcn_readlane(nt, i) - c + 1, 0);
         }
-#pragma unroll
-        for (int d = 32; d >= 1; d >>= 1) t += __shfl_xor(t, d);
-        return t;
-    };
-    int lo = 1, hi = most + 1;                             // F(lo) > rank >= F(hi)
-    while (hi - lo > 1) {
-        const int c = (lo + hi) / 2;
-        if (count(c) > rank) lo = c; else hi = c;
+        const int k = __popcll(__ballot(f > rank));                  // (at least 1, at most 63)
+        after = __builtin_amdgcn_readlane(f, k);
+        lo += (k - 1) * w;
+        width = w;
+        more = w > 1;
     }
-    int within = rank - count(lo + 1);
+    int within = rank - after;                                       // which of the sequences of lo tiles or more
     for (int b0 = 0; b0 < A.B; b0 += 64) {
-        int s0, n;
-        span(b0 + lane, s0, n);
-        const unsigned long long has = __ballot((n + ROWS - 1) / ROWS >= lo);
+        unsigned long long has = __ballot(span(b0 + lane) >= lo);
         const int here = __popcll(has);
         if (within < here) {
-            unsigned long long rest = has;
-            for (int i = 0; i < within; ++i) rest &= rest - 1;
-            const int l = __ffsll((long long)rest) - 1;
-            seq = b0 + l;
-            begin = __builtin_amdgcn_readlane(s0, l);
+            for (; within > 0; --within) has &= has - 1;
+            const int l = __ffsll((long long)has) - 1;
+            begin = __builtin_amdgcn_readlane(from, l);
             len = __builtin_amdgcn_readlane(n, l);
             tile = lo - 1;
             return true;
@@ -139,7 +129,8 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_attn(const PromptArgs A)
     constexpr int ROWS = WAVES * 32;            // query rows of a workgroup
     constexpr int ROW = D * 2, PIECES = D / 8;  // bytes and 16-byte pieces of a row
     constexpr int NC = D / 16, ND = D / 32;     // contraction steps of a logit; 32-column blocks of the output
-    __shared__ __align__(16) char s_k0[kKeys * ROW], s_v0[kKeys * ROW], s_k1[kKeys * ROW], s_v1[kKeys * ROW];
+    __shared__ __align__(16) char m_k0[kKeys * ROW], m_v0[kKeys * ROW], m_k1[kKeys * ROW], m_v1[kKeys * ROW];
+    const lds_char s_k0 = (lds_char)m_k0, s_v0 = (lds_char)m_v0, s_k1 = (lds_char)m_k1, s_v1 = (lds_char)m_v1;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n32 = lane & 31, h2 = lane >> 5;
@@ -151,18 +142,17 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_attn(const PromptArgs A)
     const int kvh = blockIdx.x % m8 + m8 * (rest / per);
     const int rank = rest % per / A.g, hq = kvh * A.g + rest % A.g;
 
-    int seq, tile, begin, len;
-    if (!locate<ROWS>(A, rank, lane, seq, tile, begin, len)) return;
+    int tile, begin, len;
+    if (!locate<ROWS>(A, rank, lane, begin, len, tile)) return;
 
-    const int row0 = tile * ROWS + wave * 32;               // the wave's first query row within the prompt
-    const int row = row0 + n32, row_in = row < len ? row : len - 1;
+    const int row0 = tile * ROWS + wave * 32;                // the wave's first query row within the prompt
+    const int row = row0 + n32;
     frag qf[NC];
-    {
-        const char* qr = A.q + (int64_t)(begin + row_in) * A.q_rs + (int64_t)hq * A.q_hs + h2 * 16;
+    const char* qr = A.q + (int64_t)(begin + min(row, len - 1)) * A.q_rs + (int64_t)hq * A.q_hs + h2 * 16;
 #pragma unroll
-        for (int c = 0; c < NC; ++c) qf[c] = *reinterpret_cast<const frag*>(qr + 32 * c);
-    }
-    float m = -INFINITY, lsum = 0.f;
+    for (int c = 0; c < NC; ++c) qf[c] = *reinterpret_cast<const frag*>(qr + 32 * c);
+    float m = -INFINITY, limit = -INFINITY;                  // the shift of the exponentials; the largest logit, unscaled, it is good for
+    float lsum = 0.f, lsum2 = 0.f;                           // (two sums: shorter chains)
     pfx16 acc[ND];
 #pragma unroll
     for (int i = 0; i < ND; ++i)
@@ -173,123 +163,197 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_attn(const PromptArgs A)
     const char* vh = A.v + (int64_t)kvh * A.v_hs + (int64_t)begin * A.v_rs;
     const int last = min(len, (tile + 1) * ROWS) - 1;        // the last key any of the tile's rows sees
     const int ntiles = last / kKeys + 1;
-    constexpr int PER = kKeys * PIECES / 64;                 // 1 KB loads of a tile
-    auto load = [&](int kt, char* dk, char* dv) __attribute__((always_inline)) {
+    const int mine = row0 < len ? row0 / 32 + 1 : 0;         // blocks of 32 keys that the wave's rows see; the last one in part
+
+    // Loads of a tile: WAVES KB at a time, a KB (RPL rows) per wave, straight into LDS.  The rows of a lane's loads differ by a number
+    // that does not change its place in the permutation.  Addresses are a uniform 64-bit one of the tile's first row and
+    // 32-bit offsets of at most 63 rows, never negative.
+    constexpr int RPL = 1024 / ROW, PER = kKeys / (RPL * WAVES);
+    static_assert(RPL * WAVES % PIECES == 0, "a lane's rows share a permutation");
+    const int lr = wave * RPL + lane / PIECES;
+    const int k_piece = k_slot<D>(lr, lane % PIECES) * 16, v_piece = v_slot<D>(lr, lane % PIECES) * 16;
+    const int k_off = lr * (int)A.k_rs + k_piece, v_off = lr * (int)A.v_rs + v_piece;
+    auto load = [&](const char* base, int rs, int off, int piece, int first, lds_char to) __attribute__((always_inline)) {
+        const int at = min(first, len - 1);
+        const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base) + (int64_t)at * rs, 0, -1, 0x00020000);
+        if (first + kKeys <= len) {
 #pragma unroll
-        for (int i = 0; i < PER / WAVES; ++i) {
-            const int at = (i * WAVES + wave) * 64;
-            const int r = (at + lane) / PIECES, s = (at + lane) % PIECES;
-            const int key = min(kt * kKeys + r, len - 1);
-            __builtin_amdgcn_global_load_lds((global_ptr)(kh + (int64_t)key * A.k_rs + k_slot<D>(r, s) * 16), (lds_ptr)(dk + at * 16), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((global_ptr)(vh + (int64_t)key * A.v_rs + v_slot<D>(r, s) * 16), (lds_ptr)(dv + at * 16), 16, 0, 0);
-        }
-    };
-    auto step = [&](int kt, const char* s_k, const char* s_v) __attribute__((always_inline)) {
-        if (kt * kKeys > row0 + 31) return;                  // all of it lies behind the wave's rows
-        pfx16 x[2];
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) x[kb][r] = 0.f;
-#pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                const int kr = 32 * kb + n32;
-                const frag kf = *reinterpret_cast<const frag*>(s_k + kr * ROW + k_slot<D>(kr, 2 * c + h2) * 16);
-                x[kb] = mma32(kf, qf[c], x[kb]);
+            for (int i = 0; i < PER; ++i)
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_ptr)(to + (i * WAVES + wave) * 1024), 16, off, i * RPL * WAVES * rs, 0, 0);
+        } else {                                             // rows behind the prompt: its last row again
+            for (int i = 0; i < PER; ++i) {
+                const int down = min(first + i * RPL * WAVES + lr, len - 1) - at;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_ptr)(to + (i * WAVES + wave) * 1024), 16, down * rs + piece, 0, 0, 0);
             }
         }
-        if (kt * kKeys + kKeys - 1 > row0) {                 // keys behind a row are hidden from it (and those behind the prompt)
+    };
+
+    // A lane's places in a tile: its pieces of key row n32 (the 32 rows below have the same permutation), and of the first value
+    // row that it transposes (so have those 8 and 16 below).
+    int k_at[NC], v_at[ND];
 #pragma unroll
-            for (int kb = 0; kb < 2; ++kb)
+    for (int c = 0; c < NC; ++c) k_at[c] = n32 * ROW + k_slot<D>(n32, 2 * c + h2) * 16;
 #pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (kt * kKeys + 32 * kb + 8 * (r / 4) + 4 * h2 + r % 4 > row) x[kb][r] = -INFINITY;
-        }
-        float top = x[0][0];
+    for (int i = 0; i < ND; ++i) {
+        const int vr = 4 * h2 + (lane & 15) / 4;
+        v_at[i] = vr * ROW + v_slot<D>(vr, 4 * i + 2 * ((lane >> 4) & 1) + (lane & 3) / 2) * 16 + (lane & 1) * 8;
+    }
+    // Operands of product i of a block of 32 keys: of its logits, of its part of the output (16 keys of 32 columns, transposed).
+    constexpr int NQ = NC, NV = 2 * ND;
+    auto k_frag = [&](lds_char s_k, int i) __attribute__((always_inline)) {
+        return *reinterpret_cast<const __attribute__((address_space(3))) frag*>(s_k + k_at[i]);
+    };
+    auto v_frag = [&](lds_char s_v, int i) __attribute__((always_inline)) {
+        lds_char at = s_v + v_at[i % ND] + 16 * ROW * (i / ND);
+        const ps16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)at);
+        const ps16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(at + 8 * ROW));
+        return __builtin_bit_cast(frag, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+    };
+    auto product = [&](frag kf, int i, pfx16& x) __attribute__((always_inline)) {          // product i of a block's logits
+        pfx16 z;
 #pragma unroll
-        for (int r = 1; r < 32; ++r) top = fmaxf(top, x[r / 16][r % 16]);
-        top = fmaxf(top, other_half(top)) * A.scale2;        // finite in the first tile: it holds the prompt's key 0
-        // The shift of the exponentials need not be the maximum itself: it is moved, and sums and outputs rescaled, only
-        // when some row of the wave has outgrown it by 2^8
-        if (__any(top > m + 8.f)) {
-            const float mn = fmaxf(m, top);
+        for (int r = 0; r < 16; ++r) z[r] = 0.f;
+        x = mma32(kf, qf[i], i == 0 ? z : x);
+    };
+    // Logits of block b that lie behind their row, and so those behind the prompt, are hidden.
+    auto hide = [&](int b, pfx16& x) __attribute__((always_inline)) {
+        if (b < mine - 1) return;
+        const int seen = row - b * 32 - 4 * h2;
+#pragma unroll
+        for (int r = 0; r < 16; ++r)
+            if (8 * (r / 4) + r % 4 > seen) x[r] = -INFINITY;
+    };
+    // The shift of the exponentials need not be the maximum itself: it is moved, and sums and outputs rescaled, only when
+    // some row of the wave has outgrown it by 2^8.
+    auto rescale = [&](float big) __attribute__((always_inline)) {
+        if (__any(big > limit)) {
+            const float mn = fmaxf(m, fmaxf(big, other_half(big)) * A.scale2);     // finite: key 0 is in the first block
             const float alpha = __builtin_amdgcn_exp2f(m - mn);
             m = mn;
+            limit = (mn + 8.f) / A.scale2;
             lsum *= alpha;
+            lsum2 *= alpha;
 #pragma unroll
             for (int i = 0; i < ND; ++i)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) acc[i][r] *= alpha;
         }
-        float sum = 0.f;
-        frag pf[4];
+    };
+    // The probabilities of logits 2 n and 2 n + 1 of a lane's 16.
+    auto two = [&](const pfx16& x, int n, float shift, frag* pf) __attribute__((always_inline)) {
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[2 * n], A.scale2, shift));
+        const float q = __builtin_amdgcn_exp2f(__builtin_fmaf(x[2 * n + 1], A.scale2, shift));
+        lsum += p;
+        lsum2 += q;
+        pf[n / 4][2 * n % 8] = (elem)p;
+        pf[n / 4][2 * n % 8 + 1] = (elem)q;
+    };
+    // Software pipeline: the logits of block b + 1 are products that nothing of block b's softmax waits for, so between two
+    // matrix instructions stand a few of the softmax's.  Operands are read from LDS AHEAD products before their own.
+    constexpr int AHEAD = 3, PAIRS = 8, EARLY = 5;
+    float big;
+    pfx16 xa, xb;
+    auto pass = [&](int b, const pfx16& x, pfx16& xn, lds_char k_next, lds_char v_now) __attribute__((always_inline)) {
+        if (b >= mine) return;
+        frag pf[2], kf[NQ], vf[NV];
 #pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
+        for (int i = 0; i < AHEAD; ++i) kf[i] = k_frag(k_next, i);
+        rescale(big);
+        const float shift = T::kShift - m;
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[kb][r], A.scale2, T::kShift - m));
-                sum += p;
-                pf[2 * kb + r / 8][r % 8] = (elem)p;
-            }
-        lsum += sum;
+        for (int i = 0; i < NQ; ++i) {
+            if (i + AHEAD < NQ) kf[i + AHEAD] = k_frag(k_next, i + AHEAD);
+            else vf[i + AHEAD - NQ] = v_frag(v_now, i + AHEAD - NQ);
+            product(kf[i], i, xn);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {                        // 16 keys
-            const int kr = 16 * j + 4 * h2 + (lane & 15) / 4;
+            for (int n = i * EARLY / NQ; n < (i + 1) * EARLY / NQ; ++n) two(x, n, shift, pf);
+            __builtin_amdgcn_sched_barrier(0);
+        }
 #pragma unroll
-            for (int i = 0; i < ND; ++i) {
-                const int piece = 4 * i + 2 * ((lane >> 4) & 1) + (lane & 3) / 2;
-                const char* a0 = s_v + kr * ROW + v_slot<D>(kr, piece) * 16 + (lane & 1) * 8;
-                const char* a1 = s_v + (kr + 8) * ROW + v_slot<D>(kr + 8, piece) * 16 + (lane & 1) * 8;
-                const ps16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)a0);
-                const ps16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)a1);
-                const frag vf = __builtin_bit_cast(frag, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-                acc[i] = mma32(vf, pf[j], acc[i]);
-            }
+        for (int i = 0; i < ND; ++i) {
+            if (i + AHEAD < NV) vf[i + AHEAD] = v_frag(v_now, i + AHEAD);
+            acc[i] = mma32(vf[i], pf[0], acc[i]);
+#pragma unroll
+            for (int n = EARLY + i * (PAIRS - EARLY) / ND; n < EARLY + (i + 1) * (PAIRS - EARLY) / ND; ++n) two(x, n, shift, pf);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        hide(b + 1, xn);
+        __builtin_amdgcn_sched_barrier(0);
+        big = xn[0];
+#pragma unroll
+        for (int i = 0; i < ND; ++i) {
+            if (ND + i + AHEAD < NV) vf[ND + i + AHEAD] = v_frag(v_now, ND + i + AHEAD);
+            acc[i] = mma32(vf[ND + i], pf[1], acc[i]);
+#pragma unroll
+            for (int r = i * 16 / ND; r < (i + 1) * 16 / ND; ++r) big = fmaxf(big, xn[r]);
+            __builtin_amdgcn_sched_barrier(0);
         }
     };
-    load(0, s_k0, s_v0);
-    for (int kt = 0;;) {
-        __syncthreads();                                     // this tile has arrived, the other buffer has been read
-        if (kt + 1 < ntiles) load(kt + 1, s_k1, s_v1);
-        step(kt, s_k0, s_v0);
-        if (++kt >= ntiles) break;
-        __syncthreads();
-        if (kt + 1 < ntiles) load(kt + 1, s_k0, s_v0);
-        step(kt, s_k1, s_v1);
-        if (++kt >= ntiles) break;
+    // Keys are half a tile ahead of values: tile t of V is blocks 2 t and 2 t + 1, that of K blocks 2 t + 1 and 2 t + 2, whose logits
+    // are taken meanwhile.  The next tiles arrive in the other two buffers.
+    auto two_blocks = [&](int t, lds_char k_now, lds_char k_free, lds_char v_now, lds_char v_free) __attribute__((always_inline)) {
+        __syncthreads();                                     // these tiles have arrived, the others have been read
+        // (a lane's places are kept as they are, and a buffer's address is the constant offset of a read: sums of the two,
+        // made once in front of the loop, would take 24 registers)
+#pragma unroll
+        for (int c = 0; c < NC; ++c) asm volatile("" : "+v"(k_at[c]));
+#pragma unroll
+        for (int i = 0; i < ND; ++i) asm volatile("" : "+v"(v_at[i]));
+        if (t + 1 < ntiles) {
+            load(kh, (int)A.k_rs, k_off, k_piece, (t + 1) * kKeys + 32, k_free);
+            load(vh, (int)A.v_rs, v_off, v_piece, (t + 1) * kKeys, v_free);
+        }
+        pass(2 * t, xa, xb, k_now, v_now);
+        pass(2 * t + 1, xb, xa, k_now + 32 * ROW, v_now + 32 * ROW);
+    };
+    load(kh, (int)A.k_rs, k_off, k_piece, 0, s_k1);
+    load(kh, (int)A.k_rs, k_off, k_piece, 32, s_k0);
+    load(vh, (int)A.v_rs, v_off, v_piece, 0, s_v0);
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NQ; ++i) product(k_frag(s_k1, i), i, xa);
+    hide(0, xa);
+    big = xa[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) big = fmaxf(big, xa[r]);
+    for (int t = 0;;) {
+        two_blocks(t, s_k0, s_k1, s_v0, s_v1);
+        if (++t >= ntiles) break;
+        two_blocks(t, s_k1, s_k0, s_v1, s_v0);
+        if (++t >= ntiles) break;
     }
-    lsum += other_half(lsum);
-    if (row < len) {
-        const float inv = 1.f / lsum;
-        elem* o = reinterpret_cast<elem*>(A.out) + ((int64_t)(begin + row) * A.Hq + hq) * D + 4 * h2;
+    float sum = lsum + lsum2;
+    sum += other_half(sum);
+    if (row >= len) return;
+    const float inv = 1.f / sum;
+    elem* o = reinterpret_cast<elem*>(A.out) + ((int64_t)(begin + row) * A.Hq + hq) * D + 4 * h2;
 #pragma unroll
-        for (int i = 0; i < ND; ++i)
+    for (int i = 0; i < ND; ++i)
 #pragma unroll
-            for (int r4 = 0; r4 < 4; ++r4) {
-                typedef __attribute__((ext_vector_type(4))) elem elem4;
-                elem4 y;
+        for (int r4 = 0; r4 < 4; ++r4) {
+            typedef __attribute__((ext_vector_type(4))) elem elem4;
+            elem4 y;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) y[r] = (elem)(acc[i][4 * r4 + r] * inv);
-                *reinterpret_cast<elem4*>(o + 32 * i + 8 * r4) = y;
-            }
-        if (A.lse && h2 == 0)
-            A.lse[(int64_t)hq * A.T + begin + row] = (m - T::kShift + __builtin_amdgcn_logf(lsum)) * 0.6931471805599453f;
-    }
+            for (int r = 0; r < 4; ++r) y[r] = (elem)(acc[i][4 * r4 + r] * inv);
+            *reinterpret_cast<elem4*>(o + 32 * i + 8 * r4) = y;
+        }
+    if (A.lse && h2 == 0)
+        A.lse[(int64_t)hq * A.T + begin + row] = (m - T::kShift + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
 }
 
 }  // namespace
 
 hipError_t launch_prompt(int dtype, int D, PromptArgs A, hipStream_t st) {
     A.scale2 = (float)(1.4426950408889634 / std::sqrt((double)D));
-    constexpr int WAVES = 4, ROWS = WAVES * 32;
-    A.ranks = (int)(A.T / ROWS) + A.B;                       // every prompt has at most one tile that is not full
+    constexpr int WAVES = 4;
+    constexpr int rows = WAVES * 32;
+    A.ranks = (int)(A.T / rows) + A.B;                       // every prompt has at most one tile that is not full
     const int64_t groups = (int64_t)A.ranks * A.Hq;
     if (groups >= (int64_t)1 << 31) return hipErrorInvalidValue;
     auto launch = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)groups), dim3(WAVES * 64), 0, st, A); };
-    if (dtype == 0 && D == 128) launch(prompt_attn<p_bf16, 128, WAVES>);
-    else if (dtype == 0 && D == 64) launch(prompt_attn<p_bf16, 64, WAVES>);
-    else if (dtype == 2 && D == 128) launch(prompt_attn<p_f16, 128, WAVES>);
-    else if (dtype == 2 && D == 64) launch(prompt_attn<p_f16, 64, WAVES>);
+    if (dtype == 0) D == 128 ? launch(prompt_attn<p_bf16, 128, WAVES>) : launch(prompt_attn<p_bf16, 64, WAVES>);
+    else if (dtype == 2) D == 128 ? launch(prompt_attn<p_f16, 128, WAVES>) : launch(prompt_attn<p_f16, 64, WAVES>);
     else return hipErrorInvalidValue;
     return hipGetLastError();
 }

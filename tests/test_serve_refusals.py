@@ -45,7 +45,7 @@ def prompt(**kw):
     (dict(T=0), 0), (dict(B=0), 0), (dict(dtype=-1), -1), (dict(T=-1), -1), (dict(B=-2), -1), (dict(Hq=0), -1), (dict(Hkv=0), -1),
     (dict(Hq=9), -1), (dict(q=None), -1), (dict(k=None), -1), (dict(v=None), -1), (dict(cu=None), -1), (dict(out=None), -1),
     (dict(qr=127), -1), (dict(kh=-1), -1), (dict(dtype=1), -2), (dict(D=96), -2), (dict(D=32), -2), (dict(T=1 << 30), -2),
-    (dict(Hq=65536, Hkv=65536), -2), (dict(q=ODD), -3), (dict(k=ODD), -3), (dict(v=ODD), -3), (dict(out=ODD), -3), (dict(lse=0x1002), -3),
+    (dict(Hq=65536, Hkv=65536), -2), (dict(kr=(1 << 24) + 8), -2), (dict(vr=(1 << 24) + 8), -2), (dict(q=ODD), -3), (dict(k=ODD), -3), (dict(v=ODD), -3), (dict(out=ODD), -3), (dict(lse=0x1002), -3),
     (dict(cu=0x1002), -3), (dict(qr=1028), -3), (dict(vh=4), -3),
 ])
 def test_prompt_attention_refuses(kw, code):
