@@ -116,6 +116,13 @@ __device__ __forceinline__ bool locate(const PromptArgs& A, int rank, int lane, 
     return false;
 }
 
+// All waves are done with what they read and what they fetched straight into LDS has arrived.  The wait is explicit: those
+// loads write no register that the compiler would wait for, and a barrier alone does not.
+__device__ __forceinline__ void tiles_ready() {
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+}
+
 // The other half of the wave: lane l gets lane l ^ 32's value.
 __device__ __forceinline__ float other_half(float x) {
     const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
@@ -293,7 +300,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_attn(const PromptArgs A)
     // Keys are half a tile ahead of values: tile t of V is blocks 2 t and 2 t + 1, that of K blocks 2 t + 1 and 2 t + 2, whose logits
     // are taken meanwhile.  The next tiles arrive in the other two buffers.
     auto two_blocks = [&](int t, lds_char k_now, lds_char k_free, lds_char v_now, lds_char v_free) __attribute__((always_inline)) {
-        __syncthreads();                                     // these tiles have arrived, the others have been read
+        tiles_ready();
         // (a lane's places are kept as they are, and a buffer's address is the constant offset of a read: sums of the two,
         // made once in front of the loop, would take 24 registers)
 #pragma unroll
@@ -310,7 +317,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_attn(const PromptArgs A)
     load(kh, (int)A.k_rs, k_off, k_piece, 0, s_k1);
     load(kh, (int)A.k_rs, k_off, k_piece, 32, s_k0);
     load(vh, (int)A.v_rs, v_off, v_piece, 0, s_v0);
-    __syncthreads();
+    tiles_ready();
 #pragma unroll
     for (int i = 0; i < NQ; ++i) product(k_frag(s_k1, i), i, xa);
     hide(0, xa);
