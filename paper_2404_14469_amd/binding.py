@@ -504,24 +504,41 @@ def snapkv_decode_attention(q: torch.Tensor, k_cache: torch.Tensor, v_cache: tor
         _stream(stream)))
 
 
-def _rows(t: torch.Tensor, name: str, dtype):
-    """Address and (row, head) strides of a [T, heads, D] view with contiguous rows; the stride of a dimension of one
+# The steps below are called once per layer and token: their checks are a few comparisons per tensor.
+def _at(t: torch.Tensor, name: str, dtype, device: int) -> int:
+    """Address of a contiguous tensor of this type on this device."""
+    if t.get_device() != device or t.dtype is not dtype or not t.is_contiguous():
+        _wrong(t, name, dtype, device)
+    return t.data_ptr()
+
+
+def _rows(t: torch.Tensor, name: str, dtype, device: int, T: int, H: int, D: int):
+    """Address and (row, head) strides of a [T, H, D] view with contiguous rows; the stride of a dimension of one
     does not matter."""
+    rs, hs, es = t.stride()
+    if t.get_device() != device or t.dtype is not dtype or es != 1:
+        _wrong(t, name, dtype, device)
+    return t.data_ptr(), rs if T > 1 else D, hs if H > 1 else 0
+
+
+def _wrong(t, name, dtype, device):
     if not t.is_cuda:
         raise ValueError(f"{name} must be a GPU tensor")
-    if t.dtype != dtype:
+    if t.get_device() != device:
+        raise ValueError(f"{name} is on cuda:{t.get_device()}, other tensors of the call on cuda:{device}")
+    if t.dtype is not dtype:
         raise ValueError(f"{name} must be {dtype}, got {t.dtype}")
-    T, H, D = t.shape
-    if D > 1 and t.stride(2) != 1:
-        raise ValueError(f"the rows of {name} must be contiguous")
-    return t.data_ptr(), t.stride(0) if T > 1 else D, t.stride(1) if H > 1 else 0
+    raise ValueError(f"{name} must be contiguous (its rows, where strides are allowed)")
 
 
-def _on_current_device(*tensors) -> None:
-    """A call runs on the current device, on a stream of it: tensors of another one are refused."""
-    for t in tensors:
-        if t is not None and t.is_cuda and t.get_device() != torch.cuda.current_device():
-            raise ValueError(f"tensors are on cuda:{t.get_device()}, the current device is cuda:{torch.cuda.current_device()}")
+def _device_of(t: torch.Tensor, name: str) -> int:
+    """The device of a call's tensors.  Calls run on the current device, on a stream of it: no other is taken."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor")
+    device = t.get_device()
+    if device != torch.cuda.current_device():
+        raise ValueError(f"{name} is on cuda:{device}, the current device is cuda:{torch.cuda.current_device()}")
+    return device
 
 
 def snapkv_append_paged(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
@@ -536,14 +553,14 @@ def snapkv_append_paged(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor,
     lib = load()
     T, Hkv, D = k.shape
     num_pages, page_size, Hp, Dp = k_pages.shape
-    if tuple(v.shape) != (T, Hkv, D) or (Hp, Dp) != (Hkv, D) or v_pages.shape != k_pages.shape:
+    if v.shape != k.shape or Hp != Hkv or Dp != D or v_pages.shape != k_pages.shape:
         raise ValueError("k, v, k_pages and v_pages disagree on their shapes")
-    if block_table.dim() != 2 or tuple(starts.shape) != (block_table.shape[0],):
+    if block_table.dim() != 2 or starts.shape != block_table.shape[:1]:
         raise ValueError("block_table must be [B, columns] and starts [B]")
-    B = block_table.shape[0]
-    if cu_seqlens is not None and tuple(cu_seqlens.shape) != (B + 1,):
+    B, columns = block_table.shape
+    if cu_seqlens is not None and cu_seqlens.shape != (B + 1,):
         raise ValueError("cu_seqlens must be [B + 1]")
-    if positions is not None and tuple(positions.shape) != (T,):
+    if positions is not None and positions.shape != (T,):
         raise ValueError("positions must be [T]")
     if (cos is None) != (sin is None) or (cos is not None and (cos.dim() != 2 or cos.shape != sin.shape)):
         raise ValueError("cos and sin must both be [positions, rot_dim / 2]")
@@ -551,21 +568,22 @@ def snapkv_append_paged(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor,
         raise ValueError("q and q_out must both be [T, Hq, D]")
     if k_out is not None and k_out.shape != k.shape:
         raise ValueError("k_out must be [T, Hkv, D]")
-    _on_current_device(k, v, k_pages, v_pages, block_table, starts, cu_seqlens, positions, cos, sin, q, q_out, k_out)
-    code, dt, none = _dtype_code(k), k.dtype, (None, 0, 0)
-    int_of = lambda t, name: _dev(t, name, torch.int32) if t is not None else None
-    qp, qr, qh = _rows(q, "q", dt) if q is not None else none
-    op, orow, oh = _rows(q_out, "q_out", dt) if q_out is not None else none
-    cp, cr, ch = _rows(k_out, "k_out", dt) if k_out is not None else none
-    kp, kr, kh = _rows(k, "k", dt)
-    vp, vr, vh = _rows(v, "v", dt)
+    dev, dt, none, i32 = _device_of(k, "k"), k.dtype, (None, 0, 0), torch.int32
+    Hq = q.shape[1] if q is not None else 0
+    kp, kr, kh = _rows(k, "k", dt, dev, T, Hkv, D)
+    vp, vr, vh = _rows(v, "v", dt, dev, T, Hkv, D)
+    qp, qr, qh = _rows(q, "q", dt, dev, T, Hq, D) if Hq else none
+    op, orow, oh = _rows(q_out, "q_out", dt, dev, T, Hq, D) if Hq else none
+    cp, cr, ch = _rows(k_out, "k_out", dt, dev, T, Hkv, D) if k_out is not None else none
+    P, half = cos.shape if cos is not None else (0, 0)
     _check(lib.snapkv_append_paged(
-        code, qp, kp, vp, int_of(cu_seqlens, "cu_seqlens"), int_of(starts, "starts"), int_of(positions, "positions"), T, B,
-        q.shape[1] if q is not None else 0, Hkv, D, qr, qh, kr, kh, vr, vh,
-        _dev(cos, "cos", torch.float32) if cos is not None else None, _dev(sin, "sin", torch.float32) if sin is not None else None,
-        cos.shape[0] if cos is not None else 0, 2 * cos.shape[1] if cos is not None else 0, int(bool(interleaved)),
-        _dev(k_pages, "k_pages", dt), _dev(v_pages, "v_pages", dt), _dev(block_table, "block_table", torch.int32),
-        block_table.shape[1], num_pages, page_size, op, orow, oh, cp, cr, ch, _stream(stream)))
+        _dtype_code(k), qp, kp, vp, _at(cu_seqlens, "cu_seqlens", i32, dev) if cu_seqlens is not None else None,
+        _at(starts, "starts", i32, dev), _at(positions, "positions", i32, dev) if positions is not None else None, T, B,
+        Hq, Hkv, D, qr, qh, kr, kh, vr, vh,
+        _at(cos, "cos", torch.float32, dev) if cos is not None else None, _at(sin, "sin", torch.float32, dev) if cos is not None else None,
+        P, 2 * half, 1 if interleaved else 0,
+        _at(k_pages, "k_pages", dt, dev), _at(v_pages, "v_pages", dt, dev), _at(block_table, "block_table", i32, dev),
+        columns, num_pages, page_size, op, orow, oh, cp, cr, ch, _stream(stream)))
 
 
 def snapkv_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqlens: torch.Tensor, out: torch.Tensor,
@@ -577,18 +595,18 @@ def snapkv_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, c
     Tk, Hkv, Dk = k.shape
     if (Tk, Dk) != (T, D) or v.shape != k.shape:
         raise ValueError("q, k and v disagree on their shapes")
-    if out.shape != q.shape or (out_lse is not None and tuple(out_lse.shape) != (Hq, T)):
+    if out.shape != q.shape or (out_lse is not None and out_lse.shape != (Hq, T)):
         raise ValueError("out must be [T, Hq, D] and out_lse [Hq, T]")
     if cu_seqlens.dim() != 1 or cu_seqlens.numel() < 1:
         raise ValueError("cu_seqlens must be [B + 1]")
-    _on_current_device(q, k, v, cu_seqlens, out, out_lse)
-    code, dt = _dtype_code(q), q.dtype
-    qp, qr, qh = _rows(q, "q", dt)
-    kp, kr, kh = _rows(k, "k", dt)
-    vp, vr, vh = _rows(v, "v", dt)
+    dev, dt = _device_of(q, "q"), q.dtype
+    qp, qr, qh = _rows(q, "q", dt, dev, T, Hq, D)
+    kp, kr, kh = _rows(k, "k", dt, dev, T, Hkv, D)
+    vp, vr, vh = _rows(v, "v", dt, dev, T, Hkv, D)
     _check(lib.snapkv_prompt_attention(
-        code, qp, kp, vp, _dev(cu_seqlens, "cu_seqlens", torch.int32), cu_seqlens.numel() - 1, T, Hq, Hkv, D, qr, qh, kr, kh,
-        vr, vh, _dev(out, "out", dt), _dev(out_lse, "out_lse", torch.float32) if out_lse is not None else None, _stream(stream)))
+        _dtype_code(q), qp, kp, vp, _at(cu_seqlens, "cu_seqlens", torch.int32, dev), cu_seqlens.shape[0] - 1, T, Hq, Hkv, D,
+        qr, qh, kr, kh, vr, vh, _at(out, "out", dt, dev),
+        _at(out_lse, "out_lse", torch.float32, dev) if out_lse is not None else None, _stream(stream)))
 
 
 def snapkv_decode_paged_workspace_bytes(B: int, Hq: int, Hkv: int, D: int, max_len: int) -> int:
@@ -606,22 +624,22 @@ def snapkv_decode_attention_paged(q: torch.Tensor, k_pages: torch.Tensor, v_page
     num_pages, page_size, Hkv, Dk = k_pages.shape
     if Dk != D or v_pages.shape != k_pages.shape:
         raise ValueError("q, k_pages and v_pages disagree on their shapes")
-    if block_table.dim() != 2 or block_table.shape[0] != B or tuple(lens.shape) != (B,):
+    if block_table.dim() != 2 or block_table.shape[0] != B or lens.shape != (B,):
         raise ValueError("block_table must be [B, columns] and lens [B]")
-    if out.shape != q.shape or (out_lse is not None and tuple(out_lse.shape) != (B, Hq)):
+    if out.shape != q.shape or (out_lse is not None and out_lse.shape != (B, Hq)):
         raise ValueError("out must be [B, Hq, D] and out_lse [B, Hq]")
-    _on_current_device(q, k_pages, v_pages, block_table, lens, out, out_lse, workspace)
-    ins = (_dev(q, "q"), _dev(k_pages, "k_pages", q.dtype), _dev(v_pages, "v_pages", q.dtype),
-           _dev(block_table, "block_table", torch.int32), block_table.shape[1], num_pages, page_size, _dev(lens, "lens", torch.int32))
-    outs = (_dev(out, "out", q.dtype), _dev(out_lse, "out_lse", torch.float32) if out_lse is not None else None)
+    dev, dt, i32 = _device_of(q, "q"), q.dtype, torch.int32
+    ins = (_at(q, "q", dt, dev), _at(k_pages, "k_pages", dt, dev), _at(v_pages, "v_pages", dt, dev),
+           _at(block_table, "block_table", i32, dev), block_table.shape[1], num_pages, page_size, _at(lens, "lens", i32, dev))
+    outs = (_at(out, "out", dt, dev), _at(out_lse, "out_lse", torch.float32, dev) if out_lse is not None else None)
     st = _stream(stream)
     if workspace is None:
         if stream is not None and st != _stream(None):
             raise ValueError("a step on another stream than the current one needs a workspace of the caller's")
-        need = lib.snapkv_decode_paged_workspace_bytes(B, Hq, Hkv, D, int(max_len))
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
-    _check(lib.snapkv_decode_attention_paged(_dtype_code(q), *ins, int(max_len), B, Hq, Hkv, D, *outs,
-                                             _dev(workspace, "workspace", torch.uint8), workspace.numel(), st))
+        need = lib.snapkv_decode_paged_workspace_bytes(B, Hq, Hkv, D, max_len)
+        workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
+    ws, size = (_at(workspace, "workspace", torch.uint8, dev), workspace.numel()) if workspace is not None else (None, 0)
+    _check(lib.snapkv_decode_attention_paged(_dtype_code(q), *ins, max_len, B, Hq, Hkv, D, *outs, ws, size, st))
 
 
 def compress(q_win, k, v, pool_kind: int, p: int, C: int, stream=None

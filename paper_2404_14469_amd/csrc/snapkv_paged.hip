@@ -34,7 +34,7 @@ __global__ __launch_bounds__(kWaves * 64) void paged_attn(const PagedArgs A) {
     constexpr int ROW = D * 2;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int n16 = lane & 15, kg = lane >> 4;
-    const int chunk = blockIdx.x, kvh = blockIdx.y, b = blockIdx.z;
+    const int kvh = blockIdx.x % A.Hkv, chunk = blockIdx.x / A.Hkv, b = blockIdx.y;    // (heads of one chunk of pages run together)
     int64_t len = A.lens[b];
     const int S = (int)(len < 0 ? 0 : (len > A.max_len ? A.max_len : len));
     const int begin = chunk * A.chunk;
@@ -67,29 +67,28 @@ __global__ __launch_bounds__(kWaves * 64) void paged_attn(const PagedArgs A) {
         at = at < 0 ? 0 : (at >= A.pages ? A.pages - 1 : at);
         return (at * A.page + (r - pg * A.page)) * token;
     };
-    struct PairRegs {
-        uint4 kx[NP], ky[NP], vx[NP], vy[NP];
+    struct Rows {                                      // the rows of a lane's two keys
+        int64_t x, y;
     };
-    auto request = [&](PairRegs& P, int key0) {
-        const int64_t rx = offset_of(key0 + n16), ry = offset_of(key0 + 16 + n16);
+    auto find = [&](int key0) { return Rows{offset_of(key0 + n16), offset_of(key0 + 16 + n16)}; };
+    auto process = [&](const Rows& at, int key0) {
+        uint4 kx[NP], ky[NP], vx[NP], vy[NP];
 #pragma unroll
         for (int c = 0; c < NP; ++c) {
-            P.kx[c] = *reinterpret_cast<const uint4*>(kbase + rx + (4 * c + kg) * 16);
-            P.ky[c] = *reinterpret_cast<const uint4*>(kbase + ry + (4 * c + kg) * 16);
+            kx[c] = *reinterpret_cast<const uint4*>(kbase + at.x + (4 * c + kg) * 16);
+            ky[c] = *reinterpret_cast<const uint4*>(kbase + at.y + (4 * c + kg) * 16);
         }
 #pragma unroll
         for (int c = 0; c < NP; ++c) {
-            P.vx[c] = *reinterpret_cast<const uint4*>(vbase + rx + (4 * c + kg) * 16);
-            P.vy[c] = *reinterpret_cast<const uint4*>(vbase + ry + (4 * c + kg) * 16);
+            vx[c] = *reinterpret_cast<const uint4*>(vbase + at.x + (4 * c + kg) * 16);
+            vy[c] = *reinterpret_cast<const uint4*>(vbase + at.y + (4 * c + kg) * 16);
         }
         __builtin_amdgcn_sched_barrier(0);
-    };
-    auto process = [&](const PairRegs& P, int key0) {
         dfx4 sx = {0.f, 0.f, 0.f, 0.f}, sy = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int c = 0; c < NP; ++c) {
-            sx = mma(T{}, P.kx[c], qf[c], sx);
-            sy = mma(T{}, P.ky[c], qf[c], sy);
+            sx = mma(T{}, kx[c], qf[c], sx);
+            sy = mma(T{}, ky[c], qf[c], sy);
         }
         const int k0 = key0 + 4 * kg;
         float e[8];
@@ -124,8 +123,8 @@ __global__ __launch_bounds__(kWaves * 64) void paged_attn(const PagedArgs A) {
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 const dfx4 z = {0.f, 0.f, 0.f, 0.f};
-                const dfx4 tx = mma(T{}, P.vx[c], half ? sel1 : sel0, z);
-                const dfx4 ty = mma(T{}, P.vy[c], half ? sel1 : sel0, z);
+                const dfx4 tx = mma(T{}, vx[c], half ? sel1 : sel0, z);
+                const dfx4 ty = mma(T{}, vy[c], half ? sel1 : sel0, z);
                 uint4 vt;
                 vt.x = pack_exact(T{}, tx[0], tx[1]);
                 vt.y = pack_exact(T{}, tx[2], tx[3]);
@@ -139,19 +138,15 @@ __global__ __launch_bounds__(kWaves * 64) void paged_attn(const PagedArgs A) {
         }
     };
     constexpr int STEP = 32 * kWaves;
-    PairRegs R0, R1;
     int key = begin + 32 * wave;
     if (key < end) {
-        request(R0, key);
+        Rows at = find(key);
         for (;;) {
-            request(R1, key + STEP < end ? key + STEP : key);
-            process(R0, key);
+            const Rows next = find(key + STEP);        // (behind the end: the last row)
+            process(at, key);
             key += STEP;
             if (key >= end) break;
-            request(R0, key + STEP < end ? key + STEP : key);
-            process(R1, key);
-            key += STEP;
-            if (key >= end) break;
+            at = next;
         }
     }
     lsum += __shfl_xor(lsum, 16);
@@ -201,18 +196,20 @@ __global__ __launch_bounds__(kWaves * 64) void paged_attn(const PagedArgs A) {
     }
 }
 
-// Joins the partials of the sequences of more than one chunk: a wave per query head.
+// Joins the partials of the sequences of more than one chunk: a workgroup per query head, its waves a quarter of the chunks each,
+// eight partial outputs in flight at a time.
 template <typename T, int D>
-__global__ __launch_bounds__(64) void paged_join(const PagedArgs A) {
+__global__ __launch_bounds__(kWaves * 64) void paged_join(const PagedArgs A) {
     typedef typename store_type<T>::type elem;
-    constexpr int E = D / 64;
+    constexpr int E = D / 64, BATCH = 8;
     const int64_t hq = blockIdx.x;
-    const int lane = threadIdx.x, b = (int)(hq / A.Hq);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, b = (int)(hq / A.Hq);
     int64_t len = A.lens[b];
     const int S = (int)(len < 0 ? 0 : (len > A.max_len ? A.max_len : len));
     if (S <= A.chunk) return;
     const int n = (S + A.chunk - 1) / A.chunk;
     const float2* ml = A.part_ml + hq * A.nchunk;
+    const float* pa = A.part_acc + hq * A.nchunk * D + lane * E;
     float M = -INFINITY;
     for (int i = lane; i < n; i += 64) M = fmaxf(M, ml[i].x);
 #pragma unroll
@@ -220,26 +217,50 @@ __global__ __launch_bounds__(64) void paged_join(const PagedArgs A) {
     float Lq = 0.f, o[E];
 #pragma unroll
     for (int e = 0; e < E; ++e) o[e] = 0.f;
-    const float* pa = A.part_acc + hq * A.nchunk * D + lane * E;
-    for (int i = 0; i < n; ++i) {
-        const float2 p = ml[i];
-        const float f = __builtin_amdgcn_exp2f(p.x - M);
-        Lq += p.y * f;
+    for (int i0 = wave * BATCH; i0 < n; i0 += kWaves * BATCH) {
+        float2 p[BATCH];
+        float x[BATCH][E];
 #pragma unroll
-        for (int e = 0; e < E; ++e) o[e] += pa[(int64_t)i * D + e] * f;
+        for (int i = 0; i < BATCH; ++i) {
+            const int c = i0 + i < n ? i0 + i : n - 1;
+            p[i] = ml[c];
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[i][e] = pa[(int64_t)c * D + e];
+        }
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            const float f = i0 + i < n ? __builtin_amdgcn_exp2f(p[i].x - M) : 0.f;
+            Lq += p[i].y * f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] += x[i][e] * f;
+        }
     }
-    elem* out = reinterpret_cast<elem*>(A.out) + hq * D + lane * E;
+    __shared__ float s_o[kWaves][D], s_l[kWaves];
 #pragma unroll
-    for (int e = 0; e < E; ++e) out[e] = (elem)(Lq > 0.f ? o[e] / Lq : 0.f);
-    if (A.lse && lane == 0) A.lse[hq] = Lq > 0.f ? (M + __builtin_amdgcn_logf(Lq)) * 0.6931471805599453f : -INFINITY;
+    for (int e = 0; e < E; ++e) s_o[wave][lane * E + e] = o[e];
+    if (lane == 0) s_l[wave] = Lq;
+    __syncthreads();
+    Lq = s_l[0] + s_l[1] + s_l[2] + s_l[3];
+    if (threadIdx.x < D) {
+        const int d = threadIdx.x;
+        const float y = s_o[0][d] + s_o[1][d] + s_o[2][d] + s_o[3][d];
+        reinterpret_cast<elem*>(A.out)[hq * D + d] = (elem)(Lq > 0.f ? y / Lq : 0.f);
+    }
+    if (A.lse && threadIdx.x == 0) A.lse[hq] = Lq > 0.f ? (M + __builtin_amdgcn_logf(Lq)) * 0.6931471805599453f : -INFINITY;
 }
 
 }  // namespace
 
+// Keys of a workgroup.  With few (sequence, KV head) pairs as few as give 1024 workgroups, four per compute unit, if all
+// sequences are as long as they may be, down to the 128 of one step of each wave; a sequence of up to 512 is not cut, so that short
+// steps are one launch.  At most 1024, and 512 where even those give 2048 workgroups: sequences are of different lengths, which
+// only the device knows, and small shares even that out.  Microseconds with at most 512 / 1024 / 2048 / 4096 keys: 32
+// sequences of 1 to 16384 keys, 8 KV heads 120 / 125 / 149 / 224; eight of about 16000, 32 KV heads 374 / 373 / 378 / 385; one of
+// 131072 keys, 8 KV heads 114 / 107 / 108 / -.
 PagedPlan paged_plan(int B, int Hq, int Hkv, int D, int64_t max_len) {
-    const int64_t pairs = (int64_t)B * Hkv, keys = pairs * max_len;
-    int64_t chunk = (keys / 768 + 127) / 128 * 128;
-    chunk = std::max<int64_t>(256, std::min<int64_t>(chunk, 4096));
+    const int64_t keys = (int64_t)B * Hkv * max_len;
+    int64_t chunk = std::max<int64_t>(128, (keys / 1024 + 127) / 128 * 128);
+    chunk = std::min<int64_t>(chunk, keys >= 2048 * 1024 ? 512 : 1024);
     if (max_len <= 512) chunk = 512;
     PagedPlan P;
     P.chunk = (int)chunk;
@@ -268,8 +289,8 @@ hipError_t launch_paged(int dtype, int D, PagedArgs A, void* workspace, hipStrea
         A.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + ((heads * P.nchunk * D * sizeof(float) + 255) & ~(size_t)255));
     }
     auto launch = [&](auto step, auto join) {
-        hipLaunchKernelGGL(step, dim3(P.nchunk, A.Hkv, A.B), dim3(kWaves * 64), 0, st, A);
-        if (P.nchunk > 1) hipLaunchKernelGGL(join, dim3((unsigned)heads), dim3(64), 0, st, A);
+        hipLaunchKernelGGL(step, dim3(P.nchunk * A.Hkv, A.B), dim3(kWaves * 64), 0, st, A);
+        if (P.nchunk > 1) hipLaunchKernelGGL(join, dim3((unsigned)heads), dim3(kWaves * 64), 0, st, A);
     };
     if (dtype == 0 && D == 128) launch(paged_attn<dec_bf16, 128>, paged_join<dec_bf16, 128>);
     else if (dtype == 0 && D == 64) launch(paged_attn<dec_bf16, 64>, paged_join<dec_bf16, 64>);
