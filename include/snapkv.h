@@ -404,7 +404,8 @@ int snapkv_append_paged(int dtype, const void* q, const void* k, const void* v, 
  *   dtype   SNAPKV_DTYPE_BF16 or SNAPKV_DTYPE_F16 (float32 storage: SNAPKV_ERR_UNSUPPORTED)
  *   q [T, Hq, D], k and v [T, Hkv, D] device, dtype: row t of head h starts row_stride * t + head_stride * h ELEMENTS after the
  *           pointer (row_stride >= D, head_stride >= 0, every row 16-byte aligned), e.g. columns of one projection's
- *           output or head-major storage (row strides of k and v up to 2^24); finite values; Hq % Hkv == 0, D in {64, 128}
+ *           output or head-major storage (row strides of k and v up to 2^24); Hq % Hkv == 0, D in {64, 128}.  Keys and values that
+ *           a row does not see reach it in no way, infinities and NaN included
  *   cu_seqlens [B + 1] device int32, ascending: prompt b is the tokens cu_seqlens[b] .. cu_seqlens[b + 1] - 1 (none: an
  *           empty prompt).  Values are clamped to [0, T]
  *   out     [T, Hq, D] device, dtype, contiguous;  out_lse [Hq, T] device float32 or NULL.  Rows that belong to no prompt

@@ -34,16 +34,19 @@ typedef __attribute__((ext_vector_type(8))) __bf16 pbf16x8;
 typedef __attribute__((ext_vector_type(8))) _Float16 pf16x8;
 typedef __attribute__((ext_vector_type(16))) float pfx16;
 typedef __attribute__((ext_vector_type(4))) short ps16x4;
+typedef __attribute__((ext_vector_type(4))) unsigned pu32x4;
 
 struct p_bf16 {
     typedef __bf16 elem;
     typedef pbf16x8 frag;
     static constexpr float kShift = 0.f;
+    static constexpr unsigned kExp = 0x7F80;                 // all ones: an infinity or NaN
 };
 struct p_f16 {
     typedef _Float16 elem;
     typedef pf16x8 frag;
     static constexpr float kShift = 7.f;
+    static constexpr unsigned kExp = 0x7C00;
 };
 __device__ __forceinline__ pfx16 mma32(pbf16x8 a, pbf16x8 b, pfx16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ pfx16 mma32(pf16x8 a, pf16x8 b, pfx16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
@@ -75,9 +78,11 @@ __device__ __forceinline__ bool locate(const PromptArgs& A, int rank, int lane, 
         }
         return (n + ROWS - 1) / ROWS;
     };
+    const int nt0 = span(lane);                                      // (mostly all there are)
+    auto tiles = [&](int b0) __attribute__((always_inline)) { return b0 == 0 ? nt0 : span(b0 + lane); };
     int most = 0, total = 0;
     for (int b0 = 0; b0 < A.B; b0 += 64) {
-        const int nt = span(b0 + lane);
+        const int nt = tiles(b0);
         for (int i = 0; i < min(64, A.B - b0); ++i) {
             const int x = __builtin_amdgcn_readlane(nt, i);
             most = max(most, x);
@@ -90,7 +95,7 @@ __device__ __forceinline__ bool locate(const PromptArgs& A, int rank, int lane, 
         const int w = (width + 62) / 63, c = lo + lane * w;
         int f = 0;
         for (int b0 = 0; b0 < A.B; b0 += 64) {
-            const int nt = span(b0 + lane);
+            const int nt = tiles(b0);
             for (int i = 0; i < min(64, A.B - b0); ++i) f += max(__builtin_amdgcn_readlane(nt, i) - c + 1, 0);
         }
         const int k = __popcll(__ballot(f > rank));                  // (at least 1, at most 63)
@@ -101,7 +106,8 @@ __device__ __forceinline__ bool locate(const PromptArgs& A, int rank, int lane, 
     }
     int within = rank - after;                                       // which of the sequences of lo tiles or more
     for (int b0 = 0; b0 < A.B; b0 += 64) {
-        unsigned long long has = __ballot(span(b0 + lane) >= lo);
+        if (A.B > 64) span(b0 + lane);
+        unsigned long long has = __ballot((n + ROWS - 1) / ROWS >= lo);
         const int here = __popcll(has);
         if (within < here) {
             for (; within > 0; --within) has &= has - 1;
@@ -130,7 +136,7 @@ __device__ __forceinline__ float other_half(float x) {
 }
 
 template <typename T, int D, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, 2) void prompt_attn(const PromptArgs A) {
+__global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void prompt_attn(const PromptArgs A) {
     typedef typename T::elem elem;
     typedef typename T::frag frag;
     constexpr int ROWS = WAVES * 32;            // query rows of a workgroup
@@ -142,12 +148,11 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_attn(const PromptArgs A)
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n32 = lane & 31, h2 = lane >> 5;
 
-    // KV heads are dealt to the XCDs (workgroup i runs on XCD i % 8), so the workgroups that read a head share an L2
+    // KV heads are dealt to the XCDs (workgroup i runs on XCD i % 8), so the workgroups that read a head share an L2; the
+    // longest row tiles of all heads come first.
     const int m8 = (A.Hkv & 7) == 0 ? 8 : ((A.Hkv & 3) == 0 ? 4 : ((A.Hkv & 1) == 0 ? 2 : 1));
-    const int rest = blockIdx.x / m8;
-    const int per = A.ranks * A.g;
-    const int kvh = blockIdx.x % m8 + m8 * (rest / per);
-    const int rank = rest % per / A.g, hq = kvh * A.g + rest % A.g;
+    const int rank = blockIdx.x / A.Hq, rest = blockIdx.x % A.Hq / m8;
+    const int kvh = blockIdx.x % m8 + m8 * (rest / A.g), hq = kvh * A.g + rest % A.g;
 
     int tile, begin, len;
     if (!locate<ROWS>(A, rank, lane, begin, len, tile)) return;
@@ -261,7 +266,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_attn(const PromptArgs A)
     float big;
     pfx16 xa, xb;
     auto pass = [&](int b, const pfx16& x, pfx16& xn, lds_char k_next, lds_char v_now) __attribute__((always_inline)) {
-        if (b >= mine) return;
+        if (b + 1 >= mine) return;
         frag pf[2], kf[NQ], vf[NV];
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) kf[i] = k_frag(k_next, i);
@@ -312,6 +317,7 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_attn(const PromptArgs A)
             load(vh, (int)A.v_rs, v_off, v_piece, (t + 1) * kKeys, v_free);
         }
         pass(2 * t, xa, xb, k_now, v_now);
+        if (2 * t + 2 == mine) xa = xb;                      // (the wave's last block: its logits wait there for the end)
         pass(2 * t + 1, xb, xa, k_now + 32 * ROW, v_now + 32 * ROW);
     };
     load(kh, (int)A.k_rs, k_off, k_piece, 0, s_k1);
@@ -329,6 +335,44 @@ __global__ __launch_bounds__(WAVES * 64, 2) void prompt_attn(const PromptArgs A)
         if (++t >= ntiles) break;
         two_blocks(t, s_k1, s_k0, s_v1, s_v0);
         if (++t >= ntiles) break;
+    }
+    // The wave's last block, the only one that its rows see in part.  Its tile is one of the last two, which are still there, and its
+    // logits are in xa.  Values that a row does not see have probability 0, but 0 times an infinity or
+    // NaN is not 0: where the block holds such a value, its keys are added one by one (the others' values taken as zeros) and
+    // the sums of rows that do not see the key kept.
+    if (mine > 0) {
+        const int b = mine - 1;
+        const lds_char v_now = (b & 2 ? s_v1 : s_v0) + (b & 1) * 32 * ROW;
+        frag pf[2];
+        rescale(big);
+        const float shift = T::kShift - m;
+#pragma unroll
+        for (int n = 0; n < 8; ++n) two(xa, n, shift, pf);
+        bool spoiled = false;
+#pragma unroll
+        for (int i = 0; i < ROW * 32 / 1024; ++i) {
+            const pu32x4 y = *reinterpret_cast<const __attribute__((address_space(3))) pu32x4*>(v_now + i * 1024 + lane * 16);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) spoiled |= (y[e] & T::kExp) == T::kExp || (y[e] >> 16 & T::kExp) == T::kExp;
+        }
+        if (!__any(spoiled)) {
+#pragma unroll
+            for (int i = 0; i < NV; ++i) acc[i % ND] = mma32(v_frag(v_now, i), pf[i / ND], acc[i % ND]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll 1
+                for (int key = 0; key < 16; ++key)
+#pragma unroll
+                    for (int i = 0; i < ND; ++i) {
+                        frag vf = v_frag(v_now, j * ND + i);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) vf[e] = 8 * (e / 4) + 4 * h2 + e % 4 == key ? vf[e] : (elem)0.f;
+                        const pfx16 y = mma32(vf, pf[j], acc[i]);
+#pragma unroll
+                        for (int r = 0; r < 16; ++r) acc[i][r] = b * 32 + 16 * j + key <= row ? y[r] : acc[i][r];
+                    }
+        }
     }
     float sum = lsum + lsum2;
     sum += other_half(sum);

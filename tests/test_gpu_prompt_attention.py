@@ -129,6 +129,29 @@ def test_a_prompt_does_not_see_its_neighbours(snapkv):
     assert torch.equal(out[100:300], again[100:300]) and torch.equal(lse[:, 100:300], again_lse[:, 100:300])
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("L,at", [(1, 0), (2, 1), (33, 32), (64, 40), (100, 99), (200, 129), (300, 297)])
+def test_values_that_a_row_does_not_see_may_be_anything(snapkv, dtype, D, L, at):
+    """Infinities and NaN in a later token's key and value reach no earlier row; a later prompt starts anew."""
+    gen = seeded(L + at)
+    q, k, v = (rows(gen, L + 50, h, D, DT[dtype], "tokens") for h in (4, 2, 2))
+    cu = offsets([L, 50])
+    want, want_lse = run(snapkv, q, k, v, cu)
+    for what in (float("nan"), float("inf"), -float("inf")):
+        k2, v2 = k.clone(), v.clone()
+        k2[at, 1] = what
+        v2[at] = torch.where(torch.rand((2, D), generator=gen, device="cuda") < 0.3, what, v[at].float()).to(v.dtype)
+        v2[at, :, 0] = what
+        out, lse = run(snapkv, q, k2, v2, cu)
+        keep = torch.ones(L + 50, dtype=torch.bool, device="cuda")
+        keep[at:L] = False
+        assert torch.equal(lse[:, keep], want_lse[:, keep])
+        # (values added one by one may round otherwise than sixteen at a time: one step of the type at most)
+        assert ((out[keep].float() - want[keep].float()).abs() <= torch.finfo(DT[dtype]).eps * want[keep].float().abs() + 1e-5).all()
+        assert not torch.isfinite(out[at]).all()
+
+
 def test_offsets_outside_the_tensors_are_clamped(snapkv):
     gen = seeded(8)
     q, k, v = (rows(gen, 150, h, 64, torch.bfloat16, "tokens") for h in (2, 2, 2))
