@@ -55,7 +55,7 @@ __global__ __launch_bounds__(kWaves * 64) void paged_attn(const PagedArgs A) {
     }
     const uint4 sel0 = selector<T>(lane, 0), sel1 = selector<T>(lane, 1);
 
-    float m = -INFINITY, lsum = 0.f;
+    float m = -3.4028235e38f, lsum = 0.f;              // (finite: logits of -infinity have probability 0 and not NaN)
     dfx4 acc[NB];
 #pragma unroll
     for (int i = 0; i < NB; ++i) acc[i] = dfx4{0.f, 0.f, 0.f, 0.f};
@@ -102,7 +102,7 @@ __global__ __launch_bounds__(kWaves * 64) void paged_attn(const PagedArgs A) {
         tmax = fmaxf(tmax, __shfl_xor(tmax, 16));
         tmax = fmaxf(tmax, __shfl_xor(tmax, 32));
         const float mn = fmaxf(m, tmax);
-        const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mn);
+        const float alpha = __builtin_amdgcn_exp2f(m - mn);
         m = mn;
         float psum = 0.f;
 #pragma unroll
@@ -165,16 +165,15 @@ __global__ __launch_bounds__(kWaves * 64) void paged_attn(const PagedArgs A) {
     constexpr int DT = D / 16;
     const int qi = tid >> 4, d0 = (tid & 15) * DT;
     if (qi < A.g) {
-        float M = -INFINITY;
+        float M = s_m[0][qi];
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s_m[w][qi]);
+        for (int w = 1; w < kWaves; ++w) M = fmaxf(M, s_m[w][qi]);
         float Lq = 0.f, o[DT];
 #pragma unroll
         for (int d = 0; d < DT; ++d) o[d] = 0.f;
 #pragma unroll
         for (int w = 0; w < kWaves; ++w) {
-            const float mw = s_m[w][qi];
-            const float f = mw == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mw - M);
+            const float f = __builtin_amdgcn_exp2f(s_m[w][qi] - M);
             Lq += s_l[w][qi] * f;
 #pragma unroll
             for (int d = 0; d < DT; ++d) o[d] += s_acc[w][qi][d0 + d] * f;

@@ -163,7 +163,9 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void prompt_attn(const
     const char* qr = A.q + (int64_t)(begin + min(row, len - 1)) * A.q_rs + (int64_t)hq * A.q_hs + h2 * 16;
 #pragma unroll
     for (int c = 0; c < NC; ++c) qf[c] = *reinterpret_cast<const frag*>(qr + 32 * c);
-    float m = -INFINITY, limit = -INFINITY;                  // the shift of the exponentials; the largest logit, unscaled, it is good for
+    // The shift of the exponentials, and the largest logit, unscaled, that it is good for.  (The shift starts finite: logits of
+    // -infinity, if a row sees nothing else yet, then have probability 0 and not NaN.)
+    float m = -3.4028235e38f, limit = -INFINITY;
     float lsum = 0.f, lsum2 = 0.f;                           // (two sums: shorter chains)
     pfx16 acc[ND];
 #pragma unroll
@@ -239,7 +241,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void prompt_attn(const
     // some row of the wave has outgrown it by 2^8.
     auto rescale = [&](float big) __attribute__((always_inline)) {
         if (__any(big > limit)) {
-            const float mn = fmaxf(m, fmaxf(big, other_half(big)) * A.scale2);     // finite: key 0 is in the first block
+            const float mn = fmaxf(m, fmaxf(big, other_half(big)) * A.scale2);
             const float alpha = __builtin_amdgcn_exp2f(m - mn);
             m = mn;
             limit = (mn + 8.f) / A.scale2;

@@ -152,6 +152,25 @@ def test_values_that_a_row_does_not_see_may_be_anything(snapkv, dtype, D, L, at)
         assert not torch.isfinite(out[at]).all()
 
 
+def test_keys_of_minus_infinity_take_no_part(snapkv):
+    """Logits of -infinity over the first blocks of a row: their probability is 0, whatever comes later."""
+    gen, L = seeded(77), 150
+    q, k, v = (rows(gen, L, h, 64, torch.bfloat16, "tokens") for h in (2, 1, 1))
+    q.copy_(q.abs() + 0.1)
+    k[:70] = -float("inf")
+    cu = offsets([L])
+    out, lse = run(snapkv, q, k, v, cu)
+    assert torch.isnan(out[:70]).all() and torch.isneginf(lse[:, :70]).all()         # (nothing to average)
+    for i in (70, 71, 96, 127, 128, 149):
+        for h in range(2):
+            s = k[70:i + 1, 0].double() @ q[i, h].double() / 8.0
+            z = torch.logsumexp(s, 0)
+            p = (s - z).exp()
+            reach = (k[70:i + 1, 0].double().abs() @ q[i, h].double().abs()).max() / 8.0
+            check_attention(num(out[i, h])[None], num(lse[h, i])[None], num(p @ v[70:i + 1, 0].double())[None], num(z)[None],
+                            num(p @ v[70:i + 1, 0].double().abs())[None], num(reach)[None], L, torch.bfloat16, parts=False)
+
+
 def test_offsets_outside_the_tensors_are_clamped(snapkv):
     gen = seeded(8)
     q, k, v = (rows(gen, 150, h, 64, torch.bfloat16, "tokens") for h in (2, 2, 2))
