@@ -52,6 +52,7 @@ __device__ __forceinline__ pfx16 mma32(pbf16x8 a, pbf16x8 b, pfx16 c) { return _
 __device__ __forceinline__ pfx16 mma32(pf16x8 a, pf16x8 b, pfx16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
 
 constexpr int kKeys = 64;      // keys of a tile
+constexpr int kWaves = 4;
 
 typedef const __attribute__((address_space(1))) void* global_ptr;
 typedef __attribute__((address_space(3))) void* lds_ptr;
@@ -122,12 +123,11 @@ __device__ __forceinline__ bool locate(const PromptArgs& A, int rank, int lane, 
     return false;
 }
 
-// All waves are done with what they read and what they fetched straight into LDS has arrived.  The wait is explicit: those
-// loads write no register that the compiler would wait for, and a barrier alone does not.
-__device__ __forceinline__ void tiles_ready() {
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-    __syncthreads();
-}
+// What the wave fetched straight into LDS has arrived.  The wait is explicit: those loads write no register that the compiler
+// would wait for, and a barrier alone does not.
+// All of it, or all but the last N loads.
+template <int N = 0>
+__device__ __forceinline__ void fetched() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
 
 // The other half of the wave: lane l gets lane l ^ 32's value.
 __device__ __forceinline__ float other_half(float x) {
@@ -135,14 +135,16 @@ __device__ __forceinline__ float other_half(float x) {
     return __uint_as_float((threadIdx.x & 32) ? y[0] : y[1]);
 }
 
-template <typename T, int D, int WAVES>
-__global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void prompt_attn(const PromptArgs A) {
+template <typename T, int D, bool SPLIT>
+__global__ __launch_bounds__(kWaves * 64, D == 64 && !SPLIT ? 3 : 2) void prompt_attn(const PromptArgs A) {
     typedef typename T::elem elem;
     typedef typename T::frag frag;
-    constexpr int ROWS = WAVES * 32;            // query rows of a workgroup
+    constexpr int WAVES = kWaves, STEP = SPLIT ? WAVES : 1;   // blocks of 32 keys from one of a wave to its next
+    constexpr int ROWS = SPLIT ? 32 : WAVES * 32;            // query rows of a workgroup
     constexpr int ROW = D * 2, PIECES = D / 8;  // bytes and 16-byte pieces of a row
     constexpr int NC = D / 16, ND = D / 32;     // contraction steps of a logit; 32-column blocks of the output
-    __shared__ __align__(16) char m_k0[kKeys * ROW], m_v0[kKeys * ROW], m_k1[kKeys * ROW], m_v1[kKeys * ROW];
+    constexpr int TILE = (SPLIT ? WAVES * 32 : kKeys) * ROW; // (split: a block of each wave's own)
+    __shared__ __align__(16) char m_k0[TILE], m_v0[TILE], m_k1[SPLIT ? 16 : TILE], m_v1[SPLIT ? 16 : TILE];
     const lds_char s_k0 = (lds_char)m_k0, s_v0 = (lds_char)m_v0, s_k1 = (lds_char)m_k1, s_v1 = (lds_char)m_v1;
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -157,7 +159,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void prompt_attn(const
     int tile, begin, len;
     if (!locate<ROWS>(A, rank, lane, begin, len, tile)) return;
 
-    const int row0 = tile * ROWS + wave * 32;                // the wave's first query row within the prompt
+    const int row0 = tile * ROWS + (SPLIT ? 0 : wave * 32);  // the wave's first query row within the prompt
     const int row = row0 + n32;
     frag qf[NC];
     const char* qr = A.q + (int64_t)(begin + min(row, len - 1)) * A.q_rs + (int64_t)hq * A.q_hs + h2 * 16;
@@ -179,38 +181,41 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void prompt_attn(const
     const int ntiles = last / kKeys + 1;
     const int mine = row0 < len ? row0 / 32 + 1 : 0;         // blocks of 32 keys that the wave's rows see; the last one in part
 
-    // Loads of a tile: WAVES KB at a time, a KB (RPL rows) per wave, straight into LDS.  The rows of a lane's loads differ by a number
-    // that does not change its place in the permutation.  Addresses are a uniform 64-bit one of the tile's first row and
-    // 32-bit offsets of at most 63 rows, never negative.
-    constexpr int RPL = 1024 / ROW, PER = kKeys / (RPL * WAVES);
-    static_assert(RPL * WAVES % PIECES == 0, "a lane's rows share a permutation");
-    const int lr = wave * RPL + lane / PIECES;
-    const int k_piece = k_slot<D>(lr, lane % PIECES) * 16, v_piece = v_slot<D>(lr, lane % PIECES) * 16;
-    const int k_off = lr * (int)A.k_rs + k_piece, v_off = lr * (int)A.v_rs + v_piece;
-    auto load = [&](const char* base, int rs, int off, int piece, int first, lds_char to) __attribute__((always_inline)) {
+    // Loads of 64 keys by all waves, or (split) of 32 by each: SHARE KB at a time, a KB (RPL rows) per wave, straight into LDS.
+    // Addresses are a uniform 64-bit one of the first row and 32-bit offsets of at most 63 rows, never negative.
+    constexpr int SHARE = SPLIT ? 1 : WAVES, RPL = 1024 / ROW, PER = (SPLIT ? 32 : kKeys) / (RPL * SHARE);
+    const int part = SPLIT ? 0 : wave, lr = part * RPL + lane / PIECES, own = SPLIT ? wave * 32 * ROW : 0;
+    // (what a lane's rows differ by changes its place in the permutation by the same number, mostly 0, whatever the lane)
+    constexpr int K_TURN = RPL * SHARE % PIECES * 16;
+    static_assert(RPL * SHARE % (D / 32) == 0 && (K_TURN == 0 || RPL * SHARE * 16 == K_TURN), "rows of a lane and the permutations");
+    int k_piece = k_slot<D>(lr, lane % PIECES) * 16, v_piece = v_slot<D>(lr, lane % PIECES) * 16;
+    auto load = [&](const char* base, int rs, int piece, int turn, int first, lds_char to) __attribute__((always_inline)) {
         const int at = min(first, len - 1);
         const auto rsrc = __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(base) + (int64_t)at * rs, 0, -1, 0x00020000);
-        if (first + kKeys <= len) {
+        if (first + (SPLIT ? 32 : kKeys) <= len) {
 #pragma unroll
             for (int i = 0; i < PER; ++i)
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_ptr)(to + (i * WAVES + wave) * 1024), 16, off, i * RPL * WAVES * rs, 0, 0);
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_ptr)(to + own + (i * SHARE + part) * 1024), 16, lr * rs + (piece ^ (i * turn & (ROW - 1))), i * RPL * SHARE * rs, 0, 0);
         } else {                                             // rows behind the prompt: its last row again
+#pragma unroll
             for (int i = 0; i < PER; ++i) {
-                const int down = min(first + i * RPL * WAVES + lr, len - 1) - at;
-                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_ptr)(to + (i * WAVES + wave) * 1024), 16, down * rs + piece, 0, 0, 0);
+                const int down = min(first + i * RPL * SHARE + lr, len - 1) - at;
+                __builtin_amdgcn_raw_ptr_buffer_load_lds(rsrc, (lds_ptr)(to + own + (i * SHARE + part) * 1024), 16, down * rs + (piece ^ (i * turn & (ROW - 1))), 0, 0, 0);
             }
         }
     };
+    auto load_k = [&](int first, lds_char to) __attribute__((always_inline)) { load(kh, (int)A.k_rs, k_piece, K_TURN, first, to); };
+    auto load_v = [&](int first, lds_char to) __attribute__((always_inline)) { load(vh, (int)A.v_rs, v_piece, 0, first, to); };
 
     // A lane's places in a tile: its pieces of key row n32 (the 32 rows below have the same permutation), and of the first value
     // row that it transposes (so have those 8 and 16 below).
     int k_at[NC], v_at[ND];
 #pragma unroll
-    for (int c = 0; c < NC; ++c) k_at[c] = n32 * ROW + k_slot<D>(n32, 2 * c + h2) * 16;
+    for (int c = 0; c < NC; ++c) k_at[c] = own + n32 * ROW + k_slot<D>(n32, 2 * c + h2) * 16;
 #pragma unroll
     for (int i = 0; i < ND; ++i) {
         const int vr = 4 * h2 + (lane & 15) / 4;
-        v_at[i] = vr * ROW + v_slot<D>(vr, 4 * i + 2 * ((lane >> 4) & 1) + (lane & 3) / 2) * 16 + (lane & 1) * 8;
+        v_at[i] = own + vr * ROW + v_slot<D>(vr, 4 * i + 2 * ((lane >> 4) & 1) + (lane & 3) / 2) * 16 + (lane & 1) * 8;
     }
     // Operands of product i of a block of 32 keys: of its logits, of its part of the output (16 keys of 32 columns, transposed).
     constexpr int NQ = NC, NV = 2 * ND;
@@ -262,14 +267,15 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void prompt_attn(const
         pf[n / 4][2 * n % 8] = (elem)p;
         pf[n / 4][2 * n % 8 + 1] = (elem)q;
     };
-    // Software pipeline: the logits of block b + 1 are products that nothing of block b's softmax waits for, so between two
+    // Software pipeline: the logits of the wave's next block are products that nothing of block b's softmax waits for, so between two
     // matrix instructions stand a few of the softmax's.  Operands are read from LDS AHEAD products before their own.
-    constexpr int AHEAD = 3, PAIRS = 8, EARLY = 5;
+    constexpr int AHEAD = SPLIT ? 2 : 3, PAIRS = 8, EARLY = 5;
     float big;
     pfx16 xa, xb;
     auto pass = [&](int b, const pfx16& x, pfx16& xn, lds_char k_next, lds_char v_now) __attribute__((always_inline)) {
-        if (b + 1 >= mine) return;
+        if (b + STEP >= mine) return;
         frag pf[2], kf[NQ], vf[NV];
+        if constexpr (SPLIT) fetched<PER>();                 // its keys; its values (PER loads) may still be on their way
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) kf[i] = k_frag(k_next, i);
         rescale(big);
@@ -277,6 +283,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void prompt_attn(const
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < NQ; ++i) {
+            if (SPLIT && i + AHEAD == NQ) fetched();
             if (i + AHEAD < NQ) kf[i + AHEAD] = k_frag(k_next, i + AHEAD);
             else vf[i + AHEAD - NQ] = v_frag(v_now, i + AHEAD - NQ);
             product(kf[i], i, xn);
@@ -284,6 +291,8 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void prompt_attn(const
             for (int n = i * EARLY / NQ; n < (i + 1) * EARLY / NQ; ++n) two(x, n, shift, pf);
             __builtin_amdgcn_sched_barrier(0);
         }
+        if constexpr (SPLIT)                                 // (all products with the keys there have been issued, so they have been read)
+            if (b + 2 * STEP < mine) load_k((b + 2 * STEP) * 32, k_next);
 #pragma unroll
         for (int i = 0; i < ND; ++i) {
             if (i + AHEAD < NV) vf[i + AHEAD] = v_frag(v_now, i + AHEAD);
@@ -292,7 +301,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void prompt_attn(const
             for (int n = EARLY + i * (PAIRS - EARLY) / ND; n < EARLY + (i + 1) * (PAIRS - EARLY) / ND; ++n) two(x, n, shift, pf);
             __builtin_amdgcn_sched_barrier(0);
         }
-        hide(b + 1, xn);
+        hide(b + STEP, xn);
         __builtin_amdgcn_sched_barrier(0);
         big = xn[0];
 #pragma unroll
@@ -303,48 +312,87 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void prompt_attn(const
             for (int r = i * 16 / ND; r < (i + 1) * 16 / ND; ++r) big = fmaxf(big, xn[r]);
             __builtin_amdgcn_sched_barrier(0);
         }
+        if constexpr (SPLIT) load_v((b + STEP) * 32, v_now);
     };
-    // Keys are half a tile ahead of values: tile t of V is blocks 2 t and 2 t + 1, that of K blocks 2 t + 1 and 2 t + 2, whose logits
-    // are taken meanwhile.  The next tiles arrive in the other two buffers.
-    auto two_blocks = [&](int t, lds_char k_now, lds_char k_free, lds_char v_now, lds_char v_free) __attribute__((always_inline)) {
-        tiles_ready();
-        // (a lane's places are kept as they are, and a buffer's address is the constant offset of a read: sums of the two,
-        // made once in front of the loop, would take 24 registers)
+    // (a lane's places are kept as they are, and a buffer's address is the constant offset of a read: sums of the two, made once
+    // in front of the loop, would take 24 registers)
+    auto keep_places = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int c = 0; c < NC; ++c) asm volatile("" : "+v"(k_at[c]));
 #pragma unroll
         for (int i = 0; i < ND; ++i) asm volatile("" : "+v"(v_at[i]));
-        if (t + 1 < ntiles) {
-            load(kh, (int)A.k_rs, k_off, k_piece, (t + 1) * kKeys + 32, k_free);
-            load(vh, (int)A.v_rs, v_off, v_piece, (t + 1) * kKeys, v_free);
-        }
-        pass(2 * t, xa, xb, k_now, v_now);
-        if (2 * t + 2 == mine) xa = xb;                      // (the wave's last block: its logits wait there for the end)
-        pass(2 * t + 1, xb, xa, k_now + 32 * ROW, v_now + 32 * ROW);
+        asm volatile("" : "+v"(k_piece), "+v"(v_piece));
     };
-    load(kh, (int)A.k_rs, k_off, k_piece, 0, s_k1);
-    load(kh, (int)A.k_rs, k_off, k_piece, 32, s_k0);
-    load(vh, (int)A.v_rs, v_off, v_piece, 0, s_v0);
-    tiles_ready();
+    auto begin_with = [&](int b, lds_char s_k) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < NQ; ++i) product(k_frag(s_k1, i), i, xa);
-    hide(0, xa);
-    big = xa[0];
+        for (int i = 0; i < NQ; ++i) product(k_frag(s_k, i), i, xa);
+        hide(b, xa);
+        big = xa[0];
 #pragma unroll
-    for (int r = 1; r < 16; ++r) big = fmaxf(big, xa[r]);
-    for (int t = 0;;) {
-        two_blocks(t, s_k0, s_k1, s_v0, s_v1);
-        if (++t >= ntiles) break;
-        two_blocks(t, s_k1, s_k0, s_v1, s_v0);
-        if (++t >= ntiles) break;
+        for (int r = 1; r < 16; ++r) big = fmaxf(big, xa[r]);
+    };
+    lds_char v_last = s_v0;                                  // values of the wave's last block
+    if constexpr (SPLIT) {
+        // A wave's blocks are its own from their loads on: nothing to wait for but its own fetches.  One buffer for keys, which the
+        // next block's replace as soon as their logits are taken, and one for values: 64 KB, so two workgroups share a compute
+        // unit, and one's arithmetic covers the other's fetches.
+        int b = wave;
+        if (b < mine) {
+            load_k(b * 32, s_k0);
+            load_v(b * 32, s_v0);
+            fetched<PER>();
+            begin_with(b, s_k0);
+            if (b + STEP < mine) load_k((b + STEP) * 32, s_k0);
+            fetched();
+        }
+        auto block = [&](const pfx16& x, pfx16& xn) __attribute__((always_inline)) {
+            keep_places();
+            pass(b, x, xn, s_k0, s_v0);
+            b += STEP;
+        };
+        while (b + STEP < mine) {
+            block(xa, xb);
+            if (b + STEP >= mine) {
+                xa = xb;
+                break;
+            }
+            block(xb, xa);
+        }
+        fetched();
+    } else {
+        // Keys are half a tile ahead of values: tile t of V is blocks 2 t and 2 t + 1, that of K blocks 2 t + 1 and 2 t + 2, whose
+        // logits are taken meanwhile.  The next tiles arrive in the other two buffers.
+        auto two_blocks = [&](int t, lds_char k_now, lds_char k_free, lds_char v_now, lds_char v_free) __attribute__((always_inline)) {
+            fetched();
+            __syncthreads();                                 // these tiles have arrived, the others have been read
+            keep_places();
+            if (t + 1 < ntiles) {
+                load_k((t + 1) * kKeys + 32, k_free);
+                load_v((t + 1) * kKeys, v_free);
+            }
+            pass(2 * t, xa, xb, k_now, v_now);
+            if (2 * t + 2 == mine) xa = xb;                  // (the wave's last block: its logits wait there for the end)
+            pass(2 * t + 1, xb, xa, k_now + 32 * ROW, v_now + 32 * ROW);
+        };
+        load_k(0, s_k1);
+        load_k(32, s_k0);
+        load_v(0, s_v0);
+        fetched();
+        __syncthreads();
+        begin_with(0, s_k1);
+        for (int t = 0;;) {
+            two_blocks(t, s_k0, s_k1, s_v0, s_v1);
+            if (++t >= ntiles) break;
+            two_blocks(t, s_k1, s_k0, s_v1, s_v0);
+            if (++t >= ntiles) break;
+        }
+        v_last = ((mine - 1) & 2 ? s_v1 : s_v0) + ((mine - 1) & 1) * 32 * ROW;   // (one of the last two tiles, which are still there)
     }
-    // The wave's last block, the only one that its rows see in part.  Its tile is one of the last two, which are still there, and its
-    // logits are in xa.  Values that a row does not see have probability 0, but 0 times an infinity or
-    // NaN is not 0: where the block holds such a value, its keys are added one by one (the others' values taken as zeros) and
-    // the sums of rows that do not see the key kept.
-    if (mine > 0) {
-        const int b = mine - 1;
-        const lds_char v_now = (b & 2 ? s_v1 : s_v0) + (b & 1) * 32 * ROW;
+    // The wave's last block; its logits are in xa.  The last one that rows see they see in part.  Values that a row does not see
+    // have probability 0, but 0 times an infinity or NaN is not 0: where the block holds such a value, its keys are added one by
+    // one (the others' values taken as zeros) and the sums of rows that do not see the key kept.
+    if (SPLIT ? wave < mine : mine > 0) {
+        const int b = SPLIT ? wave + (mine - 1 - wave) / STEP * STEP : mine - 1;
         frag pf[2];
         rescale(big);
         const float shift = T::kShift - m;
@@ -353,13 +401,13 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void prompt_attn(const
         bool spoiled = false;
 #pragma unroll
         for (int i = 0; i < ROW * 32 / 1024; ++i) {
-            const pu32x4 y = *reinterpret_cast<const __attribute__((address_space(3))) pu32x4*>(v_now + i * 1024 + lane * 16);
+            const pu32x4 y = *reinterpret_cast<const __attribute__((address_space(3))) pu32x4*>(v_last + own + i * 1024 + lane * 16);
 #pragma unroll
             for (int e = 0; e < 4; ++e) spoiled |= (y[e] & T::kExp) == T::kExp || (y[e] >> 16 & T::kExp) == T::kExp;
         }
-        if (!__any(spoiled)) {
+        if (b < mine - 1 || !__any(spoiled)) {
 #pragma unroll
-            for (int i = 0; i < NV; ++i) acc[i % ND] = mma32(v_frag(v_now, i), pf[i / ND], acc[i % ND]);
+            for (int i = 0; i < NV; ++i) acc[i % ND] = mma32(v_frag(v_last, i), pf[i / ND], acc[i % ND]);
         } else {
 #pragma unroll
             for (int j = 0; j < 2; ++j)
@@ -367,7 +415,7 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void prompt_attn(const
                 for (int key = 0; key < 16; ++key)
 #pragma unroll
                     for (int i = 0; i < ND; ++i) {
-                        frag vf = v_frag(v_now, j * ND + i);
+                        frag vf = v_frag(v_last, j * ND + i);
 #pragma unroll
                         for (int e = 0; e < 8; ++e) vf[e] = 8 * (e / 4) + 4 * h2 + e % 4 == key ? vf[e] : (elem)0.f;
                         const pfx16 y = mma32(vf, pf[j], acc[i]);
@@ -378,35 +426,100 @@ __global__ __launch_bounds__(WAVES * 64, D == 64 ? 3 : 2) void prompt_attn(const
     }
     float sum = lsum + lsum2;
     sum += other_half(sum);
-    if (row >= len) return;
-    const float inv = 1.f / sum;
-    elem* o = reinterpret_cast<elem*>(A.out) + ((int64_t)(begin + row) * A.Hq + hq) * D + 4 * h2;
+    typedef __attribute__((ext_vector_type(4))) elem elem4;
+    if constexpr (SPLIT) {
+        // The waves' sums joined, a thread an eighth of a row.
+        constexpr int OWN = D / 8;
+        static_assert(WAVES == 4 && TILE >= 2 * 32 * D * 4, "two waves' sums in a buffer");
+        __shared__ float s_m[WAVES][32], s_l[WAVES][32];
+        // (the buffers of the blocks, four floats of a row permuted so that the rows of a write meet all banks)
+        auto sums = [&](int w, int line, int four) __attribute__((always_inline)) {
+            return reinterpret_cast<float4*>((w & 2 ? m_v0 : m_k0) + (w & 1) * 32 * D * 4) + line * (D / 4) + (four ^ (line & (D / 4 - 1)));
+        };
+        __syncthreads();
 #pragma unroll
-    for (int i = 0; i < ND; ++i)
+        for (int i = 0; i < ND; ++i)
 #pragma unroll
-        for (int r4 = 0; r4 < 4; ++r4) {
-            typedef __attribute__((ext_vector_type(4))) elem elem4;
-            elem4 y;
-#pragma unroll
-            for (int r = 0; r < 4; ++r) y[r] = (elem)(acc[i][4 * r4 + r] * inv);
-            *reinterpret_cast<elem4*>(o + 32 * i + 8 * r4) = y;
+            for (int r4 = 0; r4 < 4; ++r4)
+                *sums(wave, n32, 8 * i + 2 * r4 + h2) = make_float4(acc[i][4 * r4], acc[i][4 * r4 + 1], acc[i][4 * r4 + 2], acc[i][4 * r4 + 3]);
+        if (h2 == 0) {
+            s_m[wave][n32] = m;
+            s_l[wave][n32] = sum;
         }
-    if (A.lse && h2 == 0)
-        A.lse[(int64_t)hq * A.T + begin + row] = (m - T::kShift + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+        __syncthreads();
+        const int at = tid / 8, d0 = tid % 8 * 4;            // columns d0 .. d0 + 3 of every 32
+        if (row0 + at >= len) return;
+        float M = s_m[0][at], total = 0.f, w[WAVES];
+#pragma unroll
+        for (int i = 1; i < WAVES; ++i) M = fmaxf(M, s_m[i][at]);
+#pragma unroll
+        for (int i = 0; i < WAVES; ++i) {
+            w[i] = __builtin_amdgcn_exp2f(s_m[i][at] - M);
+            total += s_l[i][at] * w[i];
+        }
+        const float inv = 1.f / total;
+        elem* o = reinterpret_cast<elem*>(A.out) + ((int64_t)(begin + row0 + at) * A.Hq + hq) * D + d0;
+#pragma unroll
+        for (int c = 0; c < OWN / 4; ++c) {
+            float y[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < WAVES; ++i) {
+                const float4 x = *sums(i, at, 8 * c + tid % 8);
+                y[0] += x.x * w[i];
+                y[1] += x.y * w[i];
+                y[2] += x.z * w[i];
+                y[3] += x.w * w[i];
+            }
+            elem4 z;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) z[e] = (elem)(y[e] * inv);
+            *reinterpret_cast<elem4*>(o + 32 * c) = z;
+        }
+        if (A.lse && tid % 8 == 0)
+            A.lse[(int64_t)hq * A.T + begin + row0 + at] = (M - T::kShift + __builtin_amdgcn_logf(total)) * 0.6931471805599453f;
+    } else {
+        if (row >= len) return;
+        const float inv = 1.f / sum;
+        elem* o = reinterpret_cast<elem*>(A.out) + ((int64_t)(begin + row) * A.Hq + hq) * D + 4 * h2;
+#pragma unroll
+        for (int i = 0; i < ND; ++i)
+#pragma unroll
+            for (int r4 = 0; r4 < 4; ++r4) {
+                elem4 y;
+#pragma unroll
+                for (int r = 0; r < 4; ++r) y[r] = (elem)(acc[i][4 * r4 + r] * inv);
+                *reinterpret_cast<elem4*>(o + 32 * i + 8 * r4) = y;
+            }
+        if (A.lse && h2 == 0)
+            A.lse[(int64_t)hq * A.T + begin + row] = (m - T::kShift + __builtin_amdgcn_logf(sum)) * 0.6931471805599453f;
+    }
 }
 
 }  // namespace
 
+// Calls whose row tiles would leave compute units idle take the form that splits a row's keys over four waves: it has four
+// times the workgroups, of a quarter of the steps each, and four times the fetches and starts.  Which is faster goes by the
+// rows of all heads (512 workgroups, two per compute unit, at 16384) and, up to twice as many, by how many steps the longest
+// tile has; prompts of under four row tiles have nothing to split.  Whole rows / split, us (bf16): 4 heads x 512 tokens
+// 14.8 / 9.2, x 2048 39.5 / 19.5, x 6000 102 / 73, x 8192 140 / 124, x 12000 223 / 242; 32 heads x 128 8.5 / 6.4, x 512 15.6 /
+// 12.5, x 700 18.0 / 21.4; 12 heads x 2500 48 / 44; 4 heads x four of 2000 40 / 42; 32 heads x eight of 64 8.0 / 9.6, x four of 200
+// 11.2 / 17.4; 20 heads of 64 x 800 14.2 / 8.9.
+bool split_keys(int64_t T, int B, int Hq) {
+    const int64_t rows = T * Hq, mean = T / B;
+    return (rows <= 16384 && mean >= 128) || (rows <= 32768 && mean >= 2048);
+}
+
 hipError_t launch_prompt(int dtype, int D, PromptArgs A, hipStream_t st) {
     A.scale2 = (float)(1.4426950408889634 / std::sqrt((double)D));
-    constexpr int WAVES = 4;
-    constexpr int rows = WAVES * 32;
+    const bool split = split_keys(A.T, A.B, A.Hq);
+    const int rows = split ? 32 : kWaves * 32;
     A.ranks = (int)(A.T / rows) + A.B;                       // every prompt has at most one tile that is not full
     const int64_t groups = (int64_t)A.ranks * A.Hq;
     if (groups >= (int64_t)1 << 31) return hipErrorInvalidValue;
-    auto launch = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)groups), dim3(WAVES * 64), 0, st, A); };
-    if (dtype == 0) D == 128 ? launch(prompt_attn<p_bf16, 128, WAVES>) : launch(prompt_attn<p_bf16, 64, WAVES>);
-    else if (dtype == 2) D == 128 ? launch(prompt_attn<p_f16, 128, WAVES>) : launch(prompt_attn<p_f16, 64, WAVES>);
+    auto launch = [&](auto kern) { hipLaunchKernelGGL(kern, dim3((unsigned)groups), dim3(kWaves * 64), 0, st, A); };
+    auto form = [&](auto wide, auto narrow) { split ? launch(narrow) : launch(wide); };
+    if (dtype == 0) D == 128 ? form(prompt_attn<p_bf16, 128, false>, prompt_attn<p_bf16, 128, true>) : form(prompt_attn<p_bf16, 64, false>, prompt_attn<p_bf16, 64, true>);
+    else if (dtype == 2) D == 128 ? form(prompt_attn<p_f16, 128, false>, prompt_attn<p_f16, 128, true>) : form(prompt_attn<p_f16, 64, false>, prompt_attn<p_f16, 64, true>);
     else return hipErrorInvalidValue;
     return hipGetLastError();
 }

@@ -45,6 +45,34 @@ def test_lengths(snapkv, lengths, D):
     check(q, k, v, cu, out, lse)
 
 
+@pytest.mark.parametrize("lengths", [[1025, 3], [511, 512, 513], [127, 128, 129, 0, 255, 256, 257]], ids=lambda x: "x".join(map(str, x[:7])))
+@pytest.mark.parametrize("D", [64, 128])
+def test_lengths_of_many_heads(snapkv, lengths, D):
+    """Whole rows to a wave: the form of calls that fill the chip (the ones above split the keys of a row over waves)."""
+    gen, T = seeded(sum(lengths) + D), sum(lengths)
+    q, k, v = (rows(gen, T, h, D, torch.float16, "fused") for h in (48, 16, 16))
+    cu = offsets(lengths)
+    out, lse = run(snapkv, q, k, v, cu)
+    check(q, k, v, cu, out, lse)
+
+
+def test_both_forms_agree(snapkv):
+    """The same heads alone (keys split) and among others (whole rows): equal up to rounding, also behind NaN values."""
+    gen, L = seeded(40), 1100
+    q, k, v = (rows(gen, L, h, 128, torch.bfloat16, "tokens") for h in (40, 40, 40))
+    v[700:, :, ::3] = float("nan")
+    cu = offsets([L])
+    wide, wide_lse = run(snapkv, q, k, v, cu)
+    some = [t[:, 8:12].contiguous() for t in (q, k, v)]
+    out, lse = run(snapkv, *some, cu)
+    assert (lse - wide_lse[8:12]).abs().max() <= 1e-5
+    a, b = out.float(), wide[:, 8:12].float()
+    assert torch.equal(torch.isnan(a), torch.isnan(b)) and torch.isfinite(a[:700]).all() and torch.isnan(a[700:, :, ::3]).all()
+    # each within two roundings of the exact value: probabilities (of mean |v|) and the result
+    near = 2 * 2.0 ** -8 * (b.nan_to_num().abs() + float(v[:700].float().abs().mean())) + 1e-4
+    assert ((a - b).nan_to_num().abs() <= near).all()
+
+
 @pytest.mark.parametrize("Hq,Hkv", [(1, 1), (8, 8), (7, 1), (6, 3), (12, 12), (16, 4), (10, 5), (32, 8), (24, 24), (20, 2)])
 @pytest.mark.parametrize("dtype", ["bf16", "f16"])
 def test_heads(snapkv, Hq, Hkv, dtype):
@@ -175,8 +203,10 @@ def test_offsets_outside_the_tensors_are_clamped(snapkv):
     gen = seeded(8)
     q, k, v = (rows(gen, 150, h, 64, torch.bfloat16, "tokens") for h in (2, 2, 2))
     out, lse = run(snapkv, q, k, v, torch.tensor([-7, 60, 40, 1 << 30], dtype=torch.int32, device="cuda"))
-    want = [run(snapkv, q, k, v, torch.tensor([a, e], dtype=torch.int32, device="cuda")) for a, e in ((0, 60), (40, 150))]
-    assert torch.equal(out[:40], want[0][0][:40]) and torch.equal(out[60:], want[1][0][60:])
+    # prompts [0, 60) and [40, 150); rows 40 .. 59 are either's
+    for (a, e), mine in (((0, 60), slice(0, 40)), ((40, 150), slice(60, 150))):
+        want, want_lse, spread, reach = orc.prompt_attention(num(q), num(k), num(v), [a, e])
+        check_attention(num(out)[mine], num(lse)[:, mine].T, want[mine], want_lse[:, mine].T, spread[mine], reach[:, mine].T, e - a, q.dtype, parts=False)
     assert torch.isfinite(out).all() and torch.isfinite(lse).all()
 
 
