@@ -381,7 +381,7 @@ int snapkv_decode_attention(int dtype, const void* q, const void* k_cache, const
  *   q_out   [T, Hq, D] device, the rotated queries (NULL with Hq = 0);  k_out [T, Hkv, D] device or NULL: the rotated keys
  *           once more, for the attention over the prompt; strides as for the inputs
  *
- * Rows that the table has no column for (or before the first) and table entries outside [0, num_pages) are not
+ * T < 2^26.  Rows that the table has no column for (or before the first) and table entries outside [0, num_pages) are not
  * written to pages.  Distinct tokens must not meet in one row of one page.  T = 0 or B = 0 does nothing.  No scratch; calls are independent and
  * may be captured.  Returns SNAPKV_OK or a negative SNAPKV_ERR_* code.
  */
@@ -412,7 +412,7 @@ int snapkv_append_paged(int dtype, const void* q, const void* k, const void* v, 
  *           are left as they were
  *
  * The probabilities are rounded to dtype before the product with v; sums and statistics are float32.  T = 0 or B = 0
- * does nothing.  No scratch; calls are independent, repeat bit for bit and may be captured.  Returns SNAPKV_OK or a negative SNAPKV_ERR_*
+ * does nothing; T < 2^30, (T / 128 + B) Hq < 2^24.  No scratch; calls are independent, repeat bit for bit and may be captured.  Returns SNAPKV_OK or a negative SNAPKV_ERR_*
  * code.
  */
 int snapkv_prompt_attention(int dtype, const void* q, const void* k, const void* v, const int32_t* cu_seqlens, int B,
@@ -433,8 +433,8 @@ int snapkv_prompt_attention(int dtype, const void* q, const void* k, const void*
  *   Hq % Hkv == 0, Hq / Hkv <= 16, D in {64, 128}
  *   out     [B, Hq, D] device, dtype (rounded once from float32);  out_lse [B, Hq] device float32 or NULL
  *   workspace device memory, 256-byte aligned, of at least snapkv_decode_paged_workspace_bytes(B, Hq, Hkv, D, max_len) bytes
- *           (which depends on the compute units of the CURRENT device, and is 0 for steps that are not split: then it may be
- *           NULL), owned by the caller and free to reuse once the enqueued work has finished; its contents do not matter
+ *           (0 for steps that are not split: then it may be NULL; also 0 for shapes that the step refuses), owned by the caller
+ *           and free to reuse once the enqueued work has finished; its contents do not matter
  *
  * Steps with distinct workspaces are independent, and a step may be captured.  Returns SNAPKV_OK or a negative
  * SNAPKV_ERR_* code.

@@ -620,6 +620,7 @@ def snapkv_decode_attention_paged(q: torch.Tensor, k_pages: torch.Tensor, v_page
     int32 (at most max_len rows) -> out [B,Hq,D] of q's dtype and, if given, out_lse [B,Hq] float32.  `workspace`: a uint8
     GPU tensor of snapkv_decode_paged_workspace_bytes; None: allocated by torch for this call, on the current stream."""
     lib = load()
+    max_len = int(max_len)
     B, Hq, D = q.shape
     num_pages, page_size, Hkv, Dk = k_pages.shape
     if Dk != D or v_pages.shape != k_pages.shape:

@@ -1262,7 +1262,7 @@ int snapkv_append_paged(int dtype, const void* q, const void* k, const void* v, 
     if (D != 64 && D != 128) return SNAPKV_ERR_UNSUPPORTED;
     const int e = elem_bytes(dtype);
     if (rot_dim % (32 / e) != 0) return SNAPKV_ERR_UNSUPPORTED;
-    if (T >= (int64_t)1 << 31 || B >= 1 << 24 || Hq + 2 * (int64_t)Hkv > 65535 || num_pages > ((int64_t)1 << 31) ||
+    if (T >= (int64_t)1 << 26 || B >= 1 << 24 || Hq + 2 * (int64_t)Hkv > 65535 || num_pages > ((int64_t)1 << 31) ||
         table_columns > ((int64_t)1 << 31) || n_positions > ((int64_t)1 << 31))
         return SNAPKV_ERR_UNSUPPORTED;
     struct { const void* p; int64_t rows, heads; } const t[] = {
@@ -1323,7 +1323,7 @@ int snapkv_prompt_attention(int dtype, const void* q, const void* k, const void*
     if (T == 0 || B == 0) return SNAPKV_OK;
     if (!q || !k || !v || !cu_seqlens || !out) return SNAPKV_ERR_INVALID_ARG;
     if (dtype == SNAPKV_DTYPE_F32 || (D != 64 && D != 128)) return SNAPKV_ERR_UNSUPPORTED;
-    if (T >= (int64_t)1 << 30 || B >= 1 << 24 || Hq > 65535 || (T / 64 + B) * Hq >= (int64_t)1 << 31) return SNAPKV_ERR_UNSUPPORTED;
+    if (T >= (int64_t)1 << 30 || B >= 1 << 24 || Hq > 65535 || (T / 128 + B) * Hq >= (int64_t)1 << 24) return SNAPKV_ERR_UNSUPPORTED;   // (threads of a launch: 2^32)
     struct { const void* p; int64_t rows, heads; } const t[] = {
         {q, q_row_stride, q_head_stride}, {k, k_row_stride, k_head_stride}, {v, v_row_stride, v_head_stride}};
     for (const auto& x : t) {
@@ -1373,10 +1373,12 @@ int snapkv_decode_attention_paged(int dtype, const void* q, const void* k_pages,
         table_columns > ((int64_t)1 << 31))
         return SNAPKV_ERR_UNSUPPORTED;
     if (max_len > table_columns * page_size) return SNAPKV_ERR_INVALID_ARG;
+    const PagedPlan plan = paged_plan(B, Hq, Hkv, D, max_len);
+    if ((int64_t)plan.nchunk * Hkv >= (int64_t)1 << 24 || (int64_t)B * Hq >= (int64_t)1 << 24) return SNAPKV_ERR_UNSUPPORTED;   // (2^32 threads)
     if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(out)) return SNAPKV_ERR_MISALIGNED;
     for (const void* x : {(const void*)out_lse, (const void*)lens, (const void*)block_table})
         if ((reinterpret_cast<uintptr_t>(x) & 3u) != 0) return SNAPKV_ERR_MISALIGNED;
-    const size_t need = paged_plan(B, Hq, Hkv, D, max_len).bytes;
+    const size_t need = plan.bytes;
     if (need > 0 && (!workspace || workspace_bytes < need)) return SNAPKV_ERR_WORKSPACE;
     if (need > 0 && (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return SNAPKV_ERR_MISALIGNED;
     PagedArgs A{};

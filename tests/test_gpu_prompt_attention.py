@@ -32,7 +32,7 @@ def check(q, k, v, cu, out, lse):
 
 
 LENGTHS = [[1], [2], [1, 1, 1], [31, 32, 33], [63, 64, 65], [127, 128, 129, 0, 255, 256, 257], [0, 5, 0], [700], [1025, 3], [17] * 70,
-           [1] * 200, [511, 512, 513]]
+           [1] * 200, [511, 512, 513], [0, 200, 1, 0, 33, 129] * 13, [7] * 64 + [0] * 70 + [300]]
 
 
 @pytest.mark.parametrize("lengths", LENGTHS, ids=lambda x: "x".join(map(str, x[:7])))
@@ -45,7 +45,7 @@ def test_lengths(snapkv, lengths, D):
     check(q, k, v, cu, out, lse)
 
 
-@pytest.mark.parametrize("lengths", [[1025, 3], [511, 512, 513], [127, 128, 129, 0, 255, 256, 257]], ids=lambda x: "x".join(map(str, x[:7])))
+@pytest.mark.parametrize("lengths", [[1025, 3], [511, 512, 513], [127, 128, 129, 0, 255, 256, 257], [0, 200, 1, 0, 33, 129] * 13], ids=lambda x: "x".join(map(str, x[:7])))
 @pytest.mark.parametrize("D", [64, 128])
 def test_lengths_of_many_heads(snapkv, lengths, D):
     """Whole rows to a wave: the form of calls that fill the chip (the ones above split the keys of a row over waves)."""
@@ -143,6 +143,22 @@ def test_rows_of_no_prompt_are_neither_read_nor_written(snapkv, first, last):
     a, e = first, T - last
     assert (out[:a] == 77).all() and (out[e:] == 77).all() and (lse[:, :a] == 77).all() and (lse[:, e:] == 77).all()
     check(q[a:e], k[a:e], v[a:e], cu - first, out[a:e], lse[:, a:e])
+
+
+def test_thousands_of_prompts(snapkv):
+    """Lengths of 0 to 140 of 4500 prompts behind tokens of none: every one found, none twice."""
+    gen = seeded(60)
+    lengths = (torch.randint(0, 71, (4500,), generator=gen, device="cuda") * (1 + torch.randint(0, 2, (4500,), generator=gen, device="cuda"))).tolist()
+    T = 999 + sum(lengths) + 50
+    q, k, v = (rows(gen, T, h, 64, torch.bfloat16, "tokens") for h in (2, 1, 1))
+    cu = offsets(lengths, 999)
+    out, lse = run(snapkv, q, k, v, cu)
+    assert (out[:999] == 77).all() and (out[T - 50:] == 77).all() and (lse[:, :999] == 77).all() and (lse[:, T - 50:] == 77).all()
+    at = cu.tolist()
+    for some in (range(0, 130), range(2200, 2230), range(4400, 4500)):
+        a, e = at[some[0]], at[some[-1] + 1]
+        check(q[a:e], k[a:e], v[a:e], cu[some[0]:some[-1] + 2] - a, out[a:e], lse[:, a:e])
+    assert torch.isfinite(out).all() and not (lse[:, 999:T - 50] == 77).any()
 
 
 def test_a_prompt_does_not_see_its_neighbours(snapkv):

@@ -24,7 +24,7 @@ def append(**kw):
     (dict(cols=0), -1), (dict(rot=-16), -1), (dict(rot=144), -1), (dict(inter=2), -1), (dict(cos=None), -1), (dict(sin=None), -1),
     (dict(npos=0), -1), (dict(kr=64), -1), (dict(vh=-128), -1), (dict(qor=8), -1), (dict(koh=-8), -1),
     (dict(D=96, kr=96, rot=96), -2), (dict(D=256), -2), (dict(rot=24), -2), (dict(rot=8), -2), (dict(dtype=1, rot=12), -2),
-    (dict(T=1 << 31), -2), (dict(pages=(1 << 31) + 1), -2), (dict(Hq=0, q=None, qo=None, Hkv=40000), -2),
+    (dict(T=1 << 26), -2), (dict(T=1 << 31), -2), (dict(pages=(1 << 31) + 1), -2), (dict(Hq=0, q=None, qo=None, Hkv=40000), -2),
     (dict(q=ODD), -3), (dict(k=ODD), -3), (dict(v=ODD), -3), (dict(qo=ODD), -3), (dict(ko=ODD), -3), (dict(kp=ODD), -3), (dict(vp=ODD), -3),
     (dict(cos=ODD), -3), (dict(sin=ODD), -3), (dict(kr=260), -3), (dict(vh=132), -3), (dict(starts=0x1002), -3), (dict(cu=0x1001), -3),
     (dict(pos=0x1002), -3), (dict(table=0x1002), -3),
@@ -45,7 +45,7 @@ def prompt(**kw):
     (dict(T=0), 0), (dict(B=0), 0), (dict(dtype=-1), -1), (dict(T=-1), -1), (dict(B=-2), -1), (dict(Hq=0), -1), (dict(Hkv=0), -1),
     (dict(Hq=9), -1), (dict(q=None), -1), (dict(k=None), -1), (dict(v=None), -1), (dict(cu=None), -1), (dict(out=None), -1),
     (dict(qr=127), -1), (dict(kh=-1), -1), (dict(dtype=1), -2), (dict(D=96), -2), (dict(D=32), -2), (dict(T=1 << 30), -2),
-    (dict(Hq=65536, Hkv=65536), -2), (dict(kr=(1 << 24) + 8), -2), (dict(vr=(1 << 24) + 8), -2), (dict(q=ODD), -3), (dict(k=ODD), -3), (dict(v=ODD), -3), (dict(out=ODD), -3), (dict(lse=0x1002), -3),
+    (dict(Hq=65536, Hkv=65536), -2), (dict(B=1 << 21), -2), (dict(T=(1 << 30) - 1, Hq=4, Hkv=4), -2), (dict(kr=(1 << 24) + 8), -2), (dict(vr=(1 << 24) + 8), -2), (dict(q=ODD), -3), (dict(k=ODD), -3), (dict(v=ODD), -3), (dict(out=ODD), -3), (dict(lse=0x1002), -3),
     (dict(cu=0x1002), -3), (dict(qr=1028), -3), (dict(vh=4), -3),
 ])
 def test_prompt_attention_refuses(kw, code):
@@ -64,7 +64,7 @@ def decode(**kw):
     (dict(dtype=9), -1), (dict(q=None), -1), (dict(kp=None), -1), (dict(vp=None), -1), (dict(table=None), -1), (dict(lens=None), -1),
     (dict(out=None), -1), (dict(B=0), -1), (dict(Hq=0), -1), (dict(Hkv=0), -1), (dict(Hq=9), -1), (dict(pages=0), -1), (dict(page=0), -1),
     (dict(cols=0), -1), (dict(max_len=0), -1), (dict(max_len=6401), -1), (dict(dtype=1), -2), (dict(D=96), -2), (dict(Hq=34), -2),
-    (dict(B=65536), -2), (dict(max_len=(1 << 30) + 1, cols=1 << 30), -2), (dict(q=ODD), -3), (dict(kp=ODD), -3), (dict(vp=ODD), -3),
+    (dict(B=65536), -2), (dict(Hq=60000, Hkv=60000, max_len=1 << 20, cols=1 << 20), -2), (dict(B=60000, Hq=512, Hkv=32), -2), (dict(max_len=(1 << 30) + 1, cols=1 << 30), -2), (dict(q=ODD), -3), (dict(kp=ODD), -3), (dict(vp=ODD), -3),
     (dict(out=ODD), -3), (dict(lse=0x1002), -3), (dict(lens=0x1002), -3), (dict(table=0x1002), -3), (dict(ws=0x10010), -3),
     (dict(ws=None), -4), (dict(ws_bytes=100), -4),
 ])
