@@ -1374,7 +1374,7 @@ int snapkv_decode_attention_paged(int dtype, const void* q, const void* k_pages,
         return SNAPKV_ERR_UNSUPPORTED;
     if (max_len > table_columns * page_size) return SNAPKV_ERR_INVALID_ARG;
     const PagedPlan plan = paged_plan(B, Hq, Hkv, D, max_len);
-    if ((int64_t)plan.nchunk * Hkv >= (int64_t)1 << 24 || (int64_t)B * Hq >= (int64_t)1 << 24) return SNAPKV_ERR_UNSUPPORTED;   // (2^32 threads)
+    if (((int64_t)plan.nchunk + 7) * B * Hkv >= (int64_t)1 << 24 || (int64_t)B * Hq >= (int64_t)1 << 24) return SNAPKV_ERR_UNSUPPORTED;   // (2^32 threads)
     if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(out)) return SNAPKV_ERR_MISALIGNED;
     for (const void* x : {(const void*)out_lse, (const void*)lens, (const void*)block_table})
         if ((reinterpret_cast<uintptr_t>(x) & 3u) != 0) return SNAPKV_ERR_MISALIGNED;

@@ -304,6 +304,7 @@ struct PagedArgs {
     int64_t table_stride, pages, max_len;
     int B, Hq, Hkv, g, page;
     int chunk, nchunk;                               // keys of a workgroup; workgroups of a (sequence, KV head)
+    bool by_xcd;                                     // how workgroups are dealt out
     unsigned page_magic;                             // r / page = r * page_magic >> page_shift, r < 2^31
     int page_shift;
     float scale2;

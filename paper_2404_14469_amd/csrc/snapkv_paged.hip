@@ -12,7 +12,7 @@
 // at once.  Sequences of one chunk are finished by their workgroup; the partial (max, sum, output) of longer
 // ones are joined by a second kernel.  Rows behind a sequence's end are never read: their lanes read the last row again.
 // The rows of a step (a table entry, then K and V) are looked up one step ahead.  Eight sequences of about 16000 rows, 32 KV
-// heads: 2.07 GB in 380 us, 5.4 TB/s; one of 131072 rows, 8 KV heads 103 us and 6 for the join; one of 2113 rows 6.0 and 3.8.
+// heads: 2.07 GB in 365 us with the join, 5.7 TB/s; one of 131072 rows, 8 KV heads 103 us and 6 for the join; one of 2113 rows 6.0 and 3.8.
 #include "snapkv_attn.h"
 #include "snapkv_internal.h"
 
@@ -36,7 +36,19 @@ __global__ __launch_bounds__(kWaves * 64) void paged_attn(const PagedArgs A) {
     constexpr int ROW = D * 2;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int n16 = lane & 15, kg = lane >> 4;
-    const int kvh = blockIdx.x % A.Hkv, chunk = blockIdx.x / A.Hkv, b = blockIdx.y;    // (heads of one chunk of pages run together)
+    // A share's heads run together.  With several sequences they run on one XCD too (workgroup i runs on XCD i % 8), which then
+    // reads whole rows; share c of sequence s goes to XCD (c + s) % 8, so that the short ones' few do not all meet on the first.
+    int kvh = blockIdx.x % A.Hkv, chunk = blockIdx.x / A.Hkv, b = 0;
+    if (A.by_xcd) {
+        const int pad = (A.nchunk + 7) / 8 * 8, unit = blockIdx.x / (8 * A.Hkv) * 8 + blockIdx.x % 8;
+        kvh = blockIdx.x / 8 % A.Hkv;
+        b = unit / pad;
+        chunk = (unit + b * (pad - 1)) % pad;                  // (unit % pad - b, modulo pad)
+        if (chunk >= A.nchunk) return;
+    } else {
+        b = chunk / A.nchunk;
+        chunk %= A.nchunk;
+    }
     int64_t len = A.lens[b];
     const int S = (int)(len < 0 ? 0 : (len > A.max_len ? A.max_len : len));
     const int begin = chunk * A.chunk;
@@ -289,8 +301,13 @@ hipError_t launch_paged(int dtype, int D, PagedArgs A, void* workspace, hipStrea
         A.part_acc = static_cast<float*>(workspace);
         A.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + ((heads * P.nchunk * D * sizeof(float) + 255) & ~(size_t)255));
     }
+    int64_t units = (int64_t)P.nchunk * A.B;
+    // (8 x 16000 rows, 32 KV heads 366 us so, 378 with heads dealt to XCDs; 32 sequences of 1 to 16384 rows 119 / 121; one of 131072
+    // rows 112 / 109)
+    A.by_xcd = A.B > 1 && units >= 64;
+    if (A.by_xcd) units = (int64_t)((P.nchunk + 7) / 8 * 8) * A.B;
     auto launch = [&](auto step, auto join) {
-        hipLaunchKernelGGL(step, dim3(P.nchunk * A.Hkv, A.B), dim3(kWaves * 64), 0, st, A);
+        hipLaunchKernelGGL(step, dim3((unsigned)(units * A.Hkv)), dim3(kWaves * 64), 0, st, A);
         if (P.nchunk > 1) hipLaunchKernelGGL(join, dim3((unsigned)heads), dim3(kWaves * 64), 0, st, A);
     };
     if (dtype == 0 && D == 128) launch(paged_attn<dec_bf16, 128>, paged_join<dec_bf16, 128>);

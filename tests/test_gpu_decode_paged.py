@@ -43,6 +43,8 @@ CASES = [   # lens, page, Hq, Hkv, D, dtype, room beyond the longest
     ([20000], 64, 4, 2, 64, "bf16", 0),
     ([900, 1], 128, 24, 24, 128, "bf16", 31000),              # cut for far longer sequences
     ([64] * 150, 16, 2, 2, 64, "f16", 0),
+    ([5000, 1, 777, 0, 4096, 130, 129], 16, 8, 4, 128, "bf16", 0),
+    ([1700] * 9 + [40, 3], 8, 3, 3, 64, "bf16", 300),
 ]
 
 
