@@ -7,7 +7,7 @@
 // the matrix units the bound of all but the shortest prompts.
 //
 // Work split.  A workgroup of four waves takes 128 query rows of one head, each wave 32 of them, and walks the keys in tiles of 64 that
-// its waves share through LDS; two workgroups share a compute unit (200 registers and 64 KB each), so one's waits are the
+// its waves share through LDS; two workgroups share a compute unit (230 registers and 64 KB each), so one's waits are the
 // other's time.  Calls of few rows give a workgroup 32 rows, and each wave every fourth block of 32 keys (split_keys says which).
 // 32749 tokens of 32/8 heads of 128 take 7.7 ms, 1.14 PFLOP/s, 84 % of a 16384^3 bf16 product's rate: the matrix units work in 62 %
 // of the cycles and the card is at its power limit (1.63 GHz).  A batch of 7499 tokens in eight prompts takes 0.13 ms, 4 heads
@@ -16,15 +16,15 @@
 // MFMA layout (32x32x16, 64 lanes): lane l supplies row (left operand) or column (right operand) l%32 and contraction
 // elements 8*(l/32) .. +7; accumulator register r of lane l is row 8*(r/4) + 4*(l/32) + r%4, column l%32.
 //
-//   logits^T = K Q^T: a lane gets 16 logits of ONE query per 32 keys, so the softmax is arithmetic within the lane and one
-//     exchange with the lane that has the other half of the keys; the maximum, the sum and the factor that rescales the
-//     output are one register each.
+//   logits^T = K Q^T: a lane gets 16 logits of ONE query per 32 keys, so the softmax is arithmetic within the lane (and, when
+//     the shift moves, one exchange with the lane that has the other half of the keys); the shift, the sum and the factor that
+//     rescales the output are one register each.
 //   out^T = V^T P^T: contraction element e of lane l stands for key 8*(e/4) + 4*(l/32) + e%4 of 16, which is where the
 //     logits left that key's probability: P never moves between lanes.  V^T comes from LDS by the transposing read (a lane
 //     gets four keys of one column).
 //
 // The probabilities enter the last product rounded to the storage type, as its operand must be: each is off by at most half
-// a step (bf16 2^-8, fp16 2^-11, relative; the fp16 ones are taken 2^8 times as large, so those down to 2^-22 of the
+// a step (bf16 2^-8, fp16 2^-11, relative; the fp16 ones are taken 2^7 times as large, so those down to 2^-21 of the
 // largest are normal numbers), which adds to an output about what its own rounding does.  Their sum is taken in fp32 from
 // the unrounded values.
 #include "snapkv_internal.h"
@@ -58,7 +58,6 @@ __device__ __forceinline__ pfx16 mma32(pf16x8 a, pf16x8 b, pfx16 c) { return __b
 constexpr int kKeys = 64;      // keys of a tile
 constexpr int kWaves = 4;
 
-typedef const __attribute__((address_space(1))) void* global_ptr;
 typedef __attribute__((address_space(3))) void* lds_ptr;
 typedef __attribute__((address_space(3))) char* lds_char;
 typedef __attribute__((address_space(3))) ps16x4* lds_s16x4;
@@ -182,8 +181,6 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 && !SPLIT ? 3 : 2) void prompt
 
     const char* kh = A.k + (int64_t)kvh * A.k_hs + (int64_t)begin * A.k_rs;
     const char* vh = A.v + (int64_t)kvh * A.v_hs + (int64_t)begin * A.v_rs;
-    const int last = min(len, (tile + 1) * ROWS) - 1;        // the last key any of the tile's rows sees
-    const int ntiles = last / kKeys + 1;
     const int mine = row0 < len ? row0 / 32 + 1 : 0;         // blocks of 32 keys that the wave's rows see; the last one in part
 
     // Loads of 64 keys by all waves, or (split) of 32 by each: SHARE KB at a time, a KB (RPL rows) per wave, straight into LDS.
@@ -331,6 +328,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 && !SPLIT ? 3 : 2) void prompt
     auto begin_with = [&](int b, lds_char s_k) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < NQ; ++i) product(k_frag(s_k, i), i, xa);
+        __builtin_amdgcn_sched_barrier(0);                   // (the products stand in front of the loads that reuse the buffer)
         hide(b, xa);
         big = xa[0];
 #pragma unroll
@@ -367,6 +365,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 && !SPLIT ? 3 : 2) void prompt
     } else {
         // Keys are half a tile ahead of values: tile t of V is blocks 2 t and 2 t + 1, that of K blocks 2 t + 1 and 2 t + 2, whose
         // logits are taken meanwhile.  The next tiles arrive in the other two buffers.
+        const int ntiles = (min(len, (tile + 1) * ROWS) - 1) / kKeys + 1;      // of keys that any of the rows sees
         auto two_blocks = [&](int t, lds_char k_now, lds_char k_free, lds_char v_now, lds_char v_free) __attribute__((always_inline)) {
             fetched();
             __syncthreads();                                 // these tiles have arrived, the others have been read

@@ -13,7 +13,8 @@ relative to a value, w = 2^-24 that of float32.
   output     a mean of v under probabilities that are rounded by at most c relative (prompts: c = u; one new token: two parts of
              the storage type, c = 2^-14 for bf16, 2^-20 for fp16), then rounded once:
              |got - want| <= u |want| + (c + 2 d + 2 n w) spread, spread = the mean of |v| under the same probabilities
-             (fp16 probabilities below 2^-22 of the largest lose up to 2^-33 of it each: n 2^-33 more)
+             (fp16 probabilities are taken 2^7 times as large: those below 2^-14 / 2^7 of the largest are subnormal and lose up to half of
+             2^-24, 2^-32 of it, each: n 2^-32 more)
   lse        d + n w + 2 w |lse|
 """
 import numpy as np
@@ -35,7 +36,7 @@ def check_attention(got, got_lse, want, want_lse, spread, reach, n, dtype, parts
     """want, spread [..., D]; want_lse, reach [...] in the same order; n: rows that a query can see, at most."""
     D = want.shape[-1]
     u = half_step(dtype)
-    c = {True: {torch.bfloat16: 2.0 ** -14, torch.float16: 2.0 ** -20}, False: {torch.bfloat16: u, torch.float16: u + n * 2.0 ** -33}}[parts][dtype]
+    c = {True: {torch.bfloat16: 2.0 ** -14, torch.float16: 2.0 ** -20}, False: {torch.bfloat16: u, torch.float16: u + n * 2.0 ** -32}}[parts][dtype]
     d = 2 * (D + 4) * W24 * reach + 2.0 ** -20
     bound = u * np.abs(want) + (c + 2 * d[..., None] + 2 * n * W24) * spread + 1e-30
     err = np.abs(got - want)
