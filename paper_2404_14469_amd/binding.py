@@ -7,6 +7,7 @@ if the library has not been built, loading raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import Optional, Tuple
 
@@ -609,6 +610,7 @@ def snapkv_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, c
         _at(out_lse, "out_lse", torch.float32, dev) if out_lse is not None else None, _stream(stream)))
 
 
+@functools.lru_cache(maxsize=256)
 def snapkv_decode_paged_workspace_bytes(B: int, Hq: int, Hkv: int, D: int, max_len: int) -> int:
     return int(load().snapkv_decode_paged_workspace_bytes(B, Hq, Hkv, D, max_len))
 
@@ -637,7 +639,7 @@ def snapkv_decode_attention_paged(q: torch.Tensor, k_pages: torch.Tensor, v_page
     if workspace is None:
         if stream is not None and st != _stream(None):
             raise ValueError("a step on another stream than the current one needs a workspace of the caller's")
-        need = lib.snapkv_decode_paged_workspace_bytes(B, Hq, Hkv, D, max_len)
+        need = snapkv_decode_paged_workspace_bytes(B, Hq, Hkv, D, max_len)
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
     ws, size = (_at(workspace, "workspace", torch.uint8, dev), workspace.numel()) if workspace is not None else (None, 0)
     _check(lib.snapkv_decode_attention_paged(_dtype_code(q), *ins, max_len, B, Hq, Hkv, D, *outs, ws, size, st))
