@@ -43,13 +43,13 @@ typedef __attribute__((ext_vector_type(4))) unsigned pu32x4;
 struct p_bf16 {
     typedef __bf16 elem;
     typedef pbf16x8 frag;
-    static constexpr float kShift = 0.f;
+    static constexpr float kShift = 0.f, kMost = 256.f;      // exponent that the probabilities are raised by; most that 16 may sum up to
     static constexpr unsigned kExp = 0x7F80;                 // all ones: an infinity or NaN
 };
 struct p_f16 {
     typedef _Float16 elem;
     typedef pf16x8 frag;
-    static constexpr float kShift = 7.f;
+    static constexpr float kShift = 7.f, kMost = 32768.f;    // (below fp16's largest number)
     static constexpr unsigned kExp = 0x7C00;
 };
 __device__ __forceinline__ pfx16 mma32(pbf16x8 a, pbf16x8 b, pfx16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
@@ -169,10 +169,9 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 && !SPLIT ? 3 : 2) void prompt
     const char* qr = A.q + (int64_t)(begin + min(row, len - 1)) * A.q_rs + (int64_t)hq * A.q_hs + h2 * 16;
 #pragma unroll
     for (int c = 0; c < NC; ++c) qf[c] = *reinterpret_cast<const frag*>(qr + 32 * c);
-    // The shift of the exponentials, and the largest logit, unscaled, that it is good for.  (The shift starts finite: logits of
-    // -infinity, if a row sees nothing else yet, then have probability 0 and not NaN.)
-    float m = -3.4028235e38f, limit = -INFINITY;
-    float lsum = 0.f, lsum2 = 0.f;                           // (two sums: shorter chains)
+    // The shift of the exponentials (finite from the start: logits of -infinity, if a row sees nothing else yet, then have
+    // probability 0 and not NaN) and their sum.
+    float m = -3.4028235e38f, lsum = 0.f;
     pfx16 acc[ND];
 #pragma unroll
     for (int i = 0; i < ND; ++i)
@@ -244,43 +243,47 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 && !SPLIT ? 3 : 2) void prompt
         for (int r = 0; r < 16; ++r)
             if (8 * (r / 4) + r % 4 > seen) x[r] = -INFINITY;
     };
-    // The shift of the exponentials need not be the maximum itself: it is moved, and sums and outputs rescaled, only when
-    // some row of the wave has outgrown it by 2^8.
-    auto rescale = [&](float big) __attribute__((always_inline)) {
-        if (__any(big > limit)) {
+    // The probabilities of logits 2 n and 2 n + 1 of a lane's 16, and their sums (two: shorter chains).
+    auto two = [&](const pfx16& x, int n, float shift, frag* pf, float* sum) __attribute__((always_inline)) {
+        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[2 * n], A.scale2, shift));
+        const float q = __builtin_amdgcn_exp2f(__builtin_fmaf(x[2 * n + 1], A.scale2, shift));
+        sum[0] = n == 0 ? p : sum[0] + p;
+        sum[1] = n == 0 ? q : sum[1] + q;
+        pf[n / 4][2 * n % 8] = (elem)p;
+        pf[n / 4][2 * n % 8 + 1] = (elem)q;
+    };
+    // The shift need not be the maximum: it is moved to it, sums and outputs rescaled and the block's probabilities taken anew,
+    // only when those of some lane of the wave sum up to more than 2^8 times what the maximum alone would give.  So no
+    // probability is larger than that, and no maximum is looked for as long as none is.
+    auto settle = [&](const pfx16& x, frag* pf, float* sum) __attribute__((always_inline)) {
+        if (__any(sum[0] + sum[1] > T::kMost)) {
+            float big = x[0];
+#pragma unroll
+            for (int r = 1; r < 16; ++r) big = fmaxf(big, x[r]);
             const float mn = fmaxf(m, fmaxf(big, other_half(big)) * A.scale2);
             const float alpha = __builtin_amdgcn_exp2f(m - mn);
             m = mn;
-            limit = (mn + 8.f) / A.scale2;
             lsum *= alpha;
-            lsum2 *= alpha;
 #pragma unroll
             for (int i = 0; i < ND; ++i)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) acc[i][r] *= alpha;
+#pragma unroll
+            for (int n = 0; n < 8; ++n) two(x, n, T::kShift - m, pf, sum);
         }
-    };
-    // The probabilities of logits 2 n and 2 n + 1 of a lane's 16.
-    auto two = [&](const pfx16& x, int n, float shift, frag* pf) __attribute__((always_inline)) {
-        const float p = __builtin_amdgcn_exp2f(__builtin_fmaf(x[2 * n], A.scale2, shift));
-        const float q = __builtin_amdgcn_exp2f(__builtin_fmaf(x[2 * n + 1], A.scale2, shift));
-        lsum += p;
-        lsum2 += q;
-        pf[n / 4][2 * n % 8] = (elem)p;
-        pf[n / 4][2 * n % 8 + 1] = (elem)q;
+        lsum += sum[0] + sum[1];
     };
     // Software pipeline: the logits of the wave's next block are products that nothing of block b's softmax waits for, so between two
     // matrix instructions stand a few of the softmax's.  Operands are read from LDS AHEAD products before their own.
-    constexpr int AHEAD = SPLIT ? 2 : 3, PAIRS = 8, EARLY = 5;
-    float big;
+    constexpr int AHEAD = SPLIT ? 2 : 3;
     pfx16 xa, xb;
     auto pass = [&](int b, const pfx16& x, pfx16& xn, lds_char k_next, lds_char v_now) __attribute__((always_inline)) {
         if (b + STEP >= mine) return;
         frag pf[2], kf[NQ], vf[NV];
+        float sum[2];
         if constexpr (SPLIT) fetched<PER>();                 // its keys; its values (PER loads) may still be on their way
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) kf[i] = k_frag(k_next, i);
-        rescale(big);
         const float shift = T::kShift - m;
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -290,28 +293,18 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 && !SPLIT ? 3 : 2) void prompt
             else vf[i + AHEAD - NQ] = v_frag(v_now, i + AHEAD - NQ);
             product(kf[i], i, xn);
 #pragma unroll
-            for (int n = i * EARLY / NQ; n < (i + 1) * EARLY / NQ; ++n) two(x, n, shift, pf);
+            for (int n = i * 8 / NQ; n < (i + 1) * 8 / NQ; ++n) two(x, n, shift, pf, sum);
             __builtin_amdgcn_sched_barrier(0);
         }
         if constexpr (SPLIT)                                 // (all products with the keys there have been issued, so they have been read)
             if (b + 2 * STEP < mine) load_k((b + 2 * STEP) * 32, k_next);
-#pragma unroll
-        for (int i = 0; i < ND; ++i) {
-            if (i + AHEAD < NV) vf[i + AHEAD] = v_frag(v_now, i + AHEAD);
-            acc[i] = mma32(vf[i], pf[0], acc[i]);
-#pragma unroll
-            for (int n = EARLY + i * (PAIRS - EARLY) / ND; n < EARLY + (i + 1) * (PAIRS - EARLY) / ND; ++n) two(x, n, shift, pf);
-            __builtin_amdgcn_sched_barrier(0);
-        }
+        settle(x, pf, sum);
         hide(b + STEP, xn);
         __builtin_amdgcn_sched_barrier(0);
-        big = xn[0];
 #pragma unroll
-        for (int i = 0; i < ND; ++i) {
-            if (ND + i + AHEAD < NV) vf[ND + i + AHEAD] = v_frag(v_now, ND + i + AHEAD);
-            acc[i] = mma32(vf[ND + i], pf[1], acc[i]);
-#pragma unroll
-            for (int r = i * 16 / ND; r < (i + 1) * 16 / ND; ++r) big = fmaxf(big, xn[r]);
+        for (int i = 0; i < NV; ++i) {
+            if (i + AHEAD < NV) vf[i + AHEAD] = v_frag(v_now, i + AHEAD);
+            acc[i % ND] = mma32(vf[i], pf[i / ND], acc[i % ND]);
             __builtin_amdgcn_sched_barrier(0);
         }
         if constexpr (SPLIT) load_v((b + STEP) * 32, v_now);
@@ -330,9 +323,6 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 && !SPLIT ? 3 : 2) void prompt
         for (int i = 0; i < NQ; ++i) product(k_frag(s_k, i), i, xa);
         __builtin_amdgcn_sched_barrier(0);                   // (the products stand in front of the loads that reuse the buffer)
         hide(b, xa);
-        big = xa[0];
-#pragma unroll
-        for (int r = 1; r < 16; ++r) big = fmaxf(big, xa[r]);
     };
     lds_char v_last = s_v0;                                  // values of the wave's last block
     if constexpr (SPLIT) {
@@ -398,10 +388,10 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 && !SPLIT ? 3 : 2) void prompt
     if (SPLIT ? wave < mine : mine > 0) {
         const int b = SPLIT ? wave + (mine - 1 - wave) / STEP * STEP : mine - 1;
         frag pf[2];
-        rescale(big);
-        const float shift = T::kShift - m;
+        float sum[2];
 #pragma unroll
-        for (int n = 0; n < 8; ++n) two(xa, n, shift, pf);
+        for (int n = 0; n < 8; ++n) two(xa, n, T::kShift - m, pf, sum);
+        settle(xa, pf, sum);
         bool spoiled = false;
 #pragma unroll
         for (int i = 0; i < ROW * 32 / 1024; ++i) {
@@ -428,8 +418,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 && !SPLIT ? 3 : 2) void prompt
                     }
         }
     }
-    float sum = lsum + lsum2;
-    sum += other_half(sum);
+    const float sum = lsum + other_half(lsum);
     typedef __attribute__((ext_vector_type(4))) elem elem4;
     if constexpr (SPLIT) {
         // The waves' sums joined, a thread an eighth of a row.
