@@ -7,11 +7,11 @@
 // the matrix units the bound of all but the shortest prompts.
 //
 // Work split.  A workgroup of four waves takes 128 query rows of one head, each wave 32 of them, and walks the keys in tiles of 64 that
-// its waves share through LDS; two workgroups share a compute unit (230 registers and 64 KB each), so one's waits are the
+// its waves share through LDS; two workgroups share a compute unit (249 registers and 64 KB each), so one's waits are the
 // other's time.  Calls of few rows give a workgroup 32 rows, and each wave every fourth block of 32 keys (split_keys says which).
-// 32749 tokens of 32/8 heads of 128 take 7.7 ms, 1.14 PFLOP/s, 84 % of a 16384^3 bf16 product's rate: the matrix units work in 62 %
-// of the cycles and the card is at its power limit (1.63 GHz).  A batch of 7499 tokens in eight prompts takes 0.13 ms, 4 heads
-// of 2048 tokens 20 us, 78 tokens 7 us, where finding the tile, fetching and storing are most of the time.
+// 32749 tokens of 32/8 heads of 128 take 7.1 ms, 1.24 PFLOP/s, 91 % of a 16384^3 bf16 product's rate, with the card at its power
+// limit.  A batch of 7499 tokens in eight prompts takes 0.13 ms, 4 heads of 2048 tokens 17 us, 78 tokens 7 us, where finding
+// the tile, fetching and storing are most of the time.
 //
 // MFMA layout (32x32x16, 64 lanes): lane l supplies row (left operand) or column (right operand) l%32 and contraction
 // elements 8*(l/32) .. +7; accumulator register r of lane l is row 8*(r/4) + 4*(l/32) + r%4, column l%32.
@@ -243,30 +243,21 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 && !SPLIT ? 3 : 2) void prompt
         for (int r = 0; r < 16; ++r)
             if (8 * (r / 4) + r % 4 > seen) x[r] = -INFINITY;
     };
-    // The probabilities of logits 2 n and 2 n + 1 of a lane's 16 and their sums (two: shorter chains), in three stages, so that
-    // none waits for the one before where several pairs are on their way.
-    auto argue = [&](const pfx16& x, int n, float shift, float* e) __attribute__((always_inline)) {
-        e[2 * n] = __builtin_fmaf(x[2 * n], A.scale2, shift);
-        e[2 * n + 1] = __builtin_fmaf(x[2 * n + 1], A.scale2, shift);
-    };
-    auto raise = [&](int n, float* e) __attribute__((always_inline)) {
-        e[2 * n] = __builtin_amdgcn_exp2f(e[2 * n]);
-        e[2 * n + 1] = __builtin_amdgcn_exp2f(e[2 * n + 1]);
-    };
-    auto collect = [&](int n, const float* e, frag* pf, float* sum) __attribute__((always_inline)) {
-        sum[0] = n == 0 ? e[0] : sum[0] + e[2 * n];
-        sum[1] = n == 0 ? e[1] : sum[1] + e[2 * n + 1];
-        pf[n / 4][2 * n % 8] = (elem)e[2 * n];
-        pf[n / 4][2 * n % 8 + 1] = (elem)e[2 * n + 1];
-    };
+    // The probabilities of a lane's 16 logits, rounded to pf, and their sums (two: shorter chains), in three stages, so that no
+    // instruction waits for the one before.
     auto probabilities = [&](const pfx16& x, frag* pf, float* sum) __attribute__((always_inline)) {
+        const float shift = T::kShift - m;
         float e[16];
 #pragma unroll
-        for (int n = 0; n < 8; ++n) argue(x, n, T::kShift - m, e);
+        for (int r = 0; r < 16; ++r) e[r] = __builtin_fmaf(x[r], A.scale2, shift);
 #pragma unroll
-        for (int n = 0; n < 8; ++n) raise(n, e);
+        for (int r = 0; r < 16; ++r) e[r] = __builtin_amdgcn_exp2f(e[r]);
+        sum[0] = e[0];
+        sum[1] = e[1];
 #pragma unroll
-        for (int n = 0; n < 8; ++n) collect(n, e, pf, sum);
+        for (int r = 2; r < 16; ++r) sum[r & 1] += e[r];
+#pragma unroll
+        for (int r = 0; r < 16; ++r) pf[r / 8][r % 8] = (elem)e[r];
     };
     // The shift need not be the maximum: it is moved to it, sums and outputs rescaled and the block's probabilities taken anew,
     // only when those of some lane of the wave sum up to more than 2^8 times what the maximum alone would give.  So no
@@ -288,55 +279,43 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 && !SPLIT ? 3 : 2) void prompt
         }
         lsum += sum[0] + sum[1];
     };
-    // Software pipeline: the logits of the wave's next block are products that nothing of block b's softmax waits for, so between two
-    // matrix instructions stand a few of the softmax's, each stage of a pair a product behind the one before.  Operands are
-    // read from LDS AHEAD products before their own.
+    // A block's softmax, which only vector instructions do, then the products of the wave's next block's logits (which take the
+    // place of this one's) and of this block's part of the output, which only matrix instructions do: the other wave of the SIMD
+    // is in the other half meanwhile, and a wave with products goes first (32749 tokens 7.27 -> 7.08 ms; with the softmax's
+    // instructions between the logits' products instead 7.1 to 7.4, and two prompts with 20 heads of 64 103 us instead of 98).
+    // Operands are read from LDS AHEAD products before their own.
     constexpr int AHEAD = SPLIT ? 2 : 3;
-    pfx16 xa, xb;
-    auto pass = [&](int b, const pfx16& x, pfx16& xn, lds_char k_next, lds_char v_now) __attribute__((always_inline)) {
+    pfx16 x;
+    auto pass = [&](int b, lds_char k_next, lds_char v_now) __attribute__((always_inline)) {
         if (b + STEP >= mine) return;
         frag pf[2], kf[NQ], vf[NV];
         float sum[2];
         if constexpr (SPLIT) fetched<PER>();                 // its keys; its values (PER loads) may still be on their way
 #pragma unroll
         for (int i = 0; i < AHEAD; ++i) kf[i] = k_frag(k_next, i);
-        // The wave that has exponentials to take goes first; the other one's products of P and V, which need few instructions, run
-        // meanwhile (32749 tokens 7.45 -> 7.09 ms, 131071 tokens of 4 heads 15.0 -> 14.3).
-        if constexpr (!SPLIT) __builtin_amdgcn_s_setprio(1);
-        const float shift = T::kShift - m;
-        constexpr int G = 8 / NQ;                            // pairs per product
-        float e[16];
-#pragma unroll
-        for (int n = 0; n < 2 * G; ++n) argue(x, n, shift, e);
-#pragma unroll
-        for (int n = 0; n < G; ++n) raise(n, e);
+        __builtin_amdgcn_sched_barrier(0);
+        probabilities(x, pf, sum);
+        settle(x, pf, sum);
+        __builtin_amdgcn_s_setprio(1);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < NQ; ++i) {
             if (SPLIT && i + AHEAD == NQ) fetched();
             if (i + AHEAD < NQ) kf[i + AHEAD] = k_frag(k_next, i + AHEAD);
             else vf[i + AHEAD - NQ] = v_frag(v_now, i + AHEAD - NQ);
-            product(kf[i], i, xn);
-#pragma unroll
-            for (int n = i * G; n < (i + 1) * G; ++n) {
-                if (n + G < 8) raise(n + G, e);
-                if (n + 2 * G < 8) argue(x, n + 2 * G, shift, e);
-                collect(n, e, pf, sum);
-            }
+            product(kf[i], i, x);
             __builtin_amdgcn_sched_barrier(0);
         }
         if constexpr (SPLIT)                                 // (all products with the keys there have been issued, so they have been read)
             if (b + 2 * STEP < mine) load_k((b + 2 * STEP) * 32, k_next);
-        settle(x, pf, sum);
-        if constexpr (!SPLIT) __builtin_amdgcn_s_setprio(0);
-        hide(b + STEP, xn);
-        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             if (i + AHEAD < NV) vf[i + AHEAD] = v_frag(v_now, i + AHEAD);
             acc[i % ND] = mma32(vf[i], pf[i / ND], acc[i % ND]);
             __builtin_amdgcn_sched_barrier(0);
         }
+        __builtin_amdgcn_s_setprio(0);
+        hide(b + STEP, x);
         if constexpr (SPLIT) load_v((b + STEP) * 32, v_now);
     };
     // (a lane's places are kept as they are, and a buffer's address is the constant offset of a read: sums of the two, made once
@@ -350,9 +329,9 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 && !SPLIT ? 3 : 2) void prompt
     };
     auto begin_with = [&](int b, lds_char s_k) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < NQ; ++i) product(k_frag(s_k, i), i, xa);
+        for (int i = 0; i < NQ; ++i) product(k_frag(s_k, i), i, x);
         __builtin_amdgcn_sched_barrier(0);                   // (the products stand in front of the loads that reuse the buffer)
-        hide(b, xa);
+        hide(b, x);
     };
     lds_char v_last = s_v0;                                  // values of the wave's last block
     if constexpr (SPLIT) {
@@ -368,18 +347,9 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 && !SPLIT ? 3 : 2) void prompt
             if (b + STEP < mine) load_k((b + STEP) * 32, s_k0);
             fetched();
         }
-        auto block = [&](const pfx16& x, pfx16& xn) __attribute__((always_inline)) {
+        for (; b + STEP < mine; b += STEP) {
             keep_places();
-            pass(b, x, xn, s_k0, s_v0);
-            b += STEP;
-        };
-        while (b + STEP < mine) {
-            block(xa, xb);
-            if (b + STEP >= mine) {
-                xa = xb;
-                break;
-            }
-            block(xb, xa);
+            pass(b, s_k0, s_v0);
         }
         fetched();
     } else {
@@ -394,9 +364,8 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 && !SPLIT ? 3 : 2) void prompt
                 load_k((t + 1) * kKeys + 32, k_free);
                 load_v((t + 1) * kKeys, v_free);
             }
-            pass(2 * t, xa, xb, k_now, v_now);
-            if (2 * t + 2 == mine) xa = xb;                  // (the wave's last block: its logits wait there for the end)
-            pass(2 * t + 1, xb, xa, k_now + 32 * ROW, v_now + 32 * ROW);
+            pass(2 * t, k_now, v_now);
+            pass(2 * t + 1, k_now + 32 * ROW, v_now + 32 * ROW);
         };
         load_k(0, s_k1);
         load_k(32, s_k0);
@@ -412,15 +381,15 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 && !SPLIT ? 3 : 2) void prompt
         }
         v_last = ((mine - 1) & 2 ? s_v1 : s_v0) + ((mine - 1) & 1) * 32 * ROW;   // (one of the last two tiles, which are still there)
     }
-    // The wave's last block; its logits are in xa.  The last one that rows see they see in part.  Values that a row does not see
+    // The wave's last block; its logits are in x.  The last one that rows see they see in part.  Values that a row does not see
     // have probability 0, but 0 times an infinity or NaN is not 0: where the block holds such a value, its keys are added one by
     // one (the others' values taken as zeros) and the sums of rows that do not see the key kept.
     if (SPLIT ? wave < mine : mine > 0) {
         const int b = SPLIT ? wave + (mine - 1 - wave) / STEP * STEP : mine - 1;
         frag pf[2];
         float sum[2];
-        probabilities(xa, pf, sum);
-        settle(xa, pf, sum);
+        probabilities(x, pf, sum);
+        settle(x, pf, sum);
         bool spoiled = false;
 #pragma unroll
         for (int i = 0; i < ROW * 32 / 1024; ++i) {
@@ -521,14 +490,14 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 && !SPLIT ? 3 : 2) void prompt
 
 // Calls whose row tiles would leave compute units idle take the form that splits a row's keys over four waves: it has four
 // times the workgroups, of a quarter of the steps each, and four times the fetches and starts.  Which is faster goes by the
-// rows of all heads (512 workgroups, two per compute unit, at 16384) and, up to twice as many, by how many steps the longest
-// tile has; prompts of under four row tiles have nothing to split.  Whole rows / split, us (bf16): 4 heads x 512 tokens
-// 14.8 / 9.2, x 2048 39.5 / 19.5, x 6000 102 / 73, x 8192 140 / 124, x 12000 223 / 242; 32 heads x 128 8.5 / 6.4, x 512 15.6 /
-// 12.5, x 700 18.0 / 21.4; 12 heads x 2500 48 / 44; 4 heads x four of 2000 40 / 42; 32 heads x eight of 64 8.0 / 9.6, x four of 200
-// 11.2 / 17.4; 20 heads of 64 x 800 14.2 / 8.9.
+// rows of all heads (512 workgroups, two per compute unit, at 16384) and, beyond that, by how many steps the longest tile
+// has, which the mean length stands for; prompts of under four row tiles have nothing to split.  Whole rows / split, us (bf16): 4
+// heads x 512 tokens 14.7 / 8.5, x 2048 39 / 17, x 8192 138 / 98, x 12000 213 / 197; 32 heads x 128 8.4 / 6.4, x 512 15.0 / 10.8, x
+// 700 17.5 / 19.0, x 1024 24.4 / 24.7; 12 heads x 2500 48 / 38; 4 heads x four of 2000 40 / 34; 32 heads x eight of 64 7.7 / 8.8, x
+// four of 200 10.6 / 16.1; 20 heads of 64 x 800 14.1 / 8.4, x 1600 24.3 / 15.9.
 bool split_keys(int64_t T, int B, int Hq) {
     const int64_t rows = T * Hq, mean = T / B;
-    return (rows <= 16384 && mean >= 128) || (rows <= 32768 && mean >= 2048);
+    return (rows <= 16384 && mean >= 128) || (rows <= 32768 && mean >= 1200) || (rows <= 49152 && mean >= 8192);
 }
 
 hipError_t launch_prompt(int dtype, int D, PromptArgs A, hipStream_t st) {
