@@ -522,6 +522,11 @@ def _rows(t: torch.Tensor, name: str, dtype, device: int, T: int, H: int, D: int
     return t.data_ptr(), rs if T > 1 else D, hs if H > 1 else 0
 
 
+def _stream_on(device: int, stream) -> int:
+    """_stream, for the current device, which is known."""
+    return _raw_stream(device) if stream is None and _raw_stream is not None else _stream(stream)
+
+
 def _wrong(t, name, dtype, device):
     if not t.is_cuda:
         raise ValueError(f"{name} must be a GPU tensor")
@@ -552,31 +557,38 @@ def snapkv_append_paged(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor,
     sequence.  With cos/sin [positions, rot_dim/2] float32 the keys, and q [T,Hq,D] -> q_out, are rotated by positions [T]
     int32 (None: the rows); k_out [T,Hkv,D]: the rotated keys once more."""
     lib = load()
-    T, Hkv, D = k.shape
-    num_pages, page_size, Hp, Dp = k_pages.shape
-    if v.shape != k.shape or Hp != Hkv or Dp != D or v_pages.shape != k_pages.shape:
+    T, Hkv, D = rows = k.shape
+    num_pages, page_size, Hp, Dp = pool = k_pages.shape
+    if v.shape != rows or Hp != Hkv or Dp != D or v_pages.shape != pool:
         raise ValueError("k, v, k_pages and v_pages disagree on their shapes")
-    if block_table.dim() != 2 or starts.shape != block_table.shape[:1]:
-        raise ValueError("block_table must be [B, columns] and starts [B]")
+    if block_table.ndim != 2:
+        raise ValueError("block_table must be [B, columns]")
     B, columns = block_table.shape
+    if starts.shape != (B,):
+        raise ValueError("starts must be [B]")
     if cu_seqlens is not None and cu_seqlens.shape != (B + 1,):
         raise ValueError("cu_seqlens must be [B + 1]")
     if positions is not None and positions.shape != (T,):
         raise ValueError("positions must be [T]")
-    if (cos is None) != (sin is None) or (cos is not None and (cos.dim() != 2 or cos.shape != sin.shape)):
-        raise ValueError("cos and sin must both be [positions, rot_dim / 2]")
-    if (q is None) != (q_out is None) or (q is not None and (q.dim() != 3 or q.shape != q_out.shape or q.shape[0] != T or q.shape[2] != D)):
-        raise ValueError("q and q_out must both be [T, Hq, D]")
-    if k_out is not None and k_out.shape != k.shape:
+    P = half = Hq = 0
+    if cos is not None or sin is not None:
+        if cos is None or sin is None or cos.ndim != 2 or sin.shape != cos.shape:
+            raise ValueError("cos and sin must both be [positions, rot_dim / 2]")
+        P, half = cos.shape
+    if q is not None or q_out is not None:
+        if q is None or q_out is None or q.ndim != 3 or q_out.shape != q.shape:
+            raise ValueError("q and q_out must both be [T, Hq, D]")
+        Tq, Hq, Dq = q.shape
+        if Tq != T or Dq != D:
+            raise ValueError("q and q_out must both be [T, Hq, D]")
+    if k_out is not None and k_out.shape != rows:
         raise ValueError("k_out must be [T, Hkv, D]")
     dev, dt, none, i32 = _device_of(k, "k"), k.dtype, (None, 0, 0), torch.int32
-    Hq = q.shape[1] if q is not None else 0
     kp, kr, kh = _rows(k, "k", dt, dev, T, Hkv, D)
     vp, vr, vh = _rows(v, "v", dt, dev, T, Hkv, D)
     qp, qr, qh = _rows(q, "q", dt, dev, T, Hq, D) if Hq else none
     op, orow, oh = _rows(q_out, "q_out", dt, dev, T, Hq, D) if Hq else none
     cp, cr, ch = _rows(k_out, "k_out", dt, dev, T, Hkv, D) if k_out is not None else none
-    P, half = cos.shape if cos is not None else (0, 0)
     _check(lib.snapkv_append_paged(
         _dtype_code(k), qp, kp, vp, _at(cu_seqlens, "cu_seqlens", i32, dev) if cu_seqlens is not None else None,
         _at(starts, "starts", i32, dev), _at(positions, "positions", i32, dev) if positions is not None else None, T, B,
@@ -584,7 +596,7 @@ def snapkv_append_paged(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor,
         _at(cos, "cos", torch.float32, dev) if cos is not None else None, _at(sin, "sin", torch.float32, dev) if cos is not None else None,
         P, 2 * half, 1 if interleaved else 0,
         _at(k_pages, "k_pages", dt, dev), _at(v_pages, "v_pages", dt, dev), _at(block_table, "block_table", i32, dev),
-        columns, num_pages, page_size, op, orow, oh, cp, cr, ch, _stream(stream)))
+        columns, num_pages, page_size, op, orow, oh, cp, cr, ch, _stream_on(dev, stream)))
 
 
 def snapkv_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqlens: torch.Tensor, out: torch.Tensor,
@@ -593,12 +605,12 @@ def snapkv_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, c
     out [T,Hq,D] of q's dtype and, if given, out_lse [Hq,T] float32."""
     lib = load()
     T, Hq, D = q.shape
-    Tk, Hkv, Dk = k.shape
-    if (Tk, Dk) != (T, D) or v.shape != k.shape:
+    Tk, Hkv, Dk = rows = k.shape
+    if Tk != T or Dk != D or v.shape != rows:
         raise ValueError("q, k and v disagree on their shapes")
-    if out.shape != q.shape or (out_lse is not None and out_lse.shape != (Hq, T)):
+    if out.shape != (T, Hq, D) or (out_lse is not None and out_lse.shape != (Hq, T)):
         raise ValueError("out must be [T, Hq, D] and out_lse [Hq, T]")
-    if cu_seqlens.dim() != 1 or cu_seqlens.numel() < 1:
+    if cu_seqlens.ndim != 1 or cu_seqlens.shape[0] < 1:
         raise ValueError("cu_seqlens must be [B + 1]")
     dev, dt = _device_of(q, "q"), q.dtype
     qp, qr, qh = _rows(q, "q", dt, dev, T, Hq, D)
@@ -607,7 +619,7 @@ def snapkv_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, c
     _check(lib.snapkv_prompt_attention(
         _dtype_code(q), qp, kp, vp, _at(cu_seqlens, "cu_seqlens", torch.int32, dev), cu_seqlens.shape[0] - 1, T, Hq, Hkv, D,
         qr, qh, kr, kh, vr, vh, _at(out, "out", dt, dev),
-        _at(out_lse, "out_lse", torch.float32, dev) if out_lse is not None else None, _stream(stream)))
+        _at(out_lse, "out_lse", torch.float32, dev) if out_lse is not None else None, _stream_on(dev, stream)))
 
 
 @functools.lru_cache(maxsize=256)
@@ -624,24 +636,29 @@ def snapkv_decode_attention_paged(q: torch.Tensor, k_pages: torch.Tensor, v_page
     lib = load()
     max_len = int(max_len)
     B, Hq, D = q.shape
-    num_pages, page_size, Hkv, Dk = k_pages.shape
-    if Dk != D or v_pages.shape != k_pages.shape:
+    num_pages, page_size, Hkv, Dk = pool = k_pages.shape
+    if Dk != D or v_pages.shape != pool:
         raise ValueError("q, k_pages and v_pages disagree on their shapes")
-    if block_table.dim() != 2 or block_table.shape[0] != B or lens.shape != (B,):
+    if block_table.ndim != 2 or lens.shape != (B,):
         raise ValueError("block_table must be [B, columns] and lens [B]")
-    if out.shape != q.shape or (out_lse is not None and out_lse.shape != (B, Hq)):
+    Bt, columns = block_table.shape
+    if Bt != B:
+        raise ValueError("block_table must be [B, columns] and lens [B]")
+    if out.shape != (B, Hq, D) or (out_lse is not None and out_lse.shape != (B, Hq)):
         raise ValueError("out must be [B, Hq, D] and out_lse [B, Hq]")
     dev, dt, i32 = _device_of(q, "q"), q.dtype, torch.int32
     ins = (_at(q, "q", dt, dev), _at(k_pages, "k_pages", dt, dev), _at(v_pages, "v_pages", dt, dev),
-           _at(block_table, "block_table", i32, dev), block_table.shape[1], num_pages, page_size, _at(lens, "lens", i32, dev))
+           _at(block_table, "block_table", i32, dev), columns, num_pages, page_size, _at(lens, "lens", i32, dev))
     outs = (_at(out, "out", dt, dev), _at(out_lse, "out_lse", torch.float32, dev) if out_lse is not None else None)
-    st = _stream(stream)
+    st = _stream_on(dev, stream)
     if workspace is None:
         if stream is not None and st != _stream(None):
             raise ValueError("a step on another stream than the current one needs a workspace of the caller's")
         need = snapkv_decode_paged_workspace_bytes(B, Hq, Hkv, D, max_len)
         workspace = torch.empty(need, dtype=torch.uint8, device=q.device) if need else None
-    ws, size = (_at(workspace, "workspace", torch.uint8, dev), workspace.numel()) if workspace is not None else (None, 0)
+        ws, size = (workspace.data_ptr(), need) if need else (None, 0)
+    else:
+        ws, size = _at(workspace, "workspace", torch.uint8, dev), workspace.numel()
     _check(lib.snapkv_decode_attention_paged(_dtype_code(q), *ins, max_len, B, Hq, Hkv, D, *outs, ws, size, st))
 
 
