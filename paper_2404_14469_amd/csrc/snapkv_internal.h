@@ -303,7 +303,7 @@ struct PagedArgs {
     const int32_t *table, *lens;                     // [B, table_stride]; [B]
     int64_t table_stride, pages, max_len;
     int B, Hq, Hkv, g, page;
-    int chunk, nchunk;                               // keys of a workgroup; workgroups of a (sequence, KV head)
+    int nchunk, least;                               // shares that a sequence's keys can have; keys of the shortest
     bool by_xcd;                                     // how workgroups are dealt out
     unsigned page_magic;                             // r / page = r * page_magic >> page_shift, r < 2^31
     int page_shift;
@@ -314,7 +314,7 @@ struct PagedArgs {
     float2* part_ml;                                 // [B, Hq, nchunk]
 };
 struct PagedPlan {
-    int chunk, nchunk;
+    int nchunk, least;
     size_t bytes;                                    // of workspace
 };
 PagedPlan paged_plan(int B, int Hq, int Hkv, int D, int64_t max_len);

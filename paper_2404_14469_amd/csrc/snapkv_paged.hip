@@ -7,10 +7,10 @@
 // caches (snapkv_decode.hip): 16x16x32 products with the g query heads of a KV head as the 16 columns, probabilities in two
 // parts of the storage type, value tiles transposed by a 0/1 product.
 //
-// Work split: a workgroup of four waves takes `chunk` keys of one (sequence, KV head), the same number in every sequence, so
-// a long sequence among short ones is shared out as finely as one by itself; workgroups beyond a sequence's end return
-// at once.  Sequences of one chunk are finished by their workgroup; the partial (max, sum, output) of longer
-// ones are joined by a second kernel.  Rows behind a sequence's end are never read: their lanes read the last row again.
+// Work split: a workgroup of four waves takes a share of the keys of one (sequence, KV head).  The host fixes how many shares a
+// sequence can have, the device how long they are, by the sequence's own length (share_of): a cache may be far longer than what
+// it holds.  Workgroups beyond a sequence's end return at once.  Sequences of one share are finished by their workgroup; the
+// partial (max, sum, output) of longer ones are joined by a second kernel.  Rows behind a sequence's end are never read: their lanes read the last row again.
 // The rows of a step (a table entry, then K and V) are looked up one step ahead.  Eight sequences of about 16000 rows, 32 KV
 // heads: 2.07 GB in 365 us with the join, 5.7 TB/s; one of 131072 rows, 8 KV heads 103 us and 6 for the join; one of 2113 rows 6.0 and 3.8.
 #include "snapkv_attn.h"
@@ -23,6 +23,12 @@ namespace snapkv {
 namespace {
 
 constexpr int kWaves = 4;
+
+// Keys of a share of a sequence of S: whole steps of all waves, so many that nchunk shares hold it, and at least `least`.
+__device__ __forceinline__ int share_of(int S, int nchunk, int least) {
+    const int c = (S + nchunk - 1) / nchunk;
+    return max(least, (c + 127) / 128 * 128);
+}
 
 template <typename T> struct store_type;
 template <> struct store_type<dec_bf16> { typedef __bf16 type; };
@@ -51,9 +57,10 @@ __global__ __launch_bounds__(kWaves * 64) void paged_attn(const PagedArgs A) {
     }
     int64_t len = A.lens[b];
     const int S = (int)(len < 0 ? 0 : (len > A.max_len ? A.max_len : len));
-    const int begin = chunk * A.chunk;
-    if (begin >= S && chunk > 0) return;
-    const int end = begin + A.chunk < S ? begin + A.chunk : S;     // keys begin .. end - 1
+    if (chunk > 0 && chunk * A.least >= S) return;                 // (most of what returns, before the division)
+    const int share = share_of(S, A.nchunk, A.least), begin = chunk * share;
+    if (chunk > 0 && begin >= S) return;
+    const int end = begin + share < S ? begin + share : S;         // keys begin .. end - 1
     const int32_t* table = A.table + (int64_t)b * A.table_stride;
     const int64_t token = (int64_t)A.Hkv * ROW;                    // bytes between the rows of a page
     const char* kbase = A.k + (int64_t)kvh * ROW;
@@ -193,7 +200,7 @@ __global__ __launch_bounds__(kWaves * 64) void paged_attn(const PagedArgs A) {
             for (int d = 0; d < DT; ++d) o[d] += s_acc[w][qi][d0 + d] * f;
         }
         const int64_t hq = (int64_t)b * A.Hq + (int64_t)kvh * A.g + qi;
-        if (S <= A.chunk) {
+        if (S <= share) {
             const float inv = Lq > 0.f ? 1.f / Lq : 0.f;
             elem* out = reinterpret_cast<elem*>(A.out) + hq * D + d0;
 #pragma unroll
@@ -219,8 +226,9 @@ __global__ __launch_bounds__(kWaves * 64) void paged_join(const PagedArgs A) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, b = (int)(hq / A.Hq);
     int64_t len = A.lens[b];
     const int S = (int)(len < 0 ? 0 : (len > A.max_len ? A.max_len : len));
-    if (S <= A.chunk) return;
-    const int n = (S + A.chunk - 1) / A.chunk;
+    const int share = share_of(S, A.nchunk, A.least);
+    if (S <= share) return;
+    const int n = (S + share - 1) / share;
     const float2* ml = A.part_ml + hq * A.nchunk;
     const float* pa = A.part_acc + hq * A.nchunk * D + lane * E;
     float M = -INFINITY;
@@ -264,20 +272,21 @@ __global__ __launch_bounds__(kWaves * 64) void paged_join(const PagedArgs A) {
 
 }  // namespace
 
-// Keys of a workgroup.  With few (sequence, KV head) pairs as few as give 1024 workgroups, four per compute unit, if all
-// sequences are as long as they may be, down to the 128 of one step of each wave; a sequence of up to 512 is not cut, so that short
-// steps are one launch.  At most 1024, and 512 where even those give 2048 workgroups: sequences are of different lengths, which
-// only the device knows, and small shares even that out.  Microseconds with at most 512 / 1024 / 2048 / 4096 keys: 32
-// sequences of 1 to 16384 keys, 8 KV heads 120 / 125 / 149 / 224; eight of about 16000, 32 KV heads 374 / 373 / 378 / 385; one of
-// 131072 keys, 8 KV heads 114 / 107 / 108 / -.
+// Shares of a sequence: as many as give 1024 workgroups, four per compute unit, if all sequences are as long as they may be, of 128
+// keys, one step of each wave, at least; but a sequence of up to 512 is not cut, so that short steps are one launch.  At most 1024
+// keys, and 512 where even those give 2048 workgroups: sequences are of different lengths, which only the device knows, and
+// small shares even that out.  Microseconds with at most 512 / 1024 / 2048 / 4096 keys: 32 sequences of 1 to 16384
+// keys, 8 KV heads 120 / 125 / 149 / 224; eight of about 16000, 32 KV heads 374 / 373 / 378 / 385; one of 131072 keys, 8 KV heads
+// 114 / 107 / 108 / -.  Shares of sequences that are shorter than they may be are as much shorter, down to 128 keys where there
+// are few (sequence, KV head) pairs.
 PagedPlan paged_plan(int B, int Hq, int Hkv, int D, int64_t max_len) {
-    const int64_t keys = (int64_t)B * Hkv * max_len;
+    const int64_t pairs = (int64_t)B * Hkv, keys = pairs * max_len;
     int64_t chunk = std::max<int64_t>(128, (keys / 1024 + 127) / 128 * 128);
     chunk = std::min<int64_t>(chunk, keys >= 2048 * 1024 ? 512 : 1024);
     if (max_len <= 512) chunk = 512;
     PagedPlan P;
-    P.chunk = (int)chunk;
     P.nchunk = (int)((max_len + chunk - 1) / chunk);
+    P.least = P.nchunk == 1 || pairs > 128 ? 512 : (pairs > 64 ? 256 : 128);
     const size_t heads = (size_t)B * Hq;
     P.bytes = P.nchunk <= 1 ? 0 : ((heads * P.nchunk * D * sizeof(float) + 255) & ~(size_t)255) + heads * P.nchunk * sizeof(float2);
     return P;
@@ -285,8 +294,8 @@ PagedPlan paged_plan(int B, int Hq, int Hkv, int D, int64_t max_len) {
 
 hipError_t launch_paged(int dtype, int D, PagedArgs A, void* workspace, hipStream_t st) {
     const PagedPlan P = paged_plan(A.B, A.Hq, A.Hkv, D, A.max_len);
-    A.chunk = P.chunk;
     A.nchunk = P.nchunk;
+    A.least = P.least;
     // r / page for 0 <= r < 2^31: with 2^(l-1) < page <= 2^l, ceil(2^(31+l) / page) fits 32 bits and its product's error stays
     // below one part in r (page 1: 2^31 and a shift by 31)
     int l = 0;

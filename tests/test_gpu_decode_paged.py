@@ -45,6 +45,9 @@ CASES = [   # lens, page, Hq, Hkv, D, dtype, room beyond the longest
     ([64] * 150, 16, 2, 2, 64, "f16", 0),
     ([5000, 1, 777, 0, 4096, 130, 129], 16, 8, 4, 128, "bf16", 0),
     ([1700] * 9 + [40, 3], 8, 3, 3, 64, "bf16", 300),
+    ([2113], 16, 8, 2, 64, "f16", 129000),                    # shares as long as the sequence asks for, not the cache
+    ([5000, 300, 129, 2], 32, 8, 8, 128, "bf16", 60000),
+    ([3000] + [1] * 40, 16, 4, 2, 64, "bf16", 20000),
 ]
 
 
