@@ -2,6 +2,7 @@
 // the launch plan.  Nothing here synchronises the stream.
 #include "../../include/snapkv.h"
 #include "snapkv_internal.h"
+#include "snapkv_serve.h"
 
 #include <algorithm>
 #include <cmath>

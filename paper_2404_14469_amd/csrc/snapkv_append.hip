@@ -10,7 +10,7 @@
 // time.  The two 16-byte pieces of a unit are the two partners of eight pairs (halves) or four pairs each (interleaved).
 // Fewer than 1024 tokens are shared out by head groups instead, so that a step's few tokens meet more waves.  65319 tokens
 // of 32/32 heads, rotated, queries too, keys twice: 3.8 GB in 735 us, 5.1 TB/s; 8 tokens of 32/8 heads 3.7 us.
-#include "snapkv_internal.h"
+#include "snapkv_serve.h"
 
 namespace snapkv {
 namespace {

@@ -14,7 +14,7 @@
 // The rows of a step (a table entry, then K and V) are looked up one step ahead.  Eight sequences of about 16000 rows, 32 KV
 // heads: 2.07 GB in 365 us with the join, 5.7 TB/s; one of 131072 rows, 8 KV heads 103 us and 6 for the join; one of 2113 rows 6.0 and 3.8.
 #include "snapkv_attn.h"
-#include "snapkv_internal.h"
+#include "snapkv_serve.h"
 
 #include <algorithm>
 #include <cmath>

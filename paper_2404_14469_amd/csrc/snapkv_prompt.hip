@@ -27,7 +27,7 @@
 // a step (bf16 2^-8, fp16 2^-11, relative; the fp16 ones are taken 2^7 times as large, so those down to 2^-21 of the
 // largest are normal numbers), which adds to an output about what its own rounding does.  Their sum is taken in fp32 from
 // the unrounded values.
-#include "snapkv_internal.h"
+#include "snapkv_serve.h"
 
 #include <cmath>
 
