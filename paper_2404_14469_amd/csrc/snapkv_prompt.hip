@@ -259,15 +259,18 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 && !SPLIT ? 3 : 2) void prompt
 #pragma unroll
         for (int r = 0; r < 16; ++r) pf[r / 8][r % 8] = (elem)e[r];
     };
-    // The shift need not be the maximum: it is moved to it, sums and outputs rescaled and the block's probabilities taken anew,
-    // only when those of some lane of the wave sum up to more than 2^8 times what the maximum alone would give.  So no
-    // probability is larger than that, and no maximum is looked for as long as none is.
+    // The shift need not be the maximum: a row's is moved to it, its sum and output rescaled and the block's probabilities taken
+    // anew, only when those of one of its two lanes sum up to more than 2^8 times what the maximum alone would give.  So no
+    // probability is larger than that, and no maximum is looked for as long as none is.  The wave's other rows keep their shift,
+    // their factor is 1 and their probabilities come out as before: what a row gives depends on what it sees alone.
     auto settle = [&](const pfx16& x, frag* pf, float* sum) __attribute__((always_inline)) {
-        if (__any(sum[0] + sum[1] > T::kMost)) {
+        const float both = sum[0] + sum[1];
+        if (__any(both > T::kMost)) {
             float big = x[0];
 #pragma unroll
             for (int r = 1; r < 16; ++r) big = fmaxf(big, x[r]);
-            const float mn = fmaxf(m, fmaxf(big, other_half(big)) * A.scale2);
+            const float others = other_half(both), top = fmaxf(big, other_half(big)) * A.scale2;   // (all lanes exchange)
+            const float mn = both > T::kMost || others > T::kMost ? fmaxf(m, top) : m;
             const float alpha = __builtin_amdgcn_exp2f(m - mn);
             m = mn;
             lsum *= alpha;
