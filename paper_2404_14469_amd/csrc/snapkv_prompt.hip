@@ -7,7 +7,7 @@
 // the matrix units the bound of all but the shortest prompts.
 //
 // Work split.  A workgroup of four waves takes 128 query rows of one head, each wave 32 of them, and walks the keys in tiles of 64 that
-// its waves share through LDS; two workgroups share a compute unit (249 registers and 64 KB each), so one's waits are the
+// its waves share through LDS; two workgroups share a compute unit (187 registers and 64 KB each), so one's waits are the
 // other's time.  Calls of few rows give a workgroup 32 rows, and each wave every fourth block of 32 keys (split_keys says which).
 // 32749 tokens of 32/8 heads of 128 take 7.1 ms, 1.24 PFLOP/s, 91 % of a 16384^3 bf16 product's rate, with the card at its power
 // limit.  A batch of 7499 tokens in eight prompts takes 0.13 ms, 4 heads of 2048 tokens 17 us, 78 tokens 7 us, where finding
@@ -385,8 +385,8 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 && !SPLIT ? 3 : 2) void prompt
         v_last = ((mine - 1) & 2 ? s_v1 : s_v0) + ((mine - 1) & 1) * 32 * ROW;   // (one of the last two tiles, which are still there)
     }
     // The wave's last block; its logits are in x.  The last one that rows see they see in part.  Values that a row does not see
-    // have probability 0, but 0 times an infinity or NaN is not 0: where the block holds such a value, its keys are added one by
-    // one (the others' values taken as zeros) and the sums of rows that do not see the key kept.
+    // have probability 0, but 0 times an infinity or NaN is not 0: where the block holds such values, they are taken as zeros, which
+    // leaves all other sums as they would be without them, and then added key by key to the rows that see the key.
     if (SPLIT ? wave < mine : mine > 0) {
         const int b = SPLIT ? wave + (mine - 1 - wave) / STEP * STEP : mine - 1;
         frag pf[2];
@@ -404,16 +404,26 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 && !SPLIT ? 3 : 2) void prompt
 #pragma unroll
             for (int i = 0; i < NV; ++i) acc[i % ND] = mma32(v_frag(v_last, i), pf[i / ND], acc[i % ND]);
         } else {
+            // the values' finite elements, or (of one key of 16) the others; zeros in their place
+            typedef __attribute__((ext_vector_type(8))) unsigned short bits8;
+            auto part = [&](frag vf, int key) __attribute__((always_inline)) {
+                const bits8 y = __builtin_bit_cast(bits8, vf);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const bool odd = (y[e] & T::kExp) == T::kExp;
+                    vf[e] = (key < 0 ? !odd : odd && 8 * (e / 4) + 4 * h2 + e % 4 == key) ? vf[e] : (elem)0.f;
+                }
+                return vf;
+            };
+#pragma unroll
+            for (int i = 0; i < NV; ++i) acc[i % ND] = mma32(part(v_frag(v_last, i), -1), pf[i / ND], acc[i % ND]);
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll 1
                 for (int key = 0; key < 16; ++key)
 #pragma unroll
                     for (int i = 0; i < ND; ++i) {
-                        frag vf = v_frag(v_last, j * ND + i);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) vf[e] = 8 * (e / 4) + 4 * h2 + e % 4 == key ? vf[e] : (elem)0.f;
-                        const pfx16 y = mma32(vf, pf[j], acc[i]);
+                        const pfx16 y = mma32(part(v_frag(v_last, j * ND + i), key), pf[j], acc[i]);
 #pragma unroll
                         for (int r = 0; r < 16; ++r) acc[i][r] = b * 32 + 16 * j + key <= row ? y[r] : acc[i][r];
                     }

@@ -58,3 +58,31 @@ def test_a_query_changes_no_bit_of_another_row(snapkv, Hq, Hkv, dtype, at):
         q2 = q.clone()
         q2[at] *= what
         same(run(snapkv, q2, k, v, cu), want, others)
+
+
+@pytest.mark.parametrize("Hq,Hkv", FORMS)
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("L,at", [(1, 0), (2, 1), (33, 32), (64, 40), (100, 99), (200, 129), (595, 590)])
+def test_a_later_infinity_or_nan_changes_no_bit_of_an_earlier_row(snapkv, Hq, Hkv, dtype, D, L, at):
+    """In a key and in some columns of a value; rows that see them keep the other columns, a later prompt all."""
+    gen = seeded(L + at)
+    q, k, v = (rows(gen, L + 50, h, D, DT[dtype], "tokens") for h in (Hq, Hkv, Hkv))
+    cu = offsets([L, 50])
+    want = run(snapkv, q, k, v, cu)
+    place = torch.arange(L + 50, device="cuda")
+    before = (place < at) | (place >= L)
+    some = torch.rand((Hkv, D), generator=gen, device="cuda") < 0.3
+    some[:, 0] = True
+    g = Hq // Hkv
+    for what in (float("nan"), float("inf"), -float("inf")):
+        k2, v2 = k.clone(), v.clone()
+        k2[at, Hkv - 1] = what
+        v2[at] = v[at].masked_fill(some, what)
+        same(run(snapkv, q, k2, v2, cu), want, before)
+        out, lse = run(snapkv, q, k, v2, cu)
+        assert torch.equal(lse, want[1])
+        same((out, lse), want, before)
+        hit = some.repeat_interleave(g, 0).expand(L - at, Hq, D)
+        assert not torch.isfinite(out[at:L][hit]).any()
+        assert torch.equal(out[at:L][~hit], want[0][at:L][~hit])
