@@ -45,12 +45,14 @@ struct p_bf16 {
     typedef pbf16x8 frag;
     static constexpr float kShift = 0.f, kMost = 256.f;      // exponent that the probabilities are raised by; most that 16 may sum up to
     static constexpr unsigned kExp = 0x7F80;                 // all ones: an infinity or NaN
+    static constexpr float kLargest = INFINITY;              // that a mean can round beyond
 };
 struct p_f16 {
     typedef _Float16 elem;
     typedef pf16x8 frag;
     static constexpr float kShift = 7.f, kMost = 32768.f;    // (below fp16's largest number)
     static constexpr unsigned kExp = 0x7C00;
+    static constexpr float kLargest = 65504.f;
 };
 __device__ __forceinline__ pfx16 mma32(pbf16x8 a, pbf16x8 b, pfx16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ pfx16 mma32(pf16x8 a, pf16x8 b, pfx16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
@@ -137,6 +139,14 @@ __device__ __forceinline__ void fetched() { asm volatile("s_waitcnt vmcnt(%0)" :
 __device__ __forceinline__ float other_half(float x) {
     const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return __uint_as_float((threadIdx.x & 32) ? y[0] : y[1]);
+}
+
+// An output that rounds to no infinity.  Probabilities that were rounded up can carry a mean of numbers near fp16's largest one,
+// 65504, past the 65520 from which on numbers round to infinity; a mean of finite values is at most the largest of them.
+// Infinities stay.  (bf16 has fp32's range, where the sum itself would be infinite.)
+template <typename T> __device__ __forceinline__ float in_range(float y) {
+    if constexpr (T::kLargest == INFINITY) return y;
+    else return __builtin_fabsf(y) < INFINITY ? __builtin_amdgcn_fmed3f(y, -T::kLargest, T::kLargest) : y;
 }
 
 template <typename T, int D, bool SPLIT>
@@ -476,7 +486,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 && !SPLIT ? 3 : 2) void prompt
             }
             elem4 z;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) z[e] = (elem)(y[e] * inv);
+            for (int e = 0; e < 4; ++e) z[e] = (elem)in_range<T>(y[e] * inv);
             *reinterpret_cast<elem4*>(o + 32 * c) = z;
         }
         if (A.lse && tid % 8 == 0)
@@ -491,7 +501,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 && !SPLIT ? 3 : 2) void prompt
             for (int r4 = 0; r4 < 4; ++r4) {
                 elem4 y;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) y[r] = (elem)(acc[i][4 * r4 + r] * inv);
+                for (int r = 0; r < 4; ++r) y[r] = (elem)in_range<T>(acc[i][4 * r4 + r] * inv);
                 *reinterpret_cast<elem4*>(o + 32 * i + 8 * r4) = y;
             }
         if (A.lse && h2 == 0)
