@@ -429,6 +429,7 @@ int snapkv_prompt_attention(int dtype, const void* q, const void* k, const void*
  *           rows below lens (the others are not read)
  *   block_table [B, table_columns] device int32; entries outside [0, num_pages) are clamped to that range
  *   lens    [B] device int32 rows per sequence, clamped to [0, max_len]; a sequence with no rows gets out = 0 and out_lse = -inf
+ *           (NaN in a head's query: NaN in its out and out_lse)
  *   max_len 1 <= max_len <= table_columns * page_size, at most 2^30: no sequence is longer (it bounds the shares that keys are split into)
  *   Hq % Hkv == 0, Hq / Hkv <= 16, D in {64, 128}
  *   out     [B, Hq, D] device, dtype (rounded once from float32);  out_lse [B, Hq] device float32 or NULL

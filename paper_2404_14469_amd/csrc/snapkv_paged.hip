@@ -201,12 +201,12 @@ __global__ __launch_bounds__(kWaves * 64) void paged_attn(const PagedArgs A) {
         }
         const int64_t hq = (int64_t)b * A.Hq + (int64_t)kvh * A.g + qi;
         if (S <= share) {
-            const float inv = Lq > 0.f ? 1.f / Lq : 0.f;
+            const float inv = Lq == 0.f ? 0.f : 1.f / Lq;      // (no rows; a sum that is NaN makes the row's answer NaN)
             elem* out = reinterpret_cast<elem*>(A.out) + hq * D + d0;
 #pragma unroll
             for (int d = 0; d < DT; ++d) out[d] = (elem)(o[d] * inv);
             if (A.lse && (tid & 15) == 0)
-                A.lse[hq] = Lq > 0.f ? (M + __builtin_amdgcn_logf(Lq)) * 0.6931471805599453f : -INFINITY;
+                A.lse[hq] = Lq == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(Lq)) * 0.6931471805599453f;
         } else {
             float* pa = A.part_acc + (hq * A.nchunk + chunk) * D;
 #pragma unroll
@@ -265,9 +265,9 @@ __global__ __launch_bounds__(kWaves * 64) void paged_join(const PagedArgs A) {
     if (threadIdx.x < D) {
         const int d = threadIdx.x;
         const float y = s_o[0][d] + s_o[1][d] + s_o[2][d] + s_o[3][d];
-        reinterpret_cast<elem*>(A.out)[hq * D + d] = (elem)(Lq > 0.f ? y / Lq : 0.f);
+        reinterpret_cast<elem*>(A.out)[hq * D + d] = (elem)(Lq == 0.f ? 0.f : y / Lq);
     }
-    if (A.lse && threadIdx.x == 0) A.lse[hq] = Lq > 0.f ? (M + __builtin_amdgcn_logf(Lq)) * 0.6931471805599453f : -INFINITY;
+    if (A.lse && threadIdx.x == 0) A.lse[hq] = Lq == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(Lq)) * 0.6931471805599453f;
 }
 
 }  // namespace
