@@ -31,8 +31,17 @@ __device__ __forceinline__ int share_of(int S, int nchunk, int least) {
 }
 
 template <typename T> struct store_type;
-template <> struct store_type<dec_bf16> { typedef __bf16 type; };
-template <> struct store_type<dec_f16> { typedef _Float16 type; };
+template <> struct store_type<dec_bf16> {
+    typedef __bf16 type;
+    static constexpr float kShift = 0.f;
+};
+// fp16 probabilities are taken 2^15 times as large (the largest, 2^15, is below fp16's largest number).  Two parts of one then lose
+// less than 2^-20 of it, or a step of fp16's smallest numbers, 2^-39 of the row's largest; taken as they are, those of about
+// 2^-17, of which a long cache can have as many as weigh all, would lose up to 2^-7 of themselves.
+template <> struct store_type<dec_f16> {
+    typedef _Float16 type;
+    static constexpr float kShift = 15.f;
+};
 
 template <typename T, int D>
 __global__ __launch_bounds__(kWaves * 64) void paged_attn(const PagedArgs A) {
@@ -40,6 +49,7 @@ __global__ __launch_bounds__(kWaves * 64) void paged_attn(const PagedArgs A) {
     constexpr int NP = D / 32;        // 16-byte pieces per lane and row
     constexpr int NB = D / 16;        // 16-column blocks of the output
     constexpr int ROW = D * 2;
+    constexpr float kShift = store_type<T>::kShift;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int n16 = lane & 15, kg = lane >> 4;
     // A share's heads run together.  With several sequences they run on one XCD too (workgroup i runs on XCD i % 8), which then
@@ -125,10 +135,11 @@ __global__ __launch_bounds__(kWaves * 64) void paged_attn(const PagedArgs A) {
         const float mn = fmaxf(m, tmax);
         const float alpha = __builtin_amdgcn_exp2f(m - mn);
         m = mn;
+        const float least = mn - kShift;
         float psum = 0.f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            e[j] = __builtin_amdgcn_exp2f(e[j] - mn);
+            e[j] = __builtin_amdgcn_exp2f(e[j] - least);
             psum += e[j];
         }
         lsum = lsum * alpha + psum;
@@ -206,7 +217,7 @@ __global__ __launch_bounds__(kWaves * 64) void paged_attn(const PagedArgs A) {
 #pragma unroll
             for (int d = 0; d < DT; ++d) out[d] = (elem)(o[d] * inv);
             if (A.lse && (tid & 15) == 0)
-                A.lse[hq] = Lq == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(Lq)) * 0.6931471805599453f;
+                A.lse[hq] = Lq == 0.f ? -INFINITY : (M - kShift + __builtin_amdgcn_logf(Lq)) * 0.6931471805599453f;
         } else {
             float* pa = A.part_acc + (hq * A.nchunk + chunk) * D;
 #pragma unroll
@@ -222,6 +233,7 @@ template <typename T, int D>
 __global__ __launch_bounds__(kWaves * 64) void paged_join(const PagedArgs A) {
     typedef typename store_type<T>::type elem;
     constexpr int E = D / 64, BATCH = 8;
+    constexpr float kShift = store_type<T>::kShift;
     const int64_t hq = blockIdx.x;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, b = (int)(hq / A.Hq);
     int64_t len = A.lens[b];
@@ -267,7 +279,7 @@ __global__ __launch_bounds__(kWaves * 64) void paged_join(const PagedArgs A) {
         const float y = s_o[0][d] + s_o[1][d] + s_o[2][d] + s_o[3][d];
         reinterpret_cast<elem*>(A.out)[hq * D + d] = (elem)(Lq == 0.f ? 0.f : y / Lq);
     }
-    if (A.lse && threadIdx.x == 0) A.lse[hq] = Lq == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(Lq)) * 0.6931471805599453f;
+    if (A.lse && threadIdx.x == 0) A.lse[hq] = Lq == 0.f ? -INFINITY : (M - kShift + __builtin_amdgcn_logf(Lq)) * 0.6931471805599453f;
 }
 
 }  // namespace
