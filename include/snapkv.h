@@ -431,11 +431,12 @@ int snapkv_prompt_attention(int dtype, const void* q, const void* k, const void*
  *   lens    [B] device int32 rows per sequence, clamped to [0, max_len]; a sequence with no rows gets out = 0 and out_lse = -inf
  *           (NaN in a head's query: NaN in its out and out_lse)
  *   max_len 1 <= max_len <= table_columns * page_size, at most 2^30: no sequence is longer (it bounds the shares that keys are split into)
- *   Hq % Hkv == 0, Hq / Hkv <= 16, D in {64, 128}
+ *   Hq % Hkv == 0, Hq / Hkv <= 16, D in {64, 128}; B and Hkv < 2^16, B * Hkv < 2^21, B * Hq < 2^24, B * Hkv * max_len <= 2^36
  *   out     [B, Hq, D] device, dtype (rounded once from float32);  out_lse [B, Hq] device float32 or NULL
  *   workspace device memory, 256-byte aligned, of at least snapkv_decode_paged_workspace_bytes(B, Hq, Hkv, D, max_len) bytes
  *           (0 for steps that are not split: then it may be NULL; also 0 for shapes that the step refuses), owned by the caller
- *           and free to reuse once the enqueued work has finished; its contents do not matter
+ *           and free to reuse once the enqueued work has finished; its contents do not matter (at most
+ *           4 D + 8 bytes for each of 7 shares of a query head, or of 16384 Hq / Hkv shares in all where those are more)
  *
  * Steps with distinct workspaces are independent, and a step may be captured.  Returns SNAPKV_OK or a negative
  * SNAPKV_ERR_* code.

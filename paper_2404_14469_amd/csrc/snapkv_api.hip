@@ -126,6 +126,17 @@ int check_rows(const void* p, int64_t row_stride, int64_t head_stride, int D, in
     return SNAPKV_OK;
 }
 
+// The shapes that a step over pages takes, for the step and for the size of its workspace.
+int check_paged_shape(int B, int Hq, int Hkv, int D, int64_t max_len) {
+    if (B < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || max_len < 1) return SNAPKV_ERR_INVALID_ARG;
+    if ((D != 64 && D != 128) || Hq / Hkv > 16 || Hkv > 65535 || B > 65535 || max_len > (int64_t)1 << 30) return SNAPKV_ERR_UNSUPPORTED;
+    // (a launch has 2^32 threads: fewer than 2^24 workgroups, up to seven for a sequence and KV head.  2^36 rows are 16 TB of keys and
+    // values and more)
+    const int64_t pairs = (int64_t)B * Hkv;
+    if (pairs >= (int64_t)1 << 21 || (int64_t)B * Hq >= (int64_t)1 << 24 || pairs * max_len > (int64_t)1 << 36) return SNAPKV_ERR_UNSUPPORTED;
+    return SNAPKV_OK;
+}
+
 // Shape checks shared by every entry point that scores (steps 1-3).
 int check_score_args(const void* q_win, const void* k, int64_t L, int Hq, int Hkv, int D, int W,
                      int pool_kind, int p) {
@@ -1356,8 +1367,7 @@ int snapkv_prompt_attention(int dtype, const void* q, const void* k, const void*
 }
 
 size_t snapkv_decode_paged_workspace_bytes(int B, int Hq, int Hkv, int D, int64_t max_len) {
-    if (B < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || max_len < 1 || max_len > (int64_t)1 << 30) return 0;
-    if (D != 64 && D != 128) return 0;
+    if (check_paged_shape(B, Hq, Hkv, D, max_len) != SNAPKV_OK) return 0;
     return paged_plan(B, Hq, Hkv, D, max_len).bytes;
 }
 
@@ -1367,19 +1377,15 @@ int snapkv_decode_attention_paged(int dtype, const void* q, const void* k_pages,
                                   float* out_lse, void* workspace, size_t workspace_bytes, void* stream) {
     if (!valid_dtype(dtype)) return SNAPKV_ERR_INVALID_ARG;
     if (!q || !k_pages || !v_pages || !block_table || !lens || !out) return SNAPKV_ERR_INVALID_ARG;
-    if (B < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || num_pages < 1 || page_size < 1 || table_columns < 1 || max_len < 1)
-        return SNAPKV_ERR_INVALID_ARG;
-    if (dtype == SNAPKV_DTYPE_F32 || (D != 64 && D != 128)) return SNAPKV_ERR_UNSUPPORTED;
-    if (Hq / Hkv > 16 || Hkv > 65535 || B > 65535 || max_len > (int64_t)1 << 30 || num_pages > ((int64_t)1 << 31) ||
-        table_columns > ((int64_t)1 << 31))
-        return SNAPKV_ERR_UNSUPPORTED;
+    if (num_pages < 1 || page_size < 1 || table_columns < 1) return SNAPKV_ERR_INVALID_ARG;
+    const int shape = check_paged_shape(B, Hq, Hkv, D, max_len);
+    if (shape != SNAPKV_OK) return shape;
+    if (dtype == SNAPKV_DTYPE_F32 || num_pages > ((int64_t)1 << 31) || table_columns > ((int64_t)1 << 31)) return SNAPKV_ERR_UNSUPPORTED;
     if (max_len > table_columns * page_size) return SNAPKV_ERR_INVALID_ARG;
-    const PagedPlan plan = paged_plan(B, Hq, Hkv, D, max_len);
-    if (((int64_t)plan.nchunk + 7) * B * Hkv >= (int64_t)1 << 24 || (int64_t)B * Hq >= (int64_t)1 << 24) return SNAPKV_ERR_UNSUPPORTED;   // (2^32 threads)
     if (!aligned16(q) || !aligned16(k_pages) || !aligned16(v_pages) || !aligned16(out)) return SNAPKV_ERR_MISALIGNED;
     for (const void* x : {(const void*)out_lse, (const void*)lens, (const void*)block_table})
         if ((reinterpret_cast<uintptr_t>(x) & 3u) != 0) return SNAPKV_ERR_MISALIGNED;
-    const size_t need = plan.bytes;
+    const size_t need = paged_plan(B, Hq, Hkv, D, max_len).bytes;
     if (need > 0 && (!workspace || workspace_bytes < need)) return SNAPKV_ERR_WORKSPACE;
     if (need > 0 && (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return SNAPKV_ERR_MISALIGNED;
     PagedArgs A{};

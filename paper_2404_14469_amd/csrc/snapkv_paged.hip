@@ -23,6 +23,7 @@ namespace snapkv {
 namespace {
 
 constexpr int kWaves = 4;
+constexpr int64_t kMostGroups = 16384;   // workgroups of a step whose sequences' shares are bounded by it
 
 // Keys of a share of a sequence of S: whole steps of all waves, so many that nchunk shares hold it, and at least `least`.
 __device__ __forceinline__ int share_of(int S, int nchunk, int least) {
@@ -53,18 +54,16 @@ __global__ __launch_bounds__(kWaves * 64) void paged_attn(const PagedArgs A) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int n16 = lane & 15, kg = lane >> 4;
     // A share's heads run together.  With several sequences they run on one XCD too (workgroup i runs on XCD i % 8), which then
-    // reads whole rows; share c of sequence s goes to XCD (c + s) % 8, so that the short ones' few do not all meet on the first.
-    int kvh = blockIdx.x % A.Hkv, chunk = blockIdx.x / A.Hkv, b = 0;
+    // reads whole rows; a sequence has an odd number of places (`places`, at most one of them empty), so that the first shares, which
+    // are all that short sequences have, do not meet on a few XCDs.
+    int kvh = blockIdx.x % A.Hkv, chunk = blockIdx.x / A.Hkv;
     if (A.by_xcd) {
-        const int pad = (A.nchunk + 7) / 8 * 8, unit = blockIdx.x / (8 * A.Hkv) * 8 + blockIdx.x % 8;
         kvh = blockIdx.x / 8 % A.Hkv;
-        b = unit / pad;
-        chunk = (unit + b * (pad - 1)) % pad;                  // (unit % pad - b, modulo pad)
-        if (chunk >= A.nchunk) return;
-    } else {
-        b = chunk / A.nchunk;
-        chunk %= A.nchunk;
+        chunk = blockIdx.x / (8 * A.Hkv) * 8 + blockIdx.x % 8;
     }
+    const int b = chunk / A.places;
+    chunk %= A.places;
+    if (chunk >= A.nchunk || b >= A.B) return;
     int64_t len = A.lens[b];
     const int S = (int)(len < 0 ? 0 : (len > A.max_len ? A.max_len : len));
     if (chunk > 0 && chunk * A.least >= S) return;                 // (most of what returns, before the division)
@@ -291,13 +290,15 @@ __global__ __launch_bounds__(kWaves * 64) void paged_join(const PagedArgs A) {
 // keys, 8 KV heads 120 / 125 / 149 / 224; eight of about 16000, 32 KV heads 374 / 373 / 378 / 385; one of 131072 keys, 8 KV heads
 // 114 / 107 / 108 / -.  Shares of sequences that are shorter than they may be are as much shorter, down to 128 keys where there
 // are few (sequence, KV head) pairs.
+// Workgroups and workspace go by how long sequences may be, so no more shares than give 16384 workgroups, or seven, whatever that
+// is; sequences that are long then have longer ones.
 PagedPlan paged_plan(int B, int Hq, int Hkv, int D, int64_t max_len) {
     const int64_t pairs = (int64_t)B * Hkv, keys = pairs * max_len;
     int64_t chunk = std::max<int64_t>(128, (keys / 1024 + 127) / 128 * 128);
     chunk = std::min<int64_t>(chunk, keys >= 2048 * 1024 ? 512 : 1024);
     if (max_len <= 512) chunk = 512;
     PagedPlan P;
-    P.nchunk = (int)((max_len + chunk - 1) / chunk);
+    P.nchunk = (int)std::min((max_len + chunk - 1) / chunk, std::max<int64_t>(7, kMostGroups / pairs));
     P.least = P.nchunk == 1 || pairs > 128 ? 512 : (pairs > 64 ? 256 : 128);
     const size_t heads = (size_t)B * Hq;
     P.bytes = P.nchunk <= 1 ? 0 : ((heads * P.nchunk * D * sizeof(float) + 255) & ~(size_t)255) + heads * P.nchunk * sizeof(float2);
@@ -322,11 +323,12 @@ hipError_t launch_paged(int dtype, int D, PagedArgs A, void* workspace, hipStrea
         A.part_acc = static_cast<float*>(workspace);
         A.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + ((heads * P.nchunk * D * sizeof(float) + 255) & ~(size_t)255));
     }
-    int64_t units = (int64_t)P.nchunk * A.B;
     // (8 x 16000 rows, 32 KV heads 366 us so, 378 with heads dealt to XCDs; 32 sequences of 1 to 16384 rows 119 / 121; one of 131072
     // rows 112 / 109)
-    A.by_xcd = A.B > 1 && units >= 64;
-    if (A.by_xcd) units = (int64_t)((P.nchunk + 7) / 8 * 8) * A.B;
+    A.by_xcd = A.B > 1 && (int64_t)P.nchunk * A.B >= 64;
+    A.places = A.by_xcd ? P.nchunk | 1 : P.nchunk;
+    int64_t units = (int64_t)A.places * A.B;
+    if (A.by_xcd) units = (units + 7) / 8 * 8;
     auto launch = [&](auto step, auto join) {
         hipLaunchKernelGGL(step, dim3((unsigned)(units * A.Hkv)), dim3(kWaves * 64), 0, st, A);
         if (P.nchunk > 1) hipLaunchKernelGGL(join, dim3((unsigned)heads), dim3(kWaves * 64), 0, st, A);

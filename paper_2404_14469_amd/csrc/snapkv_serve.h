@@ -45,6 +45,7 @@ struct PagedArgs {
     int64_t table_stride, pages, max_len;
     int B, Hq, Hkv, g, page;
     int nchunk, least;                               // shares that a sequence's keys can have; keys of the shortest
+    int places;                                      // of workgroups, per sequence and KV head
     bool by_xcd;                                     // how workgroups are dealt out
     unsigned page_magic;                             // r / page = r * page_magic >> page_shift, r < 2^31
     int page_shift;
