@@ -379,7 +379,7 @@ int snapkv_decode_attention(int dtype, const void* q, const void* k_cache, const
  *   rot_dim 0, or a multiple of 16 (float32: 8) up to D
  *   k_pages, v_pages [num_pages, page_size, Hkv, D] device;  block_table [B, table_columns] device int32
  *   q_out   [T, Hq, D] device, the rotated queries (NULL with Hq = 0);  k_out [T, Hkv, D] device or NULL: the rotated keys
- *           once more, for the attention over the prompt; strides as for the inputs, no two rows may overlap
+ *           once more, for the attention over the prompt; strides as for the inputs, rows that overlap are refused
  *
  * T < 2^26.  Rows that the table has no column for (or before the first) and table entries outside [0, num_pages) are not
  * written to pages.  Distinct tokens must not meet in one row of one page.  T = 0 or B = 0 does nothing.  No scratch; calls are independent and

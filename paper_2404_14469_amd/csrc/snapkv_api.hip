@@ -126,6 +126,20 @@ int check_rows(const void* p, int64_t row_stride, int64_t head_stride, int D, in
     return SNAPKV_OK;
 }
 
+// Whether any two of T x H such rows, which are written, share an element.  Mostly one dimension lies within a step of the other;
+// where neither does, heads h apart meet tokens t apart if t row strides come within a row of h head strides.
+bool rows_overlap(int64_t row_stride, int64_t head_stride, int64_t T, int H, int D) {
+    if (T > 1 && row_stride < D) return true;
+    if (H <= 1) return false;
+    if (head_stride < D) return true;
+    if (T <= 1 || row_stride >= (H - 1) * head_stride + D || (head_stride - D) / row_stride >= T - 1) return false;
+    for (int64_t h = 1; h < H; ++h) {
+        const int64_t t = h * head_stride / row_stride, behind = h * head_stride - t * row_stride;
+        if ((t < T && behind < D) || (t + 1 < T && row_stride - behind < D)) return true;
+    }
+    return false;
+}
+
 // The shapes that a step over pages takes, for the step and for the size of its workspace.
 int check_paged_shape(int B, int Hq, int Hkv, int D, int64_t max_len) {
     if (B < 1 || Hq < 1 || Hkv < 1 || Hq % Hkv != 0 || max_len < 1) return SNAPKV_ERR_INVALID_ARG;
@@ -1285,6 +1299,9 @@ int snapkv_append_paged(int dtype, const void* q, const void* k, const void* v, 
         const int rc = check_rows(x.p, x.rows, x.heads, D, e);
         if (rc != SNAPKV_OK) return rc;
     }
+    if ((q_out && rows_overlap(q_out_row_stride, q_out_head_stride, T, Hq, D)) ||
+        (k_out && rows_overlap(k_out_row_stride, k_out_head_stride, T, Hkv, D)))
+        return SNAPKV_ERR_INVALID_ARG;
     if (!aligned16(k_pages) || !aligned16(v_pages) || !aligned16(cos) || !aligned16(sin)) return SNAPKV_ERR_MISALIGNED;
     for (const int32_t* x : {cu_seqlens, starts, positions, block_table})
         if ((reinterpret_cast<uintptr_t>(x) & 3u) != 0) return SNAPKV_ERR_MISALIGNED;
