@@ -9,8 +9,8 @@
 // Work split.  A workgroup of four waves takes 128 query rows of one head, each wave 32 of them, and walks the keys in tiles of 64 that
 // its waves share through LDS; two workgroups share a compute unit (187 registers and 64 KB each), so one's waits are the
 // other's time.  Calls of few rows give a workgroup 32 rows, and each wave every fourth block of 32 keys (split_keys says which).
-// 32749 tokens of 32/8 heads of 128 take 7.1 ms, 1.24 PFLOP/s, 91 % of a 16384^3 bf16 product's rate, with the card at its power
-// limit.  A batch of 7499 tokens in eight prompts takes 0.13 ms, 4 heads of 2048 tokens 17 us, 78 tokens 7 us, where finding
+// 32749 tokens of 32/8 heads of 128 take 7.1 to 7.4 ms, 1.19 to 1.24 PFLOP/s, 88 to 91 % of a 16384^3 bf16 product's rate, with the
+// card at its power limit.  A batch of 7499 tokens in eight prompts takes 0.13 ms, 4 heads of 2048 tokens 17 us, 78 tokens 7 us, where finding
 // the tile, fetching and storing are most of the time.
 //
 // MFMA layout (32x32x16, 64 lanes): lane l supplies row (left operand) or column (right operand) l%32 and contraction
