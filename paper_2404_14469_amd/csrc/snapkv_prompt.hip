@@ -416,7 +416,7 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 && !SPLIT ? 3 : 2) void prompt
         } else {
             // the values' finite elements, or (of one key of 16) the others; zeros in their place
             typedef __attribute__((ext_vector_type(8))) unsigned short bits8;
-            auto part = [&](frag vf, int key) __attribute__((always_inline)) {
+            auto elements = [&](frag vf, int key) __attribute__((always_inline)) {
                 const bits8 y = __builtin_bit_cast(bits8, vf);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
@@ -426,14 +426,14 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 && !SPLIT ? 3 : 2) void prompt
                 return vf;
             };
 #pragma unroll
-            for (int i = 0; i < NV; ++i) acc[i % ND] = mma32(part(v_frag(v_last, i), -1), pf[i / ND], acc[i % ND]);
+            for (int i = 0; i < NV; ++i) acc[i % ND] = mma32(elements(v_frag(v_last, i), -1), pf[i / ND], acc[i % ND]);
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll 1
                 for (int key = 0; key < 16; ++key)
 #pragma unroll
                     for (int i = 0; i < ND; ++i) {
-                        const pfx16 y = mma32(part(v_frag(v_last, j * ND + i), key), pf[j], acc[i]);
+                        const pfx16 y = mma32(elements(v_frag(v_last, j * ND + i), key), pf[j], acc[i]);
 #pragma unroll
                         for (int r = 0; r < 16; ++r) acc[i][r] = b * 32 + 16 * j + key <= row ? y[r] : acc[i][r];
                     }
