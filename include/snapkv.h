@@ -411,7 +411,8 @@ int snapkv_append_paged(int dtype, const void* q, const void* k, const void* v, 
  *   out     [T, Hq, D] device, dtype, contiguous;  out_lse [Hq, T] device float32 or NULL.  Rows that belong to no prompt
  *           are left as they were
  *
- * The probabilities are rounded to dtype before the product with v; sums and statistics are float32.  T = 0 or B = 0
+ * The probabilities are rounded to dtype before the product with v; sums and statistics are float32 (and can overflow where
+ * bfloat16 values exceed 2^78).  T = 0 or B = 0
  * does nothing; T < 2^30, (T / 128 + B) Hq < 2^24.  No scratch; calls are independent, repeat bit for bit and may be captured.  Returns SNAPKV_OK or a negative SNAPKV_ERR_*
  * code.
  */

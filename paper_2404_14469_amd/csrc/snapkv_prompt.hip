@@ -9,8 +9,8 @@
 // Work split.  A workgroup of four waves takes 128 query rows of one head, each wave 32 of them, and walks the keys in tiles of 64 that
 // its waves share through LDS; two workgroups share a compute unit (187 registers and 64 KB each), so one's waits are the
 // other's time.  Calls of few rows give a workgroup 32 rows, and each wave every fourth block of 32 keys (split_keys says which).
-// 32749 tokens of 32/8 heads of 128 take 7.1 to 7.4 ms, 1.19 to 1.24 PFLOP/s, 88 to 91 % of a 16384^3 bf16 product's rate, with the
-// card at its power limit.  A batch of 7499 tokens in eight prompts takes 0.13 ms, 4 heads of 2048 tokens 17 us, 78 tokens 7 us, where finding
+// 32749 tokens of 32/8 heads of 128 take 7.1 to 7.6 ms by card, 1.15 to 1.24 PFLOP/s, with the card at its power limit; 88 to 91 % of
+// a 16384^3 bf16 product's rate where both were timed.  A batch of 7499 tokens in eight prompts takes 0.13 ms, 4 heads of 2048 tokens 17 us, 78 tokens 7 us, where finding
 // the tile, fetching and storing are most of the time.
 //
 // MFMA layout (32x32x16, 64 lanes): lane l supplies row (left operand) or column (right operand) l%32 and contraction
@@ -43,14 +43,16 @@ typedef __attribute__((ext_vector_type(4))) unsigned pu32x4;
 struct p_bf16 {
     typedef __bf16 elem;
     typedef pbf16x8 frag;
-    static constexpr float kShift = 0.f, kMost = 256.f;      // exponent that the probabilities are raised by; most that 16 may sum up to
+    // exponent that the probabilities are raised by; most that 16 may sum up to (2^20 times what the maximum alone gives: bf16 has the
+    // range; 16384 tokens with queries three times as long 1.98 ms, with 2^8 2.05)
+    static constexpr float kShift = 0.f, kMost = 1048576.f;
     static constexpr unsigned kExp = 0x7F80;                 // all ones: an infinity or NaN
     static constexpr float kLargest = INFINITY;              // that a mean can round beyond
 };
 struct p_f16 {
     typedef _Float16 elem;
     typedef pf16x8 frag;
-    static constexpr float kShift = 7.f, kMost = 32768.f;    // (below fp16's largest number)
+    static constexpr float kShift = 7.f, kMost = 32768.f;    // (2^8 times; below fp16's largest number)
     static constexpr unsigned kExp = 0x7C00;
     static constexpr float kLargest = 65504.f;
 };
@@ -270,9 +272,9 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 && !SPLIT ? 3 : 2) void prompt
         for (int r = 0; r < 16; ++r) pf[r / 8][r % 8] = (elem)e[r];
     };
     // The shift need not be the maximum: a row's is moved to it, its sum and output rescaled and the block's probabilities taken
-    // anew, only when those of one of its two lanes sum up to more than 2^8 times what the maximum alone would give.  So no
-    // probability is larger than that, and no maximum is looked for as long as none is.  The wave's other rows keep their shift,
-    // their factor is 1 and their probabilities come out as before: what a row gives depends on what it sees alone.
+    // anew, only when those of one of its two lanes sum up to more than kMost.  So no probability is larger than that, and no maximum
+    // is looked for as long as none is.  The wave's other rows keep their shift, their factor is 1 and their probabilities come out
+    // as before: what a row gives depends on what it sees alone.
     auto settle = [&](const pfx16& x, frag* pf, float* sum) __attribute__((always_inline)) {
         const float both = sum[0] + sum[1];
         if (__any(both > T::kMost)) {
