@@ -47,6 +47,10 @@ extern "C" {
 #define SNAPKV_DTYPE_F32 1  /* IEEE float32 q/k/v */
 #define SNAPKV_DTYPE_F16 2  /* IEEE float16 q/k/v */
 
+#define SNAPKV_CACHE_PLAIN 0 /* pages hold rows of the call's dtype */
+#define SNAPKV_CACHE_FP8 1   /* pages hold microscaled rows of e4m3 codes (8 bits) */
+#define SNAPKV_CACHE_FP4 2   /* pages hold microscaled rows of e2m1 codes (4 bits) */
+
 #define SNAPKV_OK 0
 #define SNAPKV_ERR_INVALID_ARG (-1) /* null pointer, L<1, W<1, W>L, W>C, even p, bad pool_kind, Hq%Hkv!=0 */
 #define SNAPKV_ERR_UNSUPPORTED (-2) /* D not in {64,128}, p>129, L-W>2^24, a window length the kernels do not take */
@@ -447,6 +451,80 @@ int snapkv_decode_attention_paged(int dtype, const void* q, const void* k_pages,
                                   const int32_t* lens, int64_t max_len, int B, int Hq, int Hkv, int D, void* out,
                                   float* out_lse, void* workspace, size_t workspace_bytes, void* stream);
 size_t snapkv_decode_paged_workspace_bytes(int B, int Hq, int Hkv, int D, int64_t max_len);
+
+/*
+ * Microscaled pages: the same caches in 8 or 4 bits.  A row of D values lies in blocks of 32; with A a block's largest magnitude and
+ * M the largest value of the element type (SNAPKV_CACHE_FP8: e4m3, 448; SNAPKV_CACHE_FP4: e2m1, 6), e is the smallest integer with
+ * A <= M 2^e, at least -117; scale byte e + 127; an element's code is the element type's value nearest to x 2^-e, ties to the
+ * even code.  A block that holds an infinity or NaN has scale byte 255 and codes of zero and reads as NaN.
+ *   codes   [num_pages, page_size, Hkv, D] bytes (FP8), or [.., D / 2] with the even element in a byte's low half (FP4)
+ *   scales  [num_pages, page_size, Hkv, D / 32] bytes
+ *
+ * snapkv_append_paged_mx is snapkv_append_paged into such pages: arguments as there, k_pages and v_pages the codes, k_scales and
+ * v_scales the scales (all four 16-byte aligned).  Codes are those of the rotated row before any rounding (what lies beyond
+ * float32's range counts as its largest number); q_out and k_out are rotated in float32 and rounded once, to dtype.
+ */
+int snapkv_append_paged_mx(int dtype, int cache, const void* q, const void* k, const void* v, const int32_t* cu_seqlens,
+                           const int32_t* starts, const int32_t* positions, int64_t T, int B, int Hq, int Hkv, int D,
+                           int64_t q_row_stride, int64_t q_head_stride, int64_t k_row_stride, int64_t k_head_stride,
+                           int64_t v_row_stride, int64_t v_head_stride, const float* cos, const float* sin,
+                           int64_t n_positions, int rot_dim, int interleaved, void* k_pages, void* k_scales, void* v_pages,
+                           void* v_scales, const int32_t* block_table, int64_t table_columns, int64_t num_pages,
+                           int page_size, void* q_out, int64_t q_out_row_stride, int64_t q_out_head_stride, void* k_out,
+                           int64_t k_out_row_stride, int64_t k_out_head_stride, void* stream);
+
+/*
+ * Rows of microscaled pages as values of dtype (rounded once; exact in bfloat16, where subnormal and beyond-range values of pages
+ * that others wrote may differ, and in float32): what the compression of a prompt and the attention over one take.
+ * The T rows of B sequences go packed to k_out and v_out [T, Hkv, D] (strides as for the outputs of snapkv_append_paged, rows that
+ * overlap are refused): token t of sequence b is its logical row starts[b] + t - cu_seqlens[b] (cu_seqlens NULL: one row
+ * per sequence, T == B).  Tokens of no sequence, rows that the table has no column for (or before the first) and table entries outside
+ * [0, num_pages) leave their output rows as they were.  Limits as for snapkv_append_paged.  No scratch; calls are
+ * independent and may be captured.
+ */
+int snapkv_read_paged_mx(int dtype, int cache, const void* k_pages, const void* k_scales, const void* v_pages,
+                         const void* v_scales, const int32_t* block_table, int64_t table_columns, int64_t num_pages,
+                         int page_size, const int32_t* cu_seqlens, const int32_t* starts, int64_t T, int B, int Hkv, int D,
+                         void* k_out, int64_t k_out_row_stride, int64_t k_out_head_stride, void* v_out,
+                         int64_t v_out_row_stride, int64_t v_out_head_stride, void* stream);
+
+/*
+ * snapkv_decode_attention_paged over microscaled pages (cache SNAPKV_CACHE_FP8 or SNAPKV_CACHE_FP4; all four parts of the pages 16-byte aligned):
+ * arguments, limits and errors as there; dtype is that of q and out.  Rows below lens that read as NaN give NaN.  The workspace is of at
+ * least snapkv_decode_paged_mx_workspace_bytes(B, Hq, Hkv, D, max_len) bytes.
+ */
+int snapkv_decode_attention_paged_mx(int dtype, int cache, const void* q, const void* k_pages, const void* k_scales,
+                                     const void* v_pages, const void* v_scales, const int32_t* block_table,
+                                     int64_t table_columns, int64_t num_pages, int page_size, const int32_t* lens,
+                                     int64_t max_len, int B, int Hq, int Hkv, int D, void* out, float* out_lse,
+                                     void* workspace, size_t workspace_bytes, void* stream);
+size_t snapkv_decode_paged_mx_workspace_bytes(int B, int Hq, int Hkv, int D, int64_t max_len);
+
+/*
+ * The same step for batches whose sequences share prefixes: group i is the sequences cu_groups[i] .. cu_groups[i + 1] - 1, and
+ * each of them sees the prefix_lens[i] rows that prefix_table's row i names, then its own lens[b] rows of block_table.  A
+ * prefix's rows are read once for all query heads of its group that read them (up to 64 at a time), not once per sequence.
+ *
+ *   cache   SNAPKV_CACHE_PLAIN (pages of dtype; k_scales and v_scales NULL), SNAPKV_CACHE_FP8 or SNAPKV_CACHE_FP4: of prefixes' and own rows,
+ *           which lie in one pool of pages
+ *   cu_groups [G + 1] device int32, ascending, within [0, B]; NULL with G == 1: all sequences share the prefix.  Sequences before the first
+ *           group and behind the last see their own rows only
+ *   prefix_table [G, prefix_columns], block_table [B, table_columns] device int32; entries outside [0, num_pages) are clamped
+ *   prefix_lens [G], lens [B] device int32, clamped to [0, max_prefix] and [0, max_len] (either may be zero; a sequence that sees no
+ *           row gets out = 0 and out_lse = -inf);  1 <= max_prefix <= prefix_columns * page_size, 1 <= max_len <= table_columns * page_size
+ *   1 <= G <= B (groups may be empty); B * Hkv < 2^20, G * Hkv * max_prefix <= 2^36; the rest as for snapkv_decode_attention_paged
+ *   workspace 256-byte aligned, of at least snapkv_decode_shared_workspace_bytes(B, G, Hq, Hkv, D, max_prefix, max_len) bytes, as there
+ *           (never 0 for shapes that the step takes)
+ *
+ * Answers are those of snapkv_decode_attention_paged over prefix and own rows in one table, up to rounding, and repeat bit for bit.
+ */
+int snapkv_decode_attention_shared(int dtype, int cache, const void* q, const void* k_pages, const void* k_scales,
+                                   const void* v_pages, const void* v_scales, int64_t num_pages, int page_size,
+                                   const int32_t* cu_groups, int G, const int32_t* prefix_table, int64_t prefix_columns,
+                                   const int32_t* prefix_lens, int64_t max_prefix, const int32_t* block_table,
+                                   int64_t table_columns, const int32_t* lens, int64_t max_len, int B, int Hq, int Hkv,
+                                   int D, void* out, float* out_lse, void* workspace, size_t workspace_bytes, void* stream);
+size_t snapkv_decode_shared_workspace_bytes(int B, int G, int Hq, int Hkv, int D, int64_t max_prefix, int64_t max_len);
 
 /*
  * Top-(kcount) selection alone (Eq. 2), exposed for testing the selector on arbitrary scores:

@@ -18,6 +18,7 @@ LIB_PATH = os.path.join(_PKG, "libsnapkv.so")
 
 POOL_MAX, POOL_AVG = 0, 1
 DTYPE_BF16, DTYPE_F32, DTYPE_F16 = 0, 1, 2
+CACHE_PLAIN, CACHE_FP8, CACHE_FP4 = 0, 1, 2
 
 SYMBOLS = ("snapkv_version", "snapkv_strerror", "snapkv_compress", "snapkv_compress_f32",
            "snapkv_pooled_scores", "snapkv_pooled_scores_f32", "snapkv_workspace_bytes",
@@ -29,7 +30,9 @@ SYMBOLS = ("snapkv_version", "snapkv_strerror", "snapkv_compress", "snapkv_compr
            "snapkv_capacity_for_rate", "snapkv_hit_rate", "snapkv_compress_paged",
            "snapkv_compress_varlen", "snapkv_compress_layers", "snapkv_compress_static",
            "snapkv_compress_ws_status", "snapkv_debug_set_wait_limit", "snapkv_append_paged",
-           "snapkv_prompt_attention", "snapkv_decode_attention_paged", "snapkv_decode_paged_workspace_bytes")
+           "snapkv_prompt_attention", "snapkv_decode_attention_paged", "snapkv_decode_paged_workspace_bytes",
+           "snapkv_append_paged_mx", "snapkv_read_paged_mx", "snapkv_decode_attention_paged_mx",
+           "snapkv_decode_paged_mx_workspace_bytes", "snapkv_decode_attention_shared", "snapkv_decode_shared_workspace_bytes")
 
 _lib = None
 
@@ -107,6 +110,22 @@ def load():
     L.snapkv_decode_paged_workspace_bytes.argtypes = [i32, i32, i32, i32, i64]
     L.snapkv_decode_attention_paged.restype = i32
     L.snapkv_decode_attention_paged.argtypes = [i32, vp, vp, vp, vp, i64, i64, i32, vp, i64, i32, i32, i32, i32, vp, vp, vp, sz, vp]
+    L.snapkv_append_paged_mx.restype = i32
+    L.snapkv_append_paged_mx.argtypes = [i32, i32, vp, vp, vp, vp, vp, vp, i64, i32, i32, i32, i32, i64, i64, i64, i64, i64, i64,
+                                         vp, vp, i64, i32, i32, vp, vp, vp, vp, vp, i64, i64, i32, vp, i64, i64, vp, i64, i64, vp]
+    L.snapkv_read_paged_mx.restype = i32
+    L.snapkv_read_paged_mx.argtypes = [i32, i32, vp, vp, vp, vp, vp, i64, i64, i32, vp, vp, i64, i32, i32, i32, vp, i64, i64, vp, i64,
+                                       i64, vp]
+    L.snapkv_decode_paged_mx_workspace_bytes.restype = sz
+    L.snapkv_decode_paged_mx_workspace_bytes.argtypes = [i32, i32, i32, i32, i64]
+    L.snapkv_decode_attention_paged_mx.restype = i32
+    L.snapkv_decode_attention_paged_mx.argtypes = [i32, i32, vp, vp, vp, vp, vp, vp, i64, i64, i32, vp, i64, i32, i32, i32, i32, vp, vp,
+                                                   vp, sz, vp]
+    L.snapkv_decode_shared_workspace_bytes.restype = sz
+    L.snapkv_decode_shared_workspace_bytes.argtypes = [i32, i32, i32, i32, i32, i64, i64]
+    L.snapkv_decode_attention_shared.restype = i32
+    L.snapkv_decode_attention_shared.argtypes = [i32, i32, vp, vp, vp, vp, vp, i64, i32, vp, i32, vp, i64, vp, i64, vp, i64, vp, i64,
+                                                 i32, i32, i32, i32, vp, vp, vp, sz, vp]
     L.snapkv_release.restype = None
     L.snapkv_release.argtypes = []
     L.snapkv_profile_start.restype = i32
@@ -547,20 +566,18 @@ def _device_of(t: torch.Tensor, name: str) -> int:
     return device
 
 
-def snapkv_append_paged(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
-                        block_table: torch.Tensor, starts: torch.Tensor, cu_seqlens: Optional[torch.Tensor] = None,
-                        positions: Optional[torch.Tensor] = None, cos: Optional[torch.Tensor] = None,
-                        sin: Optional[torch.Tensor] = None, interleaved: bool = False, q: Optional[torch.Tensor] = None,
-                        q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, stream=None) -> None:
-    """k, v [T,Hkv,D] (views with contiguous rows) go into k_pages/v_pages [num_pages, page_size, Hkv, D] behind
-    block_table [B, columns] int32, sequence b's from row starts[b] on; cu_seqlens [B+1] int32, or None: a token per
-    sequence.  With cos/sin [positions, rot_dim/2] float32 the keys, and q [T,Hq,D] -> q_out, are rotated by positions [T]
-    int32 (None: the rows); k_out [T,Hkv,D]: the rotated keys once more."""
-    lib = load()
+def _cache_of(k_pages, k_scales, v_pages, v_scales, Hkv: int, D: int) -> int:
+    """Which codes microscaled pages hold, by their width."""
+    pages, page_size, Hp, width = pool = k_pages.shape
+    if v_pages.shape != pool or Hp != Hkv or width not in (D, D // 2) or k_scales.shape != (pages, page_size, Hkv, D // 32) or \
+            v_scales.shape != k_scales.shape:
+        raise ValueError("microscaled pages must be codes [num_pages, page_size, Hkv, D] or [.., D / 2] and scales [.., D / 32]")
+    return CACHE_FP8 if width == D else CACHE_FP4
+
+
+def _append_args(k, v, block_table, starts, cu_seqlens, positions, cos, sin, interleaved, q, q_out, k_out):
+    """The device, and the C arguments of an append before its pages and behind them."""
     T, Hkv, D = rows = k.shape
-    num_pages, page_size, Hp, Dp = pool = k_pages.shape
-    if v.shape != rows or Hp != Hkv or Dp != D or v_pages.shape != pool:
-        raise ValueError("k, v, k_pages and v_pages disagree on their shapes")
     if block_table.ndim != 2:
         raise ValueError("block_table must be [B, columns]")
     B, columns = block_table.shape
@@ -589,14 +606,80 @@ def snapkv_append_paged(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor,
     qp, qr, qh = _rows(q, "q", dt, dev, T, Hq, D) if Hq else none
     op, orow, oh = _rows(q_out, "q_out", dt, dev, T, Hq, D) if Hq else none
     cp, cr, ch = _rows(k_out, "k_out", dt, dev, T, Hkv, D) if k_out is not None else none
+    before = (_dtype_code(k), qp, kp, vp, _at(cu_seqlens, "cu_seqlens", i32, dev) if cu_seqlens is not None else None,
+              _at(starts, "starts", i32, dev), _at(positions, "positions", i32, dev) if positions is not None else None, T, B,
+              Hq, Hkv, D, qr, qh, kr, kh, vr, vh,
+              _at(cos, "cos", torch.float32, dev) if cos is not None else None,
+              _at(sin, "sin", torch.float32, dev) if cos is not None else None, P, 2 * half, 1 if interleaved else 0)
+    return dev, before, (op, orow, oh, cp, cr, ch)
+
+
+def snapkv_append_paged(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
+                        block_table: torch.Tensor, starts: torch.Tensor, cu_seqlens: Optional[torch.Tensor] = None,
+                        positions: Optional[torch.Tensor] = None, cos: Optional[torch.Tensor] = None,
+                        sin: Optional[torch.Tensor] = None, interleaved: bool = False, q: Optional[torch.Tensor] = None,
+                        q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, stream=None) -> None:
+    """k, v [T,Hkv,D] (views with contiguous rows) go into k_pages/v_pages [num_pages, page_size, Hkv, D] behind
+    block_table [B, columns] int32, sequence b's from row starts[b] on; cu_seqlens [B+1] int32, or None: a token per
+    sequence.  With cos/sin [positions, rot_dim/2] float32 the keys, and q [T,Hq,D] -> q_out, are rotated by positions [T]
+    int32 (None: the rows); k_out [T,Hkv,D]: the rotated keys once more."""
+    lib = load()
+    T, Hkv, D = rows = k.shape
+    num_pages, page_size, Hp, Dp = pool = k_pages.shape
+    if v.shape != rows or Hp != Hkv or Dp != D or v_pages.shape != pool:
+        raise ValueError("k, v, k_pages and v_pages disagree on their shapes")
+    dev, before, after = _append_args(k, v, block_table, starts, cu_seqlens, positions, cos, sin, interleaved, q, q_out, k_out)
     _check(lib.snapkv_append_paged(
-        _dtype_code(k), qp, kp, vp, _at(cu_seqlens, "cu_seqlens", i32, dev) if cu_seqlens is not None else None,
-        _at(starts, "starts", i32, dev), _at(positions, "positions", i32, dev) if positions is not None else None, T, B,
-        Hq, Hkv, D, qr, qh, kr, kh, vr, vh,
-        _at(cos, "cos", torch.float32, dev) if cos is not None else None, _at(sin, "sin", torch.float32, dev) if cos is not None else None,
-        P, 2 * half, 1 if interleaved else 0,
-        _at(k_pages, "k_pages", dt, dev), _at(v_pages, "v_pages", dt, dev), _at(block_table, "block_table", i32, dev),
-        columns, num_pages, page_size, op, orow, oh, cp, cr, ch, _stream_on(dev, stream)))
+        *before, _at(k_pages, "k_pages", k.dtype, dev), _at(v_pages, "v_pages", k.dtype, dev),
+        _at(block_table, "block_table", torch.int32, dev), block_table.shape[1], num_pages, page_size, *after,
+        _stream_on(dev, stream)))
+
+
+def snapkv_append_paged_mx(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, k_scales: torch.Tensor, v_pages: torch.Tensor,
+                           v_scales: torch.Tensor, block_table: torch.Tensor, starts: torch.Tensor,
+                           cu_seqlens: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None,
+                           cos: Optional[torch.Tensor] = None, sin: Optional[torch.Tensor] = None, interleaved: bool = False,
+                           q: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                           k_out: Optional[torch.Tensor] = None, stream=None) -> None:
+    """snapkv_append_paged into microscaled pages, all uint8: codes k_pages/v_pages [num_pages, page_size, Hkv, D] (e4m3) or
+    [.., D/2] (e2m1, two to a byte) and k_scales/v_scales [num_pages, page_size, Hkv, D/32]."""
+    lib = load()
+    T, Hkv, D = k.shape
+    if v.shape != k.shape:
+        raise ValueError("k and v disagree on their shapes")
+    cache, u8 = _cache_of(k_pages, k_scales, v_pages, v_scales, Hkv, D), torch.uint8
+    dev, before, after = _append_args(k, v, block_table, starts, cu_seqlens, positions, cos, sin, interleaved, q, q_out, k_out)
+    num_pages, page_size = k_pages.shape[:2]
+    _check(lib.snapkv_append_paged_mx(
+        before[0], cache, *before[1:], _at(k_pages, "k_pages", u8, dev), _at(k_scales, "k_scales", u8, dev),
+        _at(v_pages, "v_pages", u8, dev), _at(v_scales, "v_scales", u8, dev), _at(block_table, "block_table", torch.int32, dev),
+        block_table.shape[1], num_pages, page_size, *after, _stream_on(dev, stream)))
+
+
+def snapkv_read_paged_mx(k_pages: torch.Tensor, k_scales: torch.Tensor, v_pages: torch.Tensor, v_scales: torch.Tensor,
+                         block_table: torch.Tensor, starts: torch.Tensor, k_out: torch.Tensor, v_out: torch.Tensor,
+                         cu_seqlens: Optional[torch.Tensor] = None, stream=None) -> None:
+    """Rows of microscaled pages (as for snapkv_append_paged_mx) -> k_out, v_out [T,Hkv,D] (views with contiguous rows, e.g. of
+    head-major storage): sequence b's from row starts[b] on, packed by cu_seqlens [B+1] int32 (None: one row per sequence)."""
+    lib = load()
+    T, Hkv, D = k_out.shape
+    if v_out.shape != k_out.shape or v_out.dtype is not k_out.dtype:
+        raise ValueError("k_out and v_out disagree on their shapes or types")
+    cache, u8, i32 = _cache_of(k_pages, k_scales, v_pages, v_scales, Hkv, D), torch.uint8, torch.int32
+    if block_table.ndim != 2:
+        raise ValueError("block_table must be [B, columns]")
+    B, columns = block_table.shape
+    if starts.shape != (B,) or (cu_seqlens is not None and cu_seqlens.shape != (B + 1,)):
+        raise ValueError("starts must be [B] and cu_seqlens [B + 1]")
+    num_pages, page_size = k_pages.shape[:2]
+    dev, dt = _device_of(k_out, "k_out"), k_out.dtype
+    kp, kr, kh = _rows(k_out, "k_out", dt, dev, T, Hkv, D)
+    vp, vr, vh = _rows(v_out, "v_out", dt, dev, T, Hkv, D)
+    _check(lib.snapkv_read_paged_mx(
+        _dtype_code(k_out), cache, _at(k_pages, "k_pages", u8, dev), _at(k_scales, "k_scales", u8, dev),
+        _at(v_pages, "v_pages", u8, dev), _at(v_scales, "v_scales", u8, dev), _at(block_table, "block_table", i32, dev), columns,
+        num_pages, page_size, _at(cu_seqlens, "cu_seqlens", i32, dev) if cu_seqlens is not None else None,
+        _at(starts, "starts", i32, dev), T, B, Hkv, D, kp, kr, kh, vp, vr, vh, _stream_on(dev, stream)))
 
 
 def snapkv_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqlens: torch.Tensor, out: torch.Tensor,
@@ -660,6 +743,98 @@ def snapkv_decode_attention_paged(q: torch.Tensor, k_pages: torch.Tensor, v_page
     else:
         ws, size = _at(workspace, "workspace", torch.uint8, dev), workspace.numel()
     _check(lib.snapkv_decode_attention_paged(_dtype_code(q), *ins, max_len, B, Hq, Hkv, D, *outs, ws, size, st))
+
+
+@functools.lru_cache(maxsize=256)
+def snapkv_decode_paged_mx_workspace_bytes(B: int, Hq: int, Hkv: int, D: int, max_len: int) -> int:
+    return int(load().snapkv_decode_paged_mx_workspace_bytes(B, Hq, Hkv, D, max_len))
+
+
+@functools.lru_cache(maxsize=256)
+def snapkv_decode_shared_workspace_bytes(B: int, G: int, Hq: int, Hkv: int, D: int, max_prefix: int, max_len: int) -> int:
+    return int(load().snapkv_decode_shared_workspace_bytes(B, G, Hq, Hkv, D, max_prefix, max_len))
+
+
+def _step_workspace(workspace, need, q, dev: int, stream):
+    """Address and size of a step's workspace, the stream, and what owns the memory (None given: need() bytes for this call)."""
+    st = _stream_on(dev, stream)
+    if workspace is not None:
+        return _at(workspace, "workspace", torch.uint8, dev), workspace.numel(), st, workspace
+    if stream is not None and st != _stream(None):
+        raise ValueError("a step on another stream than the current one needs a workspace of the caller's")
+    size = need()
+    if not size:
+        return None, 0, st, None
+    workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
+    return workspace.data_ptr(), size, st, workspace
+
+
+def snapkv_decode_attention_paged_mx(q: torch.Tensor, k_pages: torch.Tensor, k_scales: torch.Tensor, v_pages: torch.Tensor,
+                                     v_scales: torch.Tensor, block_table: torch.Tensor, lens: torch.Tensor, max_len: int,
+                                     out: torch.Tensor, out_lse: Optional[torch.Tensor] = None,
+                                     workspace: Optional[torch.Tensor] = None, stream=None) -> None:
+    """snapkv_decode_attention_paged over microscaled pages (as for snapkv_append_paged_mx); q and out bf16 or fp16.  `workspace`: of
+    snapkv_decode_paged_mx_workspace_bytes, or None, as there."""
+    lib = load()
+    max_len = int(max_len)
+    B, Hq, D = q.shape
+    num_pages, page_size, Hkv = k_pages.shape[:3]
+    cache, u8, i32 = _cache_of(k_pages, k_scales, v_pages, v_scales, Hkv, D), torch.uint8, torch.int32
+    if block_table.ndim != 2 or block_table.shape[0] != B or lens.shape != (B,):
+        raise ValueError("block_table must be [B, columns] and lens [B]")
+    if out.shape != (B, Hq, D) or (out_lse is not None and out_lse.shape != (B, Hq)):
+        raise ValueError("out must be [B, Hq, D] and out_lse [B, Hq]")
+    dev, dt = _device_of(q, "q"), q.dtype
+    ins = (_at(q, "q", dt, dev), _at(k_pages, "k_pages", u8, dev), _at(k_scales, "k_scales", u8, dev),
+           _at(v_pages, "v_pages", u8, dev), _at(v_scales, "v_scales", u8, dev), _at(block_table, "block_table", i32, dev),
+           block_table.shape[1], num_pages, page_size, _at(lens, "lens", i32, dev))
+    outs = (_at(out, "out", dt, dev), _at(out_lse, "out_lse", torch.float32, dev) if out_lse is not None else None)
+    ws, size, st, _owner = _step_workspace(
+        workspace, lambda: snapkv_decode_paged_mx_workspace_bytes(B, Hq, Hkv, D, max_len), q, dev, stream)
+    _check(lib.snapkv_decode_attention_paged_mx(_dtype_code(q), cache, *ins, max_len, B, Hq, Hkv, D, *outs, ws, size, st))
+
+
+def snapkv_decode_attention_shared(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, prefix_table: torch.Tensor,
+                                   prefix_lens: torch.Tensor, max_prefix: int, block_table: torch.Tensor, lens: torch.Tensor,
+                                   max_len: int, out: torch.Tensor, out_lse: Optional[torch.Tensor] = None,
+                                   cu_groups: Optional[torch.Tensor] = None, k_scales: Optional[torch.Tensor] = None,
+                                   v_scales: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None,
+                                   stream=None) -> None:
+    """One step for sequences that share prefixes: group i's, cu_groups[i] .. cu_groups[i+1] - 1 ([G+1] int32; None: one group of
+    all), see the prefix_lens[i] rows (at most max_prefix) behind prefix_table [G, columns], then their own lens rows (at
+    most max_len) behind block_table [B, columns].  q, out [B,Hq,D] bf16 or fp16; pages of q's type or, with k_scales and
+    v_scales, microscaled ones (as for snapkv_append_paged_mx).  `workspace`: of snapkv_decode_shared_workspace_bytes; None:
+    allocated by torch for this call, on the current stream."""
+    lib = load()
+    max_prefix, max_len = int(max_prefix), int(max_len)
+    B, Hq, D = q.shape
+    num_pages, page_size, Hkv, width = pool = k_pages.shape
+    i32, cache, kind = torch.int32, CACHE_PLAIN, q.dtype
+    if k_scales is not None or v_scales is not None:
+        if k_scales is None or v_scales is None:
+            raise ValueError("k_scales and v_scales must both be given")
+        cache, kind = _cache_of(k_pages, k_scales, v_pages, v_scales, Hkv, D), torch.uint8
+    elif width != D or v_pages.shape != pool:
+        raise ValueError("q, k_pages and v_pages disagree on their shapes")
+    if prefix_table.ndim != 2:
+        raise ValueError("prefix_table must be [G, columns]")
+    G = prefix_table.shape[0]
+    if prefix_lens.shape != (G,) or (cu_groups is not None and cu_groups.shape != (G + 1,)) or (cu_groups is None and G != 1):
+        raise ValueError("prefix_lens must be [G] and cu_groups [G + 1] (None: one group)")
+    if block_table.ndim != 2 or block_table.shape[0] != B or lens.shape != (B,):
+        raise ValueError("block_table must be [B, columns] and lens [B]")
+    if out.shape != (B, Hq, D) or (out_lse is not None and out_lse.shape != (B, Hq)):
+        raise ValueError("out must be [B, Hq, D] and out_lse [B, Hq]")
+    dev, dt = _device_of(q, "q"), q.dtype
+    ks, vs = (_at(k_scales, "k_scales", kind, dev), _at(v_scales, "v_scales", kind, dev)) if cache else (None, None)
+    ins = (_at(q, "q", dt, dev), _at(k_pages, "k_pages", kind, dev), ks, _at(v_pages, "v_pages", kind, dev), vs, num_pages, page_size,
+           _at(cu_groups, "cu_groups", i32, dev) if cu_groups is not None else None, G,
+           _at(prefix_table, "prefix_table", i32, dev), prefix_table.shape[1], _at(prefix_lens, "prefix_lens", i32, dev), max_prefix,
+           _at(block_table, "block_table", i32, dev), block_table.shape[1], _at(lens, "lens", i32, dev), max_len)
+    outs = (_at(out, "out", dt, dev), _at(out_lse, "out_lse", torch.float32, dev) if out_lse is not None else None)
+    ws, size, st, _owner = _step_workspace(
+        workspace, lambda: snapkv_decode_shared_workspace_bytes(B, G, Hq, Hkv, D, max_prefix, max_len), q, dev, stream)
+    _check(lib.snapkv_decode_attention_shared(_dtype_code(q), cache, *ins, B, Hq, Hkv, D, *outs, ws, size, st))
 
 
 def compress(q_win, k, v, pool_kind: int, p: int, C: int, stream=None

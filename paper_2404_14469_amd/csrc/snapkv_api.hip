@@ -151,6 +151,126 @@ int check_paged_shape(int B, int Hq, int Hkv, int D, int64_t max_len) {
     return SNAPKV_OK;
 }
 
+// The checks of snapkv_append_paged and what its kernels take; *empty: there is nothing to do.
+int append_args(int dtype, const void* q, const void* k, const void* v, const int32_t* cu_seqlens, const int32_t* starts,
+                const int32_t* positions, int64_t T, int B, int Hq, int Hkv, int D, int64_t q_row_stride,
+                int64_t q_head_stride, int64_t k_row_stride, int64_t k_head_stride, int64_t v_row_stride,
+                int64_t v_head_stride, const float* cos, const float* sin, int64_t n_positions, int rot_dim,
+                int interleaved, void* k_pages, void* v_pages, const int32_t* block_table, int64_t table_columns,
+                int64_t num_pages, int page_size, void* q_out, int64_t q_out_row_stride, int64_t q_out_head_stride,
+                void* k_out, int64_t k_out_row_stride, int64_t k_out_head_stride, AppendArgs& A, bool* empty) {
+    if (!valid_dtype(dtype)) return SNAPKV_ERR_INVALID_ARG;
+    if (T < 0 || B < 0 || Hq < 0 || Hkv < 1) return SNAPKV_ERR_INVALID_ARG;
+    *empty = T == 0 || B == 0;
+    if (*empty) return SNAPKV_OK;
+    if (!k || !v || !starts || !k_pages || !v_pages || !block_table) return SNAPKV_ERR_INVALID_ARG;
+    if ((Hq > 0) != (q != nullptr) || (Hq > 0) != (q_out != nullptr) || Hq % Hkv != 0) return SNAPKV_ERR_INVALID_ARG;
+    if (!cu_seqlens && T != B) return SNAPKV_ERR_INVALID_ARG;
+    if (num_pages < 1 || page_size < 1 || table_columns < 1) return SNAPKV_ERR_INVALID_ARG;
+    if (rot_dim < 0 || rot_dim > D || (interleaved != 0 && interleaved != 1)) return SNAPKV_ERR_INVALID_ARG;
+    if (rot_dim > 0 && (!cos || !sin || n_positions < 1)) return SNAPKV_ERR_INVALID_ARG;
+    if (D != 64 && D != 128) return SNAPKV_ERR_UNSUPPORTED;
+    const int e = elem_bytes(dtype);
+    if (rot_dim % (32 / e) != 0) return SNAPKV_ERR_UNSUPPORTED;
+    if (T >= (int64_t)1 << 26 || B >= 1 << 24 || Hq + 2 * (int64_t)Hkv > 65535 || num_pages > ((int64_t)1 << 31) ||
+        table_columns > ((int64_t)1 << 31) || n_positions > ((int64_t)1 << 31))
+        return SNAPKV_ERR_UNSUPPORTED;
+    struct { const void* p; int64_t rows, heads; } const t[] = {
+        {k, k_row_stride, k_head_stride}, {v, v_row_stride, v_head_stride}, {q, q_row_stride, q_head_stride},
+        {q_out, q_out_row_stride, q_out_head_stride}, {k_out, k_out_row_stride, k_out_head_stride}};
+    for (const auto& x : t) {
+        if (!x.p) continue;
+        const int rc = check_rows(x.p, x.rows, x.heads, D, e);
+        if (rc != SNAPKV_OK) return rc;
+    }
+    if ((q_out && rows_overlap(q_out_row_stride, q_out_head_stride, T, Hq, D)) ||
+        (k_out && rows_overlap(k_out_row_stride, k_out_head_stride, T, Hkv, D)))
+        return SNAPKV_ERR_INVALID_ARG;
+    if (!aligned16(k_pages) || !aligned16(v_pages) || !aligned16(cos) || !aligned16(sin)) return SNAPKV_ERR_MISALIGNED;
+    for (const int32_t* x : {cu_seqlens, starts, positions, block_table})
+        if ((reinterpret_cast<uintptr_t>(x) & 3u) != 0) return SNAPKV_ERR_MISALIGNED;
+    A.q = static_cast<const char*>(q);
+    A.k = static_cast<const char*>(k);
+    A.v = static_cast<const char*>(v);
+    A.q_rs = q_row_stride * e;
+    A.q_hs = q_head_stride * e;
+    A.k_rs = k_row_stride * e;
+    A.k_hs = k_head_stride * e;
+    A.v_rs = v_row_stride * e;
+    A.v_hs = v_head_stride * e;
+    A.q_out = static_cast<char*>(q_out);
+    A.k_out = static_cast<char*>(k_out);
+    A.qo_rs = q_out_row_stride * e;
+    A.qo_hs = q_out_head_stride * e;
+    A.ko_rs = k_out_row_stride * e;
+    A.ko_hs = k_out_head_stride * e;
+    A.k_pages = static_cast<char*>(k_pages);
+    A.v_pages = static_cast<char*>(v_pages);
+    A.table = block_table;
+    A.table_stride = table_columns;
+    A.table_rows = table_columns * page_size;
+    A.pages = num_pages;
+    A.starts = starts;
+    A.cu = cu_seqlens;
+    A.positions = positions;
+    A.cos = cos;
+    A.sin = sin;
+    A.npos = n_positions;
+    A.T = T;
+    A.B = B;
+    A.Hq = Hq;
+    A.Hkv = Hkv;
+    A.page = page_size;
+    A.rot = rot_dim;
+    return SNAPKV_OK;
+}
+
+// The shapes that a step over shared prefixes takes.
+int check_shared_shape(int B, int G, int Hq, int Hkv, int D, int64_t max_prefix, int64_t max_len) {
+    const int rc = check_paged_shape(B, Hq, Hkv, D, max_len);
+    if (rc == SNAPKV_ERR_INVALID_ARG || G < 1 || G > B || max_prefix < 1) return SNAPKV_ERR_INVALID_ARG;
+    if (rc != SNAPKV_OK || max_prefix > (int64_t)1 << 30) return SNAPKV_ERR_UNSUPPORTED;
+    // (one launch for prefixes and own rows)
+    if ((int64_t)B * Hkv >= (int64_t)1 << 20 || (int64_t)G * Hkv * max_prefix > (int64_t)1 << 36) return SNAPKV_ERR_UNSUPPORTED;
+    return SNAPKV_OK;
+}
+
+// The checks that both steps over plain or microscaled pages share, in the order of snapkv_decode_attention_paged's; shape: of the sizes.
+int shared_args(int dtype, int cache, const void* q, const void* k_pages, const void* k_scales, const void* v_pages,
+                const void* v_scales, int64_t num_pages, int page_size, const int32_t* block_table, int64_t table_columns,
+                const int32_t* lens, int64_t max_len, int shape, int B, int Hq, int Hkv, void* out, float* out_lse,
+                SharedArgs& A) {
+    if (!valid_dtype(dtype) || cache < SNAPKV_CACHE_PLAIN || cache > SNAPKV_CACHE_FP4) return SNAPKV_ERR_INVALID_ARG;
+    if (!q || !k_pages || !v_pages || !block_table || !lens || !out) return SNAPKV_ERR_INVALID_ARG;
+    if ((cache != SNAPKV_CACHE_PLAIN) != (k_scales != nullptr) || (k_scales != nullptr) != (v_scales != nullptr)) return SNAPKV_ERR_INVALID_ARG;
+    if (num_pages < 1 || page_size < 1 || table_columns < 1) return SNAPKV_ERR_INVALID_ARG;
+    if (shape != SNAPKV_OK) return shape;
+    if (dtype == SNAPKV_DTYPE_F32 || num_pages > ((int64_t)1 << 31) || table_columns > ((int64_t)1 << 31)) return SNAPKV_ERR_UNSUPPORTED;
+    if (max_len > table_columns * page_size) return SNAPKV_ERR_INVALID_ARG;
+    for (const void* x : {q, k_pages, k_scales, v_pages, v_scales, (const void*)out})
+        if (!aligned16(x)) return SNAPKV_ERR_MISALIGNED;
+    for (const void* x : {(const void*)out_lse, (const void*)lens, (const void*)block_table})
+        if ((reinterpret_cast<uintptr_t>(x) & 3u) != 0) return SNAPKV_ERR_MISALIGNED;
+    A.q = static_cast<const char*>(q);
+    A.k = static_cast<const char*>(k_pages);
+    A.v = static_cast<const char*>(v_pages);
+    A.k_scales = static_cast<const unsigned char*>(k_scales);
+    A.v_scales = static_cast<const unsigned char*>(v_scales);
+    A.table = block_table;
+    A.lens = lens;
+    A.table_stride = table_columns;
+    A.pages = num_pages;
+    A.max_len = max_len;
+    A.B = B;
+    A.Hq = Hq;
+    A.Hkv = Hkv;
+    A.g = Hq / Hkv;
+    A.page = page_size;
+    A.out = static_cast<char*>(out);
+    A.lse = out_lse;
+    return SNAPKV_OK;
+}
+
 // Shape checks shared by every entry point that scores (steps 1-3).
 int check_score_args(const void* q_win, const void* k, int64_t L, int Hq, int Hkv, int D, int W,
                      int pool_kind, int p) {
@@ -1276,71 +1396,91 @@ int snapkv_append_paged(int dtype, const void* q, const void* k, const void* v, 
                         const int32_t* block_table, int64_t table_columns, int64_t num_pages, int page_size, void* q_out,
                         int64_t q_out_row_stride, int64_t q_out_head_stride, void* k_out, int64_t k_out_row_stride,
                         int64_t k_out_head_stride, void* stream) {
-    if (!valid_dtype(dtype)) return SNAPKV_ERR_INVALID_ARG;
-    if (T < 0 || B < 0 || Hq < 0 || Hkv < 1) return SNAPKV_ERR_INVALID_ARG;
+    AppendArgs A{};
+    bool empty = false;
+    const int rc = append_args(dtype, q, k, v, cu_seqlens, starts, positions, T, B, Hq, Hkv, D, q_row_stride, q_head_stride,
+                               k_row_stride, k_head_stride, v_row_stride, v_head_stride, cos, sin, n_positions, rot_dim, interleaved,
+                               k_pages, v_pages, block_table, table_columns, num_pages, page_size, q_out, q_out_row_stride,
+                               q_out_head_stride, k_out, k_out_row_stride, k_out_head_stride, A, &empty);
+    if (rc != SNAPKV_OK || empty) return rc;
+    return launch_append(dtype, D, interleaved != 0, A, static_cast<hipStream_t>(stream)) == hipSuccess ? SNAPKV_OK
+                                                                                                    : SNAPKV_ERR_HIP;
+}
+
+int snapkv_append_paged_mx(int dtype, int cache, const void* q, const void* k, const void* v, const int32_t* cu_seqlens,
+                           const int32_t* starts, const int32_t* positions, int64_t T, int B, int Hq, int Hkv, int D,
+                           int64_t q_row_stride, int64_t q_head_stride, int64_t k_row_stride, int64_t k_head_stride,
+                           int64_t v_row_stride, int64_t v_head_stride, const float* cos, const float* sin,
+                           int64_t n_positions, int rot_dim, int interleaved, void* k_pages, void* k_scales, void* v_pages,
+                           void* v_scales, const int32_t* block_table, int64_t table_columns, int64_t num_pages,
+                           int page_size, void* q_out, int64_t q_out_row_stride, int64_t q_out_head_stride, void* k_out,
+                           int64_t k_out_row_stride, int64_t k_out_head_stride, void* stream) {
+    if (cache != SNAPKV_CACHE_FP8 && cache != SNAPKV_CACHE_FP4) return SNAPKV_ERR_INVALID_ARG;
+    AppendArgs A{};
+    bool empty = false;
+    const int rc = append_args(dtype, q, k, v, cu_seqlens, starts, positions, T, B, Hq, Hkv, D, q_row_stride, q_head_stride,
+                               k_row_stride, k_head_stride, v_row_stride, v_head_stride, cos, sin, n_positions, rot_dim, interleaved,
+                               k_pages, v_pages, block_table, table_columns, num_pages, page_size, q_out, q_out_row_stride,
+                               q_out_head_stride, k_out, k_out_row_stride, k_out_head_stride, A, &empty);
+    if (rc != SNAPKV_OK || empty) return rc;
+    if (!k_scales || !v_scales) return SNAPKV_ERR_INVALID_ARG;
+    if (!aligned16(k_scales) || !aligned16(v_scales)) return SNAPKV_ERR_MISALIGNED;
+    A.k_scales = static_cast<unsigned char*>(k_scales);
+    A.v_scales = static_cast<unsigned char*>(v_scales);
+    return launch_append_mx(dtype, cache, D, interleaved != 0, A, static_cast<hipStream_t>(stream)) == hipSuccess ? SNAPKV_OK
+                                                                                                              : SNAPKV_ERR_HIP;
+}
+
+int snapkv_read_paged_mx(int dtype, int cache, const void* k_pages, const void* k_scales, const void* v_pages,
+                         const void* v_scales, const int32_t* block_table, int64_t table_columns, int64_t num_pages,
+                         int page_size, const int32_t* cu_seqlens, const int32_t* starts, int64_t T, int B, int Hkv, int D,
+                         void* k_out, int64_t k_out_row_stride, int64_t k_out_head_stride, void* v_out,
+                         int64_t v_out_row_stride, int64_t v_out_head_stride, void* stream) {
+    if (!valid_dtype(dtype) || (cache != SNAPKV_CACHE_FP8 && cache != SNAPKV_CACHE_FP4)) return SNAPKV_ERR_INVALID_ARG;
+    if (T < 0 || B < 0 || Hkv < 1) return SNAPKV_ERR_INVALID_ARG;
     if (T == 0 || B == 0) return SNAPKV_OK;
-    if (!k || !v || !starts || !k_pages || !v_pages || !block_table) return SNAPKV_ERR_INVALID_ARG;
-    if ((Hq > 0) != (q != nullptr) || (Hq > 0) != (q_out != nullptr) || Hq % Hkv != 0) return SNAPKV_ERR_INVALID_ARG;
+    if (!starts || !block_table || !k_out || !v_out) return SNAPKV_ERR_INVALID_ARG;
+    for (const void* x : {k_pages, k_scales, v_pages, v_scales})
+        if (!x) return SNAPKV_ERR_INVALID_ARG;
     if (!cu_seqlens && T != B) return SNAPKV_ERR_INVALID_ARG;
     if (num_pages < 1 || page_size < 1 || table_columns < 1) return SNAPKV_ERR_INVALID_ARG;
-    if (rot_dim < 0 || rot_dim > D || (interleaved != 0 && interleaved != 1)) return SNAPKV_ERR_INVALID_ARG;
-    if (rot_dim > 0 && (!cos || !sin || n_positions < 1)) return SNAPKV_ERR_INVALID_ARG;
     if (D != 64 && D != 128) return SNAPKV_ERR_UNSUPPORTED;
-    const int e = elem_bytes(dtype);
-    if (rot_dim % (32 / e) != 0) return SNAPKV_ERR_UNSUPPORTED;
-    if (T >= (int64_t)1 << 26 || B >= 1 << 24 || Hq + 2 * (int64_t)Hkv > 65535 || num_pages > ((int64_t)1 << 31) ||
-        table_columns > ((int64_t)1 << 31) || n_positions > ((int64_t)1 << 31))
+    if (T >= (int64_t)1 << 26 || B >= 1 << 24 || 2 * (int64_t)Hkv > 65535 || num_pages > ((int64_t)1 << 31) ||
+        table_columns > ((int64_t)1 << 31))
         return SNAPKV_ERR_UNSUPPORTED;
-    struct { const void* p; int64_t rows, heads; } const t[] = {
-        {k, k_row_stride, k_head_stride}, {v, v_row_stride, v_head_stride}, {q, q_row_stride, q_head_stride},
-        {q_out, q_out_row_stride, q_out_head_stride}, {k_out, k_out_row_stride, k_out_head_stride}};
+    const int e = elem_bytes(dtype);
+    struct { const void* p; int64_t rows, heads; } const t[] = {{k_out, k_out_row_stride, k_out_head_stride}, {v_out, v_out_row_stride, v_out_head_stride}};
     for (const auto& x : t) {
-        if (!x.p) continue;
         const int rc = check_rows(x.p, x.rows, x.heads, D, e);
         if (rc != SNAPKV_OK) return rc;
+        if (rows_overlap(x.rows, x.heads, T, Hkv, D)) return SNAPKV_ERR_INVALID_ARG;
     }
-    if ((q_out && rows_overlap(q_out_row_stride, q_out_head_stride, T, Hq, D)) ||
-        (k_out && rows_overlap(k_out_row_stride, k_out_head_stride, T, Hkv, D)))
-        return SNAPKV_ERR_INVALID_ARG;
-    if (!aligned16(k_pages) || !aligned16(v_pages) || !aligned16(cos) || !aligned16(sin)) return SNAPKV_ERR_MISALIGNED;
-    for (const int32_t* x : {cu_seqlens, starts, positions, block_table})
+    for (const void* x : {k_pages, k_scales, v_pages, v_scales})
+        if (!aligned16(x)) return SNAPKV_ERR_MISALIGNED;
+    for (const int32_t* x : {cu_seqlens, starts, block_table})
         if ((reinterpret_cast<uintptr_t>(x) & 3u) != 0) return SNAPKV_ERR_MISALIGNED;
     AppendArgs A{};
-    A.q = static_cast<const char*>(q);
-    A.k = static_cast<const char*>(k);
-    A.v = static_cast<const char*>(v);
-    A.q_rs = q_row_stride * e;
-    A.q_hs = q_head_stride * e;
-    A.k_rs = k_row_stride * e;
-    A.k_hs = k_head_stride * e;
-    A.v_rs = v_row_stride * e;
-    A.v_hs = v_head_stride * e;
-    A.q_out = static_cast<char*>(q_out);
+    A.k_pages = static_cast<char*>(const_cast<void*>(k_pages));         // (only read)
+    A.v_pages = static_cast<char*>(const_cast<void*>(v_pages));
+    A.k_scales = static_cast<unsigned char*>(const_cast<void*>(k_scales));
+    A.v_scales = static_cast<unsigned char*>(const_cast<void*>(v_scales));
     A.k_out = static_cast<char*>(k_out);
-    A.qo_rs = q_out_row_stride * e;
-    A.qo_hs = q_out_head_stride * e;
+    A.v_out = static_cast<char*>(v_out);
     A.ko_rs = k_out_row_stride * e;
     A.ko_hs = k_out_head_stride * e;
-    A.k_pages = static_cast<char*>(k_pages);
-    A.v_pages = static_cast<char*>(v_pages);
+    A.vo_rs = v_out_row_stride * e;
+    A.vo_hs = v_out_head_stride * e;
     A.table = block_table;
     A.table_stride = table_columns;
     A.table_rows = table_columns * page_size;
     A.pages = num_pages;
     A.starts = starts;
     A.cu = cu_seqlens;
-    A.positions = positions;
-    A.cos = cos;
-    A.sin = sin;
-    A.npos = n_positions;
     A.T = T;
     A.B = B;
-    A.Hq = Hq;
     A.Hkv = Hkv;
     A.page = page_size;
-    A.rot = rot_dim;
-    return launch_append(dtype, D, interleaved != 0, A, static_cast<hipStream_t>(stream)) == hipSuccess ? SNAPKV_OK
-                                                                                                    : SNAPKV_ERR_HIP;
+    return launch_read_mx(dtype, cache, D, A, static_cast<hipStream_t>(stream)) == hipSuccess ? SNAPKV_OK : SNAPKV_ERR_HIP;
 }
 
 int snapkv_prompt_attention(int dtype, const void* q, const void* k, const void* v, const int32_t* cu_seqlens, int B,
@@ -1422,6 +1562,58 @@ int snapkv_decode_attention_paged(int dtype, const void* q, const void* k_pages,
     A.out = static_cast<char*>(out);
     A.lse = out_lse;
     return launch_paged(dtype, D, A, workspace, static_cast<hipStream_t>(stream)) == hipSuccess ? SNAPKV_OK : SNAPKV_ERR_HIP;
+}
+
+size_t snapkv_decode_paged_mx_workspace_bytes(int B, int Hq, int Hkv, int D, int64_t max_len) {
+    if (check_paged_shape(B, Hq, Hkv, D, max_len) != SNAPKV_OK) return 0;
+    return shared_plan(B, 0, Hq, Hkv, D, 0, max_len).bytes;
+}
+
+size_t snapkv_decode_shared_workspace_bytes(int B, int G, int Hq, int Hkv, int D, int64_t max_prefix, int64_t max_len) {
+    if (check_shared_shape(B, G, Hq, Hkv, D, max_prefix, max_len) != SNAPKV_OK) return 0;
+    return shared_plan(B, G, Hq, Hkv, D, max_prefix, max_len).bytes;
+}
+
+int snapkv_decode_attention_paged_mx(int dtype, int cache, const void* q, const void* k_pages, const void* k_scales,
+                                     const void* v_pages, const void* v_scales, const int32_t* block_table,
+                                     int64_t table_columns, int64_t num_pages, int page_size, const int32_t* lens,
+                                     int64_t max_len, int B, int Hq, int Hkv, int D, void* out, float* out_lse,
+                                     void* workspace, size_t workspace_bytes, void* stream) {
+    if (cache != SNAPKV_CACHE_FP8 && cache != SNAPKV_CACHE_FP4) return SNAPKV_ERR_INVALID_ARG;
+    SharedArgs A{};
+    const int rc = shared_args(dtype, cache, q, k_pages, k_scales, v_pages, v_scales, num_pages, page_size, block_table, table_columns,
+                               lens, max_len, check_paged_shape(B, Hq, Hkv, D, max_len), B, Hq, Hkv, out, out_lse, A);
+    if (rc != SNAPKV_OK) return rc;
+    const size_t need = shared_plan(B, 0, Hq, Hkv, D, 0, max_len).bytes;
+    if (need > 0 && (!workspace || workspace_bytes < need)) return SNAPKV_ERR_WORKSPACE;
+    if (need > 0 && (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return SNAPKV_ERR_MISALIGNED;
+    return launch_shared(dtype, cache, D, A, workspace, static_cast<hipStream_t>(stream)) == hipSuccess ? SNAPKV_OK : SNAPKV_ERR_HIP;
+}
+
+int snapkv_decode_attention_shared(int dtype, int cache, const void* q, const void* k_pages, const void* k_scales,
+                                   const void* v_pages, const void* v_scales, int64_t num_pages, int page_size,
+                                   const int32_t* cu_groups, int G, const int32_t* prefix_table, int64_t prefix_columns,
+                                   const int32_t* prefix_lens, int64_t max_prefix, const int32_t* block_table,
+                                   int64_t table_columns, const int32_t* lens, int64_t max_len, int B, int Hq, int Hkv,
+                                   int D, void* out, float* out_lse, void* workspace, size_t workspace_bytes, void* stream) {
+    if (!prefix_table || !prefix_lens || prefix_columns < 1 || (!cu_groups && G != 1)) return SNAPKV_ERR_INVALID_ARG;
+    SharedArgs A{};
+    const int rc = shared_args(dtype, cache, q, k_pages, k_scales, v_pages, v_scales, num_pages, page_size, block_table, table_columns,
+                               lens, max_len, check_shared_shape(B, G, Hq, Hkv, D, max_prefix, max_len), B, Hq, Hkv, out, out_lse, A);
+    if (rc != SNAPKV_OK) return rc;
+    if (prefix_columns > ((int64_t)1 << 31)) return SNAPKV_ERR_UNSUPPORTED;
+    if (max_prefix > prefix_columns * page_size) return SNAPKV_ERR_INVALID_ARG;
+    for (const int32_t* x : {cu_groups, prefix_table, prefix_lens})
+        if ((reinterpret_cast<uintptr_t>(x) & 3u) != 0) return SNAPKV_ERR_MISALIGNED;
+    if (!workspace || workspace_bytes < shared_plan(B, G, Hq, Hkv, D, max_prefix, max_len).bytes) return SNAPKV_ERR_WORKSPACE;
+    if ((reinterpret_cast<uintptr_t>(workspace) & 255u) != 0) return SNAPKV_ERR_MISALIGNED;
+    A.G = G;
+    A.cu = cu_groups;
+    A.prefix_table = prefix_table;
+    A.prefix_lens = prefix_lens;
+    A.prefix_stride = prefix_columns;
+    A.max_prefix = max_prefix;
+    return launch_shared(dtype, cache, D, A, workspace, static_cast<hipStream_t>(stream)) == hipSuccess ? SNAPKV_OK : SNAPKV_ERR_HIP;
 }
 
 void snapkv_release(void) {

@@ -10,6 +10,7 @@
 // time.  The two 16-byte pieces of a unit are the two partners of eight pairs (halves) or four pairs each (interleaved).
 // Fewer than 1024 tokens are shared out by head groups instead, so that a step's few tokens meet more waves.  65319 tokens
 // of 32/32 heads, rotated, queries too, keys twice: 3.8 GB in 735 us, 5.1 TB/s; 8 tokens of 32/8 heads 3.7 us.
+#include "snapkv_sequence.h"
 #include "snapkv_serve.h"
 
 namespace snapkv {
@@ -27,20 +28,6 @@ struct a_f32 {
     typedef __attribute__((ext_vector_type(4))) float piece;
     static constexpr int N = 4;
 };
-
-// Sequences whose end lies at or before token t (cu ascending): t's sequence, or B behind the last.  All lanes look at once, each at
-// the last end of a 64th of those in question, and go on within the first 64th whose end lies behind t: one trip to memory for
-// up to 64 sequences, four for 2^24.  (2^18 sequences of one token each 21 ms with all ends counted, 0.14 so.)
-__device__ __forceinline__ int sequence_of(const int32_t* cu, int B, int t, int lane) {
-    int lo = 0;
-    for (int width = B; width > 0;) {                 // the ends before lo are at or before t, those from lo + width on are not
-        const int w = (width + 63) / 64, last = min((lane + 1) * w, width) - 1;
-        const int k = __popcll(__ballot(lane * w < width && cu[lo + last + 1] <= t));
-        lo += min(k * w, width);
-        width = min(w, width - k * w) - 1;            // (its last end lies behind t)
-    }
-    return lo;
-}
 
 template <typename T, int D, bool INTERLEAVED>
 __global__ __launch_bounds__(256) void append_paged(const AppendArgs A) {

@@ -21,8 +21,15 @@ struct AppendArgs {
     int64_t npos, T;
     int B, Hq, Hkv, page, rot;
     int parts;                                       // waves that share a token's heads
+    // microscaled pages (snapkv_mx.hip): their scale bytes [pages, page, Hkv, D / 32], and where their rows are read to
+    unsigned char *k_scales, *v_scales;
+    char* v_out;                                     // (with k_out)
+    int64_t vo_rs, vo_hs;
 };
 hipError_t launch_append(int dtype, int D, bool interleaved, AppendArgs A, hipStream_t st);
+// cache: 1 e4m3, 2 e2m1 codes.
+hipError_t launch_append_mx(int dtype, int cache, int D, bool interleaved, AppendArgs A, hipStream_t st);
+hipError_t launch_read_mx(int dtype, int cache, int D, AppendArgs A, hipStream_t st);
 
 // Causal attention over packed prompts (snapkv_prompt.hip); strides in bytes.
 struct PromptArgs {
@@ -61,6 +68,37 @@ struct PagedPlan {
 };
 PagedPlan paged_plan(int B, int Hq, int Hkv, int D, int64_t max_len);
 hipError_t launch_paged(int dtype, int D, PagedArgs A, void* workspace, hipStream_t st);
+
+// One new token per sequence over plain or microscaled pages, groups of sequences sharing a prefix (snapkv_shared.hip).
+struct SharedArgs {
+    const char *q, *k, *v;                           // [B, Hq, D]; rows or codes of the pages
+    const unsigned char *k_scales, *v_scales;        // [pages, page, Hkv, D / 32] (microscaled pages)
+    const int32_t *table, *lens;                     // the sequences' own rows: [B, table_stride]; [B]
+    const int32_t *prefix_table, *prefix_lens, *cu;  // [G, prefix_stride]; [G]; [G + 1] or null: one group
+    int64_t table_stride, prefix_stride, pages, max_len, max_prefix;
+    int B, G, Hq, Hkv, g, page;                      // G: 0 without prefixes
+    int nchunk, least, prefix_chunks, prefix_least;  // shares of a sequence or prefix at most, and keys of the shortest
+    int tiles;                                       // places of a prefix's query heads, all groups together
+    int slots;                                       // partials of a query head: the prefix's, then its own
+    int places;                                      // of workgroups, per sequence and KV head
+    bool by_xcd, prefix_by_xcd;                      // how the workgroups of own and of prefixes' shares are dealt out
+    unsigned prefix_groups;                          // workgroups for prefixes, which come first
+    unsigned page_magic;                             // r / page = r * page_magic >> page_shift, r < 2^31
+    int page_shift;
+    float scale2;
+    char* out;                                       // [B, Hq, D]
+    float* lse;                                      // [B, Hq] or null
+    float* part_acc;                                 // [B, Hq, slots, D]
+    float2* part_ml;                                 // [B, Hq, slots]
+};
+struct SharedPlan {
+    int nchunk, least, prefix_chunks, prefix_least, slots;
+    int columns, tiles;                              // query heads of a tile; places of tiles
+    size_t acc_bytes, bytes;                         // of the partial outputs, and of the workspace
+};
+SharedPlan shared_plan(int B, int G, int Hq, int Hkv, int D, int64_t max_prefix, int64_t max_len);
+// cache: 0 pages of the queries' type, 1 e4m3, 2 e2m1 codes.
+hipError_t launch_shared(int dtype, int cache, int D, SharedArgs A, void* workspace, hipStream_t st);
 
 }  // namespace snapkv
 

@@ -1,0 +1,561 @@
+// Attention of one new token per sequence over paged rows, plain or microscaled, of prefixes that groups of sequences share and of
+// the sequences' own.
+//
+//   out[b, h] = sum_j softmax_j(q[b, h] . k_j / sqrt(D)) v_j,   lse[b, h] = log sum_j exp(q[b, h] . k_j / sqrt(D)),
+//
+// j over the rows of the prefix of b's group and then over b's own: one pass with the running maximum and sum of each part, and
+// the parts joined.  A prefix is met by the query heads of all its sequences that read one KV head, as the columns of the same
+// products, so its rows are read once for up to 16 NC of them.  Rows of caches in 8 or 4 bits become bfloat16 numbers
+// (exactly: a code has at most 4 significant bits) between the load and the product; fp16 queries meet them in two bfloat16 parts.
+//
+// MFMA layout (16x16x32): lane l = 16 kg + n supplies row or column n and contraction elements 8 kg .. +7 of an operand; accumulator
+// register r of lane l is row 4 kg + r, column n.  Which element of a head is which contraction element is free, as long as
+// queries and keys agree: a lane has those that lie in its 16-byte loads (element_of).
+//
+//   logits^T = K Q^T, 32 keys a step, 16 after 16: a lane gets keys 4 kg .. +3 of both.  out^T = V^T P^T with P in two parts:
+//     contraction elements 8 kg .. +7 are those keys, so P never moves.  V goes through LDS, its rows' 16-byte pieces permuted,
+//     and comes back by the transposing read (16 lanes read four rows of 16 columns, a lane gets the four of one column).
+#include "snapkv_attn.h"
+#include "snapkv_sequence.h"
+#include "snapkv_serve.h"
+
+#include <algorithm>
+#include <cmath>
+
+namespace snapkv {
+namespace {
+
+constexpr int kWaves = 4;
+
+// Keys of a share of S: whole steps of all waves, so many that nchunk shares hold it, and at least `least`.
+__device__ __forceinline__ int share_of(int S, int nchunk, int least) {
+    const int c = (S + nchunk - 1) / nchunk;
+    return max(least, (c + 127) / 128 * 128);
+}
+__device__ __forceinline__ int clamped(int64_t n, int64_t most) { return (int)(n < 0 ? 0 : (n > most ? most : n)); }
+
+// T: the type of queries and outputs; CACHE 0: pages of that type, 1 e4m3, 2 e2m1 codes.
+template <typename T, int CACHE> struct kind {
+    typedef dec_bf16 mat;                             // of the products
+    typedef __bf16 elem;
+    static constexpr int kQ = 1;                      // parts of a query
+    static constexpr float kShift = 0.f;              // probabilities are taken 2^kShift times as large
+};
+template <> struct kind<dec_f16, 0> {
+    typedef dec_f16 mat;
+    typedef _Float16 elem;
+    static constexpr int kQ = 1;
+    static constexpr float kShift = 15.f;             // (two fp16 parts of one keep 20 bits down to 2^-19 of the largest so)
+};
+template <int CACHE> struct kind<dec_f16, CACHE> {
+    typedef dec_bf16 mat;
+    typedef _Float16 elem;
+    static constexpr int kQ = 2;
+    static constexpr float kShift = 0.f;
+};
+
+// The head's element that is contraction element j of lane group kg in product c.
+template <int CACHE, int D> __device__ __forceinline__ constexpr int element_of(int kg, int c, int j) {
+    return CACHE == 0 ? 32 * c + 8 * kg + j : D / 4 * kg + 8 * c + j;
+}
+
+typedef __attribute__((ext_vector_type(2))) __bf16 dbf16x2;
+
+// A lane's part of a row as it lies in memory, and its operands.
+template <int CACHE, int D> struct Row;
+template <int D> struct Row<0, D> {
+    uint4 w[D / 32];
+    __device__ __forceinline__ void load(const char* base, const unsigned char*, int64_t at, int kg) {
+        const char* p = base + at * (2 * D);
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) w[c] = *reinterpret_cast<const uint4*>(p + (4 * c + kg) * 16);
+    }
+    __device__ __forceinline__ uint4 operand(int c) const { return w[c]; }
+};
+template <int D> struct Row<1, D> {
+    unsigned w[D / 16], s;
+    __device__ __forceinline__ void load(const char* base, const unsigned char* scales, int64_t at, int kg) {
+        const char* p = base + at * D + kg * (D / 4);
+#pragma unroll
+        for (int c = 0; c < D / 64; ++c) {
+            const uint4 x = *reinterpret_cast<const uint4*>(p + 16 * c);
+            w[4 * c] = x.x;
+            w[4 * c + 1] = x.y;
+            w[4 * c + 2] = x.z;
+            w[4 * c + 3] = x.w;
+        }
+        s = scales[at * (D / 32) + kg * (D / 4) / 32];
+    }
+    __device__ __forceinline__ uint4 operand(int c) const {
+        const float u = __uint_as_float(s << 23);
+        return make_uint4(__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * c], u, false)),
+                          __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * c], u, true)),
+                          __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * c + 1], u, false)),
+                          __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * c + 1], u, true)));
+    }
+};
+template <int D> struct Row<2, D> {
+    unsigned w[D / 32], s;
+    __device__ __forceinline__ void load(const char* base, const unsigned char* scales, int64_t at, int kg) {
+        const char* p = base + at * (D / 2) + kg * (D / 8);
+        if constexpr (D == 128) {
+            const uint4 x = *reinterpret_cast<const uint4*>(p);
+            w[0] = x.x;
+            w[1] = x.y;
+            w[2] = x.z;
+            w[3] = x.w;
+        } else {
+            const uint2 x = *reinterpret_cast<const uint2*>(p);
+            w[0] = x.x;
+            w[1] = x.y;
+        }
+        s = scales[at * (D / 32) + kg * (D / 4) / 32];
+    }
+    __device__ __forceinline__ uint4 operand(int c) const {
+        const float u = __uint_as_float(s << 23);
+        return make_uint4(__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[c], u, 0)),
+                          __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[c], u, 1)),
+                          __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[c], u, 2)),
+                          __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[c], u, 3)));
+    }
+};
+
+// Eight of a query's elements as one operand, or the two operands whose sum they are (11 bits: the high part has 8).
+template <typename T, int CACHE> __device__ __forceinline__ void query_operands(uint4 x, uint4* q) {
+    if constexpr (kind<T, CACHE>::kQ == 1) {
+        q[0] = x;
+    } else {
+        const df16x8 h = __builtin_bit_cast(df16x8, x);
+        unsigned hi[4], lo[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) split2(dec_bf16{}, (float)h[2 * i], (float)h[2 * i + 1], hi[i], lo[i]);
+        q[0] = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+        q[1] = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+    }
+}
+
+// What a workgroup has to do: keys begin .. end - 1 of the rows that `table` names, for the query heads row0 .. of rows of them,
+// sequence by sequence from b0 on, that read KV head kvh; its answer is partial `slot` of theirs, or (slot < 0) the whole.
+struct Task {
+    int b0, row0, rows, kvh;
+    const int32_t* table;
+    int begin, end, slot;
+};
+
+// LDS of a workgroup: the waves' values of a step, and behind the loop their sums.
+template <int D> union Shared {
+    char v[kWaves][32 * 2 * D];
+    struct {
+        float acc[kWaves][16][D + 4], m[kWaves][16], l[kWaves][16];
+    } sum;
+};
+typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
+typedef __attribute__((address_space(3))) char* lds_char;
+
+// Which of its row's 16-byte places holds a piece: the rows that a read meets are in different banks, and those that a write does.
+template <int D> __device__ __forceinline__ int place_of(int row, int piece) {
+    return piece ^ (D == 128 ? (row & 3) << 2 | (row >> 2 & 3) : (row & 1) << 2 | (row >> 1 & 3));
+}
+
+template <typename T, int CACHE, int D, int NC>
+__device__ __forceinline__ void attend(const SharedArgs& A, const Task& W, Shared<D>& s) {
+    typedef kind<T, CACHE> K;
+    typedef typename K::mat M;
+    typedef typename K::elem elem;
+    constexpr int NP = D / 32;        // products along a head
+    constexpr int NB = D / 16;        // blocks of 16 output elements
+    constexpr float kShift = K::kShift;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int n16 = lane & 15, kg = lane >> 4;
+    auto head_of = [&](int row) { return ((int64_t)W.b0 + row / A.g) * A.Hq + (int64_t)W.kvh * A.g + row % A.g; };
+
+    uint4 qf[NC][NP][K::kQ];
+#pragma unroll
+    for (int b = 0; b < NC; ++b) {
+        const int row = W.row0 + 16 * b + n16;
+        const char* q = A.q + (row < W.rows ? head_of(row) : 0) * (2 * D);
+#pragma unroll
+        for (int c = 0; c < NP; ++c) {
+            uint4 x = make_uint4(0, 0, 0, 0);
+            if (row < W.rows) x = *reinterpret_cast<const uint4*>(q + 2 * element_of<CACHE, D>(kg, c, 0));
+            query_operands<T, CACHE>(x, qf[b][c]);
+        }
+    }
+    char* const sv = s.v[wave];
+    const int tr = 4 * kg + (n16 >> 2);                // row and place of the lane's first transposing read
+    const unsigned tr_at = tr * (2 * D) + place_of<D>(tr, (n16 & 3) >> 1) * 16 + (n16 & 1) * 8;
+    float m[NC], lsum[NC];
+    dfx4 acc[NC][NB];
+#pragma unroll
+    for (int b = 0; b < NC; ++b) {
+        m[b] = -3.4028235e38f;                         // (finite: logits of -infinity have probability 0 and not NaN)
+        lsum[b] = 0.f;
+#pragma unroll
+        for (int i = 0; i < NB; ++i) acc[b][i] = dfx4{0.f, 0.f, 0.f, 0.f};
+    }
+    auto slot_of = [&](int key) {                      // the pool's row, pages behind each other, head by head
+        const int r = key < W.end ? key : W.end - 1;
+        const int pg = (int)(((uint64_t)(unsigned)r * A.page_magic) >> A.page_shift);
+        int64_t at = W.table[pg];
+        at = at < 0 ? 0 : (at >= A.pages ? A.pages - 1 : at);
+        return (at * A.page + (r - pg * A.page)) * A.Hkv + W.kvh;
+    };
+    constexpr int STEP = 32 * kWaves;
+    for (int key = W.begin + 32 * wave; key < W.end; key += STEP) {
+        const int64_t x = slot_of(key + n16), y = slot_of(key + 16 + n16);
+        Row<CACHE, D> kx, ky, vx, vy;
+        kx.load(A.k, A.k_scales, x, kg);
+        ky.load(A.k, A.k_scales, y, kg);
+        vx.load(A.v, A.v_scales, x, kg);
+        vy.load(A.v, A.v_scales, y, kg);
+        dfx4 sx[NC], sy[NC];
+#pragma unroll
+        for (int b = 0; b < NC; ++b) sx[b] = sy[b] = dfx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int c = 0; c < NP; ++c) {
+            const uint4 ox = kx.operand(c), oy = ky.operand(c);
+#pragma unroll
+            for (int b = 0; b < NC; ++b)
+#pragma unroll
+                for (int i = 0; i < K::kQ; ++i) {
+                    sx[b] = mma(M{}, ox, qf[b][c][i], sx[b]);
+                    sy[b] = mma(M{}, oy, qf[b][c][i], sy[b]);
+                }
+        }
+        uint4 ph[NC], pl[NC];
+        const int k0 = key + 4 * kg;
+#pragma unroll
+        for (int b = 0; b < NC; ++b) {
+            float e[8], tmax = -INFINITY;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                e[r] = k0 + r < W.end ? sx[b][r] * A.scale2 : -INFINITY;
+                e[4 + r] = k0 + 16 + r < W.end ? sy[b][r] * A.scale2 : -INFINITY;
+                tmax = fmaxf(tmax, fmaxf(e[r], e[4 + r]));
+            }
+            tmax = fmaxf(tmax, __shfl_xor(tmax, 16));
+            tmax = fmaxf(tmax, __shfl_xor(tmax, 32));
+            const float mn = fmaxf(m[b], tmax);
+            const float alpha = __builtin_amdgcn_exp2f(m[b] - mn);
+            m[b] = mn;
+            const float least = mn - kShift;
+            float psum = 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                e[j] = __builtin_amdgcn_exp2f(e[j] - least);
+                psum += e[j];
+            }
+            lsum[b] = lsum[b] * alpha + psum;
+            split2(M{}, e[0], e[1], ph[b].x, pl[b].x);
+            split2(M{}, e[2], e[3], ph[b].y, pl[b].y);
+            split2(M{}, e[4], e[5], ph[b].z, pl[b].z);
+            split2(M{}, e[6], e[7], ph[b].w, pl[b].w);
+#pragma unroll
+            for (int i = 0; i < NB; ++i) acc[b][i] *= alpha;
+        }
+#pragma unroll
+        for (int c = 0; c < NP; ++c) {
+            const int piece = element_of<CACHE, D>(kg, c, 0) / 8;
+            *reinterpret_cast<uint4*>(sv + n16 * (2 * D) + place_of<D>(n16, piece) * 16) = vx.operand(c);
+            *reinterpret_cast<uint4*>(sv + (16 + n16) * (2 * D) + place_of<D>(n16, piece) * 16) = vy.operand(c);
+        }
+        asm volatile("" ::: "memory");                 // (a wave's LDS operations are done in order)
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+            const lds_char at = (lds_char)sv + (tr_at ^ (unsigned)(i * 32));
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)at);
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(at + 16 * 2 * D));
+            const uint4 vt = __builtin_bit_cast(uint4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+            for (int b = 0; b < NC; ++b) {
+                acc[b][i] = mma(M{}, vt, ph[b], acc[b][i]);
+                acc[b][i] = mma(M{}, vt, pl[b], acc[b][i]);
+            }
+        }
+        asm volatile("" ::: "memory");
+    }
+    __syncthreads();                                   // (all waves have read their values)
+    constexpr int DT = D / 16;
+    const int qi = tid >> 4, d0 = (tid & 15) * DT;
+#pragma unroll
+    for (int b = 0; b < NC; ++b) {
+        if (b > 0) __syncthreads();                    // (the waves have read the block before)
+        lsum[b] += __shfl_xor(lsum[b], 16);
+        lsum[b] += __shfl_xor(lsum[b], 32);
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+            *reinterpret_cast<float4*>(&s.sum.acc[wave][n16][16 * i + 4 * kg]) = make_float4(acc[b][i][0], acc[b][i][1], acc[b][i][2], acc[b][i][3]);
+        if (kg == 0) {
+            s.sum.m[wave][n16] = m[b];
+            s.sum.l[wave][n16] = lsum[b];
+        }
+        __syncthreads();
+        const int row = W.row0 + 16 * b + qi;
+        if (row >= W.rows) continue;
+        float most = s.sum.m[0][qi];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) most = fmaxf(most, s.sum.m[w][qi]);
+        float Lq = 0.f, o[DT];
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[d] = 0.f;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const float f = __builtin_amdgcn_exp2f(s.sum.m[w][qi] - most);
+            Lq += s.sum.l[w][qi] * f;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[d] += s.sum.acc[w][qi][d0 + d] * f;
+        }
+        const int64_t hq = head_of(row);
+        if (W.slot < 0) {
+            const float inv = Lq == 0.f ? 0.f : 1.f / Lq;      // (no rows; a sum that is NaN makes the row's answer NaN)
+            elem* out = reinterpret_cast<elem*>(A.out) + hq * D + d0;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) out[d] = (elem)(o[d] * inv);
+            if (A.lse && (tid & 15) == 0)
+                A.lse[hq] = Lq == 0.f ? -INFINITY : (most - kShift + __builtin_amdgcn_logf(Lq)) * 0.6931471805599453f;
+        } else {
+            float* pa = A.part_acc + (hq * A.slots + W.slot) * D + d0;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) pa[d] = o[d];
+            if ((tid & 15) == 0) A.part_ml[hq * A.slots + W.slot] = make_float2(most, Lq);
+        }
+    }
+}
+
+// The share of a sequence's own rows that workgroup i of those for them takes; false: none.
+template <bool SHARED> __device__ __forceinline__ bool own_task(const SharedArgs& A, unsigned i, Task& W) {
+    // A share's heads run on one XCD (workgroup i runs on XCD i % 8), which then reads whole lines of all heads; a sequence has
+    // an odd number of places, so that the first shares, which are all that short sequences have, do not meet on a few XCDs.
+    W.kvh = i % A.Hkv;
+    int chunk = i / A.Hkv;
+    if (A.by_xcd) {
+        W.kvh = i / 8 % A.Hkv;
+        chunk = i / (8 * A.Hkv) * 8 + i % 8;
+    }
+    W.b0 = chunk / A.places;
+    chunk %= A.places;
+    if (chunk >= A.nchunk || W.b0 >= A.B) return false;
+    const int S = clamped(A.lens[W.b0], A.max_len);
+    const int share = share_of(S, A.nchunk, A.least);
+    W.begin = chunk * share;
+    if (W.begin >= S && (SHARED || chunk > 0)) return false;
+    W.end = W.begin + share < S ? W.begin + share : S;
+    W.row0 = 0;
+    W.rows = A.g;
+    W.table = A.table + (int64_t)W.b0 * A.table_stride;
+    W.slot = !SHARED && S <= share ? -1 : A.prefix_chunks + chunk;
+    return true;
+}
+
+// The share of a prefix and the tile of its query heads that workgroup i of those for prefixes takes.  Group i's tiles have the places
+// from first(i) = i + floor(cu[i] g / R) on, R query heads a tile: rows / R rounded up is at most one more than the difference
+// of the floors, so nobody counts through the groups before.
+template <int R> __device__ __forceinline__ bool prefix_task(const SharedArgs& A, unsigned i, int lane, Task& W) {
+    // the tiles of a share run together, and on one XCD where there are shares for all
+    const unsigned units = (unsigned)A.Hkv * A.tiles;
+    int chunk = i / units;
+    unsigned j = i % units;
+    if (A.prefix_by_xcd) {
+        chunk = i / (8 * units) * 8 + i % 8;
+        j = i / 8 % units;
+    }
+    const int tile = j % A.tiles;
+    W.kvh = j / A.tiles;
+    if (chunk >= A.prefix_chunks) return false;
+    auto at = [&](int i) { return A.cu ? clamped(A.cu[i], A.B) : (i == 0 ? 0 : A.B); };
+    auto first = [&](int i) { return i + (int)((int64_t)at(i) * A.g / R); };
+    int lo = 0;                                        // the last group whose places begin at or before the tile's
+    for (int width = A.G; width > 1;) {                // (it is among lo .. lo + width - 1)
+        const int w = (width + 63) / 64;
+        const int k = __popcll(__ballot(lane * w < width && first(lo + lane * w) <= tile));
+        const int n = k > 0 ? k - 1 : 0;
+        lo += n * w;
+        width = min(w, width - n * w);
+    }
+    W.b0 = at(lo);
+    W.rows = (at(lo + 1) - W.b0) * A.g;
+    W.row0 = (tile - first(lo)) * R;
+    if (W.row0 < 0 || W.row0 >= W.rows) return false;
+    const int P = clamped(A.prefix_lens[lo], A.max_prefix);
+    const int share = share_of(P, A.prefix_chunks, A.prefix_least);
+    W.begin = chunk * share;
+    if (W.begin >= P) return false;
+    W.end = W.begin + share < P ? W.begin + share : P;
+    W.table = A.prefix_table + (int64_t)lo * A.prefix_stride;
+    W.slot = chunk;
+    return true;
+}
+
+template <typename T, int CACHE, int D>
+__global__ __launch_bounds__(kWaves * 64) void cached_attn(const SharedArgs A) {
+    __shared__ __align__(256) Shared<D> s;
+    Task W;
+    if (own_task<false>(A, blockIdx.x, W)) attend<T, CACHE, D, 1>(A, W, s);
+}
+
+template <typename T, int CACHE, int D, int NC>
+__global__ __launch_bounds__(kWaves * 64) void shared_attn(const SharedArgs A) {
+    __shared__ __align__(256) Shared<D> s;
+    Task W;
+    if (blockIdx.x >= A.prefix_groups) {
+        if (own_task<true>(A, blockIdx.x - A.prefix_groups, W)) attend<T, CACHE, D, 1>(A, W, s);
+    } else if (prefix_task<16 * NC>(A, blockIdx.x, threadIdx.x & 63, W)) {
+        attend<T, CACHE, D, NC>(A, W, s);
+    }
+}
+
+// Joins the partials of a query head: a workgroup for each, its waves a quarter of them, eight outputs in flight at a time.
+template <typename T, int CACHE, int D, bool SHARED>
+__global__ __launch_bounds__(kWaves * 64) void cached_join(const SharedArgs A) {
+    typedef typename kind<T, CACHE>::elem elem;
+    constexpr int E = D / 64, BATCH = 8;
+    constexpr float kShift = kind<T, CACHE>::kShift;
+    const int64_t hq = blockIdx.x;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, b = (int)(hq / A.Hq);
+    const int S = clamped(A.lens[b], A.max_len);
+    const int share = share_of(S, A.nchunk, A.least);
+    int n = (S + share - 1) / share, before = 0;
+    if (SHARED) {
+        int G = 0;                                     // b's group
+        bool in = true;
+        if (A.cu) {
+            G = sequence_of(A.cu, A.G, b, lane);
+            in = G < A.G && A.cu[G] <= b;              // (before the first and behind the last: none)
+        }
+        if (in) {
+            const int P = clamped(A.prefix_lens[G], A.max_prefix);
+            const int ps = share_of(P, A.prefix_chunks, A.prefix_least);
+            before = (P + ps - 1) / ps;
+        }
+        n += before;
+    } else if (n <= 1) {
+        return;
+    }
+    auto slot = [&](int i) { return i < before ? i : A.prefix_chunks + (i - before); };
+    const float2* ml = A.part_ml + hq * A.slots;
+    const float* pa = A.part_acc + hq * A.slots * D + lane * E;
+    float M = -3.4028235e38f;
+    for (int i = lane; i < n; i += 64) M = fmaxf(M, ml[slot(i)].x);
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) M = fmaxf(M, __shfl_xor(M, d));
+    float Lq = 0.f, o[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) o[e] = 0.f;
+    for (int i0 = wave * BATCH; i0 < n; i0 += kWaves * BATCH) {
+        float2 p[BATCH];
+        float x[BATCH][E];
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            const int64_t c = slot(i0 + i < n ? i0 + i : n - 1);
+            p[i] = ml[c];
+#pragma unroll
+            for (int e = 0; e < E; ++e) x[i][e] = pa[c * D + e];
+        }
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            if (i0 + i >= n) break;
+            const float f = __builtin_amdgcn_exp2f(p[i].x - M);
+            Lq += p[i].y * f;
+#pragma unroll
+            for (int e = 0; e < E; ++e) o[e] += x[i][e] * f;
+        }
+    }
+    __shared__ float s_o[kWaves][D], s_l[kWaves];
+#pragma unroll
+    for (int e = 0; e < E; ++e) s_o[wave][lane * E + e] = o[e];
+    if (lane == 0) s_l[wave] = Lq;
+    __syncthreads();
+    Lq = s_l[0] + s_l[1] + s_l[2] + s_l[3];
+    if (threadIdx.x < D) {
+        const int d = threadIdx.x;
+        const float y = s_o[0][d] + s_o[1][d] + s_o[2][d] + s_o[3][d];
+        reinterpret_cast<elem*>(A.out)[hq * D + d] = (elem)(Lq == 0.f ? 0.f : y / Lq);
+    }
+    if (A.lse && threadIdx.x == 0) A.lse[hq] = Lq == 0.f ? -INFINITY : (M - kShift + __builtin_amdgcn_logf(Lq)) * 0.6931471805599453f;
+}
+
+}  // namespace
+
+// Shares of a sequence's own rows: as many as give 1024 workgroups if all sequences are as long as they may be, of 128 to 1024 keys (512 where
+// even those give 2048 workgroups), but no more than give 16384 workgroups, or seven; a sequence of up to 512 rows is not cut.  Shares of a prefix: as
+// many as give 1024 workgroups with all tiles and KV heads, of 128 keys at least, no more than 256.
+SharedPlan shared_plan(int B, int G, int Hq, int Hkv, int D, int64_t max_prefix, int64_t max_len) {
+    SharedPlan P{};
+    const int g = Hq / Hkv;
+    const int64_t pairs = (int64_t)B * Hkv, keys = pairs * max_len;
+    int64_t chunk = std::max<int64_t>(128, (keys / 1024 + 127) / 128 * 128);
+    chunk = std::min<int64_t>(chunk, keys >= 2048 * 1024 ? 512 : 1024);
+    if (max_len <= 512) chunk = 512;
+    P.nchunk = (int)std::min((max_len + chunk - 1) / chunk, std::max<int64_t>(7, 16384 / pairs));
+    P.least = P.nchunk == 1 || pairs > 128 ? 512 : (pairs > 64 ? 256 : 128);
+    if (G > 0) {
+        const int64_t rows = ((int64_t)B * g + G - 1) / G;    // of a group, on the average
+        P.columns = rows <= 16 ? 16 : (rows <= 32 ? 32 : 64);
+        P.tiles = (int)(G + (int64_t)B * g / P.columns);
+        const int64_t units = (int64_t)P.tiles * Hkv;
+        P.prefix_chunks = (int)std::max<int64_t>(1, std::min<int64_t>({256, (max_prefix + 127) / 128, (1024 + units - 1) / units}));
+        P.prefix_least = 128;
+    }
+    P.slots = P.prefix_chunks + P.nchunk;
+    const size_t heads = (size_t)B * Hq;
+    P.acc_bytes = (heads * P.slots * D * sizeof(float) + 255) & ~(size_t)255;
+    P.bytes = P.slots <= 1 ? 0 : P.acc_bytes + heads * P.slots * sizeof(float2);
+    return P;
+}
+
+hipError_t launch_shared(int dtype, int cache, int D, SharedArgs A, void* workspace, hipStream_t st) {
+    const SharedPlan P = shared_plan(A.B, A.G, A.Hq, A.Hkv, D, A.max_prefix, A.max_len);
+    A.nchunk = P.nchunk;
+    A.least = P.least;
+    A.prefix_chunks = P.prefix_chunks;
+    A.prefix_least = P.prefix_least;
+    A.tiles = P.tiles;
+    A.slots = P.slots;
+    // r / page for 0 <= r < 2^31: with 2^(l-1) < page <= 2^l, ceil(2^(31+l) / page) fits 32 bits and its product's error stays
+    // below one part in r (page 1: 2^31 and a shift by 31)
+    int l = 0;
+    while (l < 31 && (1ll << l) < A.page) ++l;
+    A.page_magic = (unsigned)(((1ull << (31 + l)) + A.page - 1) / A.page);
+    A.page_shift = 31 + l;
+    A.scale2 = (float)(1.4426950408889634 / std::sqrt((double)D));
+    A.part_acc = static_cast<float*>(workspace);
+    A.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + P.acc_bytes);
+    A.by_xcd = (int64_t)P.nchunk * A.B >= 8;
+    A.places = A.by_xcd ? P.nchunk | 1 : P.nchunk;
+    int64_t units = (int64_t)A.places * A.B;
+    if (A.by_xcd) units = (units + 7) / 8 * 8;
+    A.prefix_by_xcd = P.prefix_chunks >= 8;
+    A.prefix_groups = (unsigned)((A.prefix_by_xcd ? (P.prefix_chunks + 7) / 8 * 8 : P.prefix_chunks) * (int64_t)P.tiles * A.Hkv);
+    const dim3 grid((unsigned)(A.prefix_groups + units * A.Hkv)), block(kWaves * 64), heads((unsigned)((int64_t)A.B * A.Hq));
+    auto form = [&](auto t, auto c, auto d) {
+        typedef decltype(t) T;
+        constexpr int C = decltype(c)::value, DD = decltype(d)::value;
+        if (A.G == 0) {
+            if constexpr (C != 0) {
+                hipLaunchKernelGGL((cached_attn<T, C, DD>), grid, block, 0, st, A);
+                if (P.slots > 1) hipLaunchKernelGGL((cached_join<T, C, DD, false>), heads, block, 0, st, A);
+            }
+            return;
+        }
+        if (P.columns == 16) hipLaunchKernelGGL((shared_attn<T, C, DD, 1>), grid, block, 0, st, A);
+        else if (P.columns == 32) hipLaunchKernelGGL((shared_attn<T, C, DD, 2>), grid, block, 0, st, A);
+        else hipLaunchKernelGGL((shared_attn<T, C, DD, 4>), grid, block, 0, st, A);
+        hipLaunchKernelGGL((cached_join<T, C, DD, true>), heads, block, 0, st, A);
+    };
+    auto of = [&](auto t, auto c) {
+        if (D == 128) form(t, c, std::integral_constant<int, 128>{});
+        else form(t, c, std::integral_constant<int, 64>{});
+    };
+    auto with = [&](auto t) {
+        if (cache == 0) of(t, std::integral_constant<int, 0>{});
+        else if (cache == 1) of(t, std::integral_constant<int, 1>{});
+        else of(t, std::integral_constant<int, 2>{});
+    };
+    if (dtype == 0) with(dec_bf16{});
+    else if (dtype == 2) with(dec_f16{});
+    else return hipErrorInvalidValue;
+    return hipGetLastError();
+}
+
+}  // namespace snapkv
