@@ -83,8 +83,8 @@ struct SharedArgs {
     int places;                                      // of workgroups, per sequence and KV head
     bool by_xcd, prefix_by_xcd;                      // how the workgroups of own and of prefixes' shares are dealt out
     unsigned prefix_groups;                          // workgroups for prefixes, which come first
-    unsigned page_magic;                             // r / page = r * page_magic >> page_shift, r < 2^31
-    int page_shift;
+    unsigned page_magic;                             // r / page = (2 r * page_magic >> 32) >> page_shift, r < 2^31
+    int page_shift, last_page;
     float scale2;
     char* out;                                       // [B, Hq, D]
     float* lse;                                      // [B, Hq] or null

@@ -39,19 +39,21 @@ template <typename T, int CACHE> struct kind {
     typedef dec_bf16 mat;                             // of the products
     typedef __bf16 elem;
     static constexpr int kQ = 1;                      // parts of a query
-    static constexpr float kShift = 0.f;              // probabilities are taken 2^kShift times as large
+    // Probabilities are taken 2^kShift times as large, and relative to a maximum that is moved, and the sums with it, once it is outgrown by
+    // 2^kGrowth.
+    static constexpr float kShift = 0.f, kGrowth = 8.f;
 };
 template <> struct kind<dec_f16, 0> {
     typedef dec_f16 mat;
     typedef _Float16 elem;
     static constexpr int kQ = 1;
-    static constexpr float kShift = 15.f;             // (two fp16 parts of one keep 20 bits down to 2^-19 of the largest so)
+    static constexpr float kShift = 15.f, kGrowth = 0.f;   // (two fp16 parts of one keep 20 bits down to 2^-19 of the largest so)
 };
 template <int CACHE> struct kind<dec_f16, CACHE> {
     typedef dec_bf16 mat;
     typedef _Float16 elem;
     static constexpr int kQ = 2;
-    static constexpr float kShift = 0.f;
+    static constexpr float kShift = 0.f, kGrowth = 8.f;
 };
 
 // The head's element that is contraction element j of lane group kg in product c.
@@ -65,26 +67,25 @@ typedef __attribute__((ext_vector_type(2))) __bf16 dbf16x2;
 template <int CACHE, int D> struct Row;
 template <int D> struct Row<0, D> {
     uint4 w[D / 32];
-    __device__ __forceinline__ void load(const char* base, const unsigned char*, int64_t at, int kg) {
-        const char* p = base + at * (2 * D);
+    // base, scales: the lane's part of the pool's first row; at: the row's place in bytes.
+    __device__ __forceinline__ void load(const char* base, const unsigned char*, int64_t at) {
 #pragma unroll
-        for (int c = 0; c < D / 32; ++c) w[c] = *reinterpret_cast<const uint4*>(p + (4 * c + kg) * 16);
+        for (int c = 0; c < D / 32; ++c) w[c] = *reinterpret_cast<const uint4*>(base + at + 64 * c);
     }
     __device__ __forceinline__ uint4 operand(int c) const { return w[c]; }
 };
 template <int D> struct Row<1, D> {
     unsigned w[D / 16], s;
-    __device__ __forceinline__ void load(const char* base, const unsigned char* scales, int64_t at, int kg) {
-        const char* p = base + at * D + kg * (D / 4);
+    __device__ __forceinline__ void load(const char* base, const unsigned char* scales, int64_t at) {
 #pragma unroll
         for (int c = 0; c < D / 64; ++c) {
-            const uint4 x = *reinterpret_cast<const uint4*>(p + 16 * c);
+            const uint4 x = *reinterpret_cast<const uint4*>(base + at + 16 * c);
             w[4 * c] = x.x;
             w[4 * c + 1] = x.y;
             w[4 * c + 2] = x.z;
             w[4 * c + 3] = x.w;
         }
-        s = scales[at * (D / 32) + kg * (D / 4) / 32];
+        s = scales[at >> 5];
     }
     __device__ __forceinline__ uint4 operand(int c) const {
         const float u = __uint_as_float(s << 23);
@@ -96,20 +97,19 @@ template <int D> struct Row<1, D> {
 };
 template <int D> struct Row<2, D> {
     unsigned w[D / 32], s;
-    __device__ __forceinline__ void load(const char* base, const unsigned char* scales, int64_t at, int kg) {
-        const char* p = base + at * (D / 2) + kg * (D / 8);
+    __device__ __forceinline__ void load(const char* base, const unsigned char* scales, int64_t at) {
         if constexpr (D == 128) {
-            const uint4 x = *reinterpret_cast<const uint4*>(p);
+            const uint4 x = *reinterpret_cast<const uint4*>(base + at);
             w[0] = x.x;
             w[1] = x.y;
             w[2] = x.z;
             w[3] = x.w;
         } else {
-            const uint2 x = *reinterpret_cast<const uint2*>(p);
+            const uint2 x = *reinterpret_cast<const uint2*>(base + at);
             w[0] = x.x;
             w[1] = x.y;
         }
-        s = scales[at * (D / 32) + kg * (D / 4) / 32];
+        s = scales[at >> 4];
     }
     __device__ __forceinline__ uint4 operand(int c) const {
         const float u = __uint_as_float(s << 23);
@@ -158,6 +158,14 @@ template <int D> __device__ __forceinline__ int place_of(int row, int piece) {
     return piece ^ (D == 128 ? (row & 3) << 2 | (row >> 2 & 3) : (row & 1) << 2 | (row >> 1 & 3));
 }
 
+// The largest x of the four lanes that have a query's keys.
+__device__ __forceinline__ float across_groups(float x) {
+    const auto y = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    x = fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
+    const auto z = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(z[0]), __uint_as_float(z[1]));
+}
+
 template <typename T, int CACHE, int D, int NC>
 __device__ __forceinline__ void attend(const SharedArgs& A, const Task& W, Shared<D>& s) {
     typedef kind<T, CACHE> K;
@@ -166,7 +174,7 @@ __device__ __forceinline__ void attend(const SharedArgs& A, const Task& W, Share
     constexpr int NP = D / 32;        // products along a head
     constexpr int NB = D / 16;        // blocks of 16 output elements
     constexpr float kShift = K::kShift;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n16 = lane & 15, kg = lane >> 4;
     auto head_of = [&](int row) { return ((int64_t)W.b0 + row / A.g) * A.Hq + (int64_t)W.kvh * A.g + row % A.g; };
 
@@ -194,21 +202,46 @@ __device__ __forceinline__ void attend(const SharedArgs& A, const Task& W, Share
 #pragma unroll
         for (int i = 0; i < NB; ++i) acc[b][i] = dfx4{0.f, 0.f, 0.f, 0.f};
     }
-    auto slot_of = [&](int key) {                      // the pool's row, pages behind each other, head by head
-        const int r = key < W.end ? key : W.end - 1;
-        const int pg = (int)(((uint64_t)(unsigned)r * A.page_magic) >> A.page_shift);
-        int64_t at = W.table[pg];
-        at = at < 0 ? 0 : (at >= A.pages ? A.pages - 1 : at);
-        return (at * A.page + (r - pg * A.page)) * A.Hkv + W.kvh;
+    // Where a key's row lies, in bytes of codes or rows (a row's scales lie as many 32nds or 16ths of that behind theirs); its page is
+    // looked up one step before.
+    constexpr int ROW = CACHE == 0 ? 2 * D : (CACHE == 1 ? D : D / 2);
+    const unsigned token = (unsigned)A.Hkv * ROW;      // bytes between the rows of a page
+    const uint64_t page_bytes = (uint64_t)token * (unsigned)A.page;
+    const int lane_at = W.kvh * ROW + kg * (CACHE == 0 ? 16 : ROW / 4), scale_at = W.kvh * (D / 32) + kg * (D / 4) / 32;
+    const char *kb = A.k + lane_at, *vb = A.v + lane_at;
+    const unsigned char *ks = CACHE ? A.k_scales + scale_at : nullptr, *vs = CACHE ? A.v_scales + scale_at : nullptr;
+    struct Place {
+        int entry, line;                               // of the table, and row within the page
+    };
+    auto look_up = [&](int key) {
+        const int r = min(key, W.end - 1);             // (behind the end: the last row again)
+        const int pg = (int)(__umulhi((unsigned)r << 1, A.page_magic) >> A.page_shift);
+        return Place{W.table[pg], r - pg * A.page};
+    };
+    auto place = [&](const Place& p) {
+        const unsigned at = (unsigned)min(max(p.entry, 0), A.last_page);
+        return (int64_t)(at * page_bytes + (uint64_t)token * (unsigned)p.line);
     };
     constexpr int STEP = 32 * kWaves;
-    for (int key = W.begin + 32 * wave; key < W.end; key += STEP) {
-        const int64_t x = slot_of(key + n16), y = slot_of(key + 16 + n16);
-        Row<CACHE, D> kx, ky, vx, vy;
-        kx.load(A.k, A.k_scales, x, kg);
-        ky.load(A.k, A.k_scales, y, kg);
-        vx.load(A.v, A.v_scales, x, kg);
-        vy.load(A.v, A.v_scales, y, kg);
+    const float rest = K::kGrowth / A.scale2;
+    int key = W.begin + 32 * wave;
+    Row<CACHE, D> kx, ky, vx, vy;
+    Place px{}, py{};
+    if (key < W.end) {
+        px = look_up(key + n16);
+        py = look_up(key + 16 + n16);
+        const int64_t x = place(px), y = place(py);
+        kx.load(kb, ks, x);
+        ky.load(kb, ks, y);
+        vx.load(vb, vs, x);
+        vy.load(vb, vs, y);
+        px = look_up(key + STEP + n16);
+        py = look_up(key + STEP + 16 + n16);
+    }
+    for (; key < W.end; key += STEP) {
+        const int64_t x = place(px), y = place(py);    // of the next step
+        px = look_up(key + 2 * STEP + n16);
+        py = look_up(key + 2 * STEP + 16 + n16);
         dfx4 sx[NC], sy[NC];
 #pragma unroll
         for (int b = 0; b < NC; ++b) sx[b] = sy[b] = dfx4{0.f, 0.f, 0.f, 0.f};
@@ -223,43 +256,68 @@ __device__ __forceinline__ void attend(const SharedArgs& A, const Task& W, Share
                     sy[b] = mma(M{}, oy, qf[b][c][i], sy[b]);
                 }
         }
-        uint4 ph[NC], pl[NC];
-        const int k0 = key + 4 * kg;
+        __builtin_amdgcn_sched_barrier(0);             // (the next keys come into these registers)
+        kx.load(kb, ks, x);
+        ky.load(kb, ks, y);
+        __builtin_amdgcn_sched_barrier(0);
+        if (key + 32 > W.end) {                        // the last step
+            const int k0 = key + 4 * kg;
+#pragma unroll
+            for (int b = 0; b < NC; ++b)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    sx[b][r] = k0 + r < W.end ? sx[b][r] : -INFINITY;
+                    sy[b][r] = k0 + 16 + r < W.end ? sy[b][r] : -INFINITY;
+                }
+        }
+        // m: in units of the logits before their scaling
+        bool grown = false;
+        float top[NC];
 #pragma unroll
         for (int b = 0; b < NC; ++b) {
-            float e[8], tmax = -INFINITY;
+            top[b] = fmaxf(fmaxf(fmaxf(sx[b][0], sx[b][1]), fmaxf(sx[b][2], sx[b][3])), fmaxf(fmaxf(sy[b][0], sy[b][1]), fmaxf(sy[b][2], sy[b][3])));
+            grown |= top[b] > m[b] + rest;
+        }
+        if (__any(grown)) {
+#pragma unroll
+            for (int b = 0; b < NC; ++b) {
+                const float mn = fmaxf(m[b], across_groups(top[b]));
+                const float alpha = __builtin_amdgcn_exp2f((m[b] - mn) * A.scale2);
+                m[b] = mn;
+                lsum[b] *= alpha;
+#pragma unroll
+                for (int i = 0; i < NB; ++i) acc[b][i] *= alpha;
+            }
+        }
+        uint4 ph[NC], pl[NC];
+#pragma unroll
+        for (int b = 0; b < NC; ++b) {
+            const float shift = kShift - m[b] * A.scale2;
+            float e[8], sum[2];
 #pragma unroll
             for (int r = 0; r < 4; ++r) {
-                e[r] = k0 + r < W.end ? sx[b][r] * A.scale2 : -INFINITY;
-                e[4 + r] = k0 + 16 + r < W.end ? sy[b][r] * A.scale2 : -INFINITY;
-                tmax = fmaxf(tmax, fmaxf(e[r], e[4 + r]));
+                e[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(sx[b][r], A.scale2, shift));
+                e[4 + r] = __builtin_amdgcn_exp2f(__builtin_fmaf(sy[b][r], A.scale2, shift));
             }
-            tmax = fmaxf(tmax, __shfl_xor(tmax, 16));
-            tmax = fmaxf(tmax, __shfl_xor(tmax, 32));
-            const float mn = fmaxf(m[b], tmax);
-            const float alpha = __builtin_amdgcn_exp2f(m[b] - mn);
-            m[b] = mn;
-            const float least = mn - kShift;
-            float psum = 0.f;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                e[j] = __builtin_amdgcn_exp2f(e[j] - least);
-                psum += e[j];
-            }
-            lsum[b] = lsum[b] * alpha + psum;
+            sum[0] = e[0] + e[4];
+            sum[1] = e[1] + e[5];
+            sum[0] += e[2] + e[6];
+            sum[1] += e[3] + e[7];
+            lsum[b] += sum[0] + sum[1];
             split2(M{}, e[0], e[1], ph[b].x, pl[b].x);
             split2(M{}, e[2], e[3], ph[b].y, pl[b].y);
             split2(M{}, e[4], e[5], ph[b].z, pl[b].z);
             split2(M{}, e[6], e[7], ph[b].w, pl[b].w);
-#pragma unroll
-            for (int i = 0; i < NB; ++i) acc[b][i] *= alpha;
         }
 #pragma unroll
         for (int c = 0; c < NP; ++c) {
-            const int piece = element_of<CACHE, D>(kg, c, 0) / 8;
-            *reinterpret_cast<uint4*>(sv + n16 * (2 * D) + place_of<D>(n16, piece) * 16) = vx.operand(c);
-            *reinterpret_cast<uint4*>(sv + (16 + n16) * (2 * D) + place_of<D>(n16, piece) * 16) = vy.operand(c);
+            const int to = n16 * (2 * D) + place_of<D>(n16, element_of<CACHE, D>(kg, c, 0) / 8) * 16;
+            *reinterpret_cast<uint4*>(sv + to) = vx.operand(c);
+            *reinterpret_cast<uint4*>(sv + 16 * (2 * D) + to) = vy.operand(c);
         }
+        __builtin_amdgcn_sched_barrier(0);             // (as the next values)
+        vx.load(vb, vs, x);
+        vy.load(vb, vs, y);
         asm volatile("" ::: "memory");                 // (a wave's LDS operations are done in order)
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
@@ -275,6 +333,8 @@ __device__ __forceinline__ void attend(const SharedArgs& A, const Task& W, Share
         }
         asm volatile("" ::: "memory");
     }
+#pragma unroll
+    for (int b = 0; b < NC; ++b) m[b] *= A.scale2;     // (what saw no keys: the lowest number, or -infinity)
     __syncthreads();                                   // (all waves have read their values)
     constexpr int DT = D / 16;
     const int qi = tid >> 4, d0 = (tid & 15) * DT;
@@ -373,6 +433,7 @@ template <int R> __device__ __forceinline__ bool prefix_task(const SharedArgs& A
         lo += n * w;
         width = min(w, width - n * w);
     }
+    lo = __builtin_amdgcn_readfirstlane(lo);
     W.b0 = at(lo);
     W.rows = (at(lo + 1) - W.b0) * A.g;
     W.row0 = (tile - first(lo)) * R;
@@ -388,14 +449,14 @@ template <int R> __device__ __forceinline__ bool prefix_task(const SharedArgs& A
 }
 
 template <typename T, int CACHE, int D>
-__global__ __launch_bounds__(kWaves * 64) void cached_attn(const SharedArgs A) {
+__global__ __launch_bounds__(kWaves * 64, D == 64 ? 4 : 3) void cached_attn(const SharedArgs A) {
     __shared__ __align__(256) Shared<D> s;
     Task W;
     if (own_task<false>(A, blockIdx.x, W)) attend<T, CACHE, D, 1>(A, W, s);
 }
 
 template <typename T, int CACHE, int D, int NC>
-__global__ __launch_bounds__(kWaves * 64) void shared_attn(const SharedArgs A) {
+__global__ __launch_bounds__(kWaves * 64, NC == 1 ? (D == 64 ? 4 : 3) : (NC == 2 || D == 64 ? 2 : 1)) void shared_attn(const SharedArgs A) {
     __shared__ __align__(256) Shared<D> s;
     Task W;
     if (blockIdx.x >= A.prefix_groups) {
@@ -513,11 +574,12 @@ hipError_t launch_shared(int dtype, int cache, int D, SharedArgs A, void* worksp
     A.tiles = P.tiles;
     A.slots = P.slots;
     // r / page for 0 <= r < 2^31: with 2^(l-1) < page <= 2^l, ceil(2^(31+l) / page) fits 32 bits and its product's error stays
-    // below one part in r (page 1: 2^31 and a shift by 31)
+    // below one part in r; 2 r times that is shifted by 32 and l
     int l = 0;
     while (l < 31 && (1ll << l) < A.page) ++l;
     A.page_magic = (unsigned)(((1ull << (31 + l)) + A.page - 1) / A.page);
-    A.page_shift = 31 + l;
+    A.page_shift = l;
+    A.last_page = (int)(A.pages - 1);
     A.scale2 = (float)(1.4426950408889634 / std::sqrt((double)D));
     A.part_acc = static_cast<float*>(workspace);
     A.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + P.acc_bytes);
