@@ -21,6 +21,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 namespace snapkv {
 namespace {
@@ -63,6 +64,21 @@ template <int CACHE, int D> __device__ __forceinline__ constexpr int element_of(
 
 typedef __attribute__((ext_vector_type(2))) __bf16 dbf16x2;
 
+// Eight values of codes (8 bits: two words, 4 bits: one) under a scale byte, as bfloat16 numbers.
+template <int CACHE> __device__ __forceinline__ uint4 values_of(const unsigned* w, unsigned s) {
+    const float u = __uint_as_float(s << 23);
+    if constexpr (CACHE == 1)
+        return make_uint4(__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[0], u, false)),
+                          __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[0], u, true)),
+                          __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[1], u, false)),
+                          __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[1], u, true)));
+    else
+        return make_uint4(__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[0], u, 0)),
+                          __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[0], u, 1)),
+                          __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[0], u, 2)),
+                          __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[0], u, 3)));
+}
+
 // A lane's part of a row as it lies in memory, and its operands.
 template <int CACHE, int D> struct Row;
 template <int D> struct Row<0, D> {
@@ -87,13 +103,7 @@ template <int D> struct Row<1, D> {
         }
         s = scales[at >> 5];
     }
-    __device__ __forceinline__ uint4 operand(int c) const {
-        const float u = __uint_as_float(s << 23);
-        return make_uint4(__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * c], u, false)),
-                          __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * c], u, true)),
-                          __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * c + 1], u, false)),
-                          __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[2 * c + 1], u, true)));
-    }
+    __device__ __forceinline__ uint4 operand(int c) const { return values_of<1>(w + 2 * c, s); }
 };
 template <int D> struct Row<2, D> {
     unsigned w[D / 32], s;
@@ -111,13 +121,7 @@ template <int D> struct Row<2, D> {
         }
         s = scales[at >> 4];
     }
-    __device__ __forceinline__ uint4 operand(int c) const {
-        const float u = __uint_as_float(s << 23);
-        return make_uint4(__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[c], u, 0)),
-                          __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[c], u, 1)),
-                          __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[c], u, 2)),
-                          __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[c], u, 3)));
-    }
+    __device__ __forceinline__ uint4 operand(int c) const { return values_of<2>(w + c, s); }
 };
 
 // Eight of a query's elements as one operand, or the two operands whose sum they are (11 bits: the high part has 8).
@@ -142,6 +146,33 @@ struct Task {
     int begin, end, slot;
 };
 
+// Bytes of a row of codes or elements.
+template <int CACHE, int D> constexpr int row_bytes() { return CACHE == 0 ? 2 * D : (CACHE == 1 ? D : D / 2); }
+
+// Where a key's row lies, in bytes of codes or elements of the pool (the row's scales lie a 32nd of that behind theirs, a 16th for 4-bit codes).
+// The table is read some time before the place is used.
+template <int ROW> struct Rows {
+    struct Place {
+        int entry, line;                               // of the table, and row within the page
+    };
+    const int32_t* table;
+    unsigned token, magic;                             // bytes between the rows of a page; of the division by the page size
+    uint64_t page_bytes;
+    int last, page, shift, last_page;
+    __device__ __forceinline__ Rows(const SharedArgs& A, const Task& W)
+        : table(W.table), token((unsigned)A.Hkv * ROW), magic(A.page_magic), page_bytes((uint64_t)((unsigned)A.Hkv * ROW) * (unsigned)A.page),
+          last(W.end - 1), page(A.page), shift(A.page_shift), last_page(A.last_page) {}
+    __device__ __forceinline__ Place look_up(int key) const {
+        const int r = min(key, last);                  // (behind the end: the last row again)
+        const int pg = (int)(__umulhi((unsigned)r << 1, magic) >> shift);
+        return Place{table[pg], r - pg * page};
+    }
+    __device__ __forceinline__ int64_t place(const Place& p) const {
+        const unsigned at = (unsigned)min(max(p.entry, 0), last_page);
+        return (int64_t)(at * page_bytes + (uint64_t)token * (unsigned)p.line);
+    }
+};
+
 // LDS of a workgroup: the waves' values of a step, and behind the loop their sums.
 template <int D> union Shared {
     char v[kWaves][32 * 2 * D];
@@ -164,6 +195,12 @@ __device__ __forceinline__ float across_groups(float x) {
     x = fmaxf(__uint_as_float(y[0]), __uint_as_float(y[1]));
     const auto z = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return fmaxf(__uint_as_float(z[0]), __uint_as_float(z[1]));
+}
+
+// The other half of the wave: lane l gets lane l ^ 32's value.
+__device__ __forceinline__ float other_half(float x) {
+    const auto y = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float((threadIdx.x & 32) ? y[0] : y[1]);
 }
 
 template <typename T, int CACHE, int D, int NC>
@@ -202,46 +239,31 @@ __device__ __forceinline__ void attend(const SharedArgs& A, const Task& W, Share
 #pragma unroll
         for (int i = 0; i < NB; ++i) acc[b][i] = dfx4{0.f, 0.f, 0.f, 0.f};
     }
-    // Where a key's row lies, in bytes of codes or rows (a row's scales lie as many 32nds or 16ths of that behind theirs); its page is
-    // looked up one step before.
-    constexpr int ROW = CACHE == 0 ? 2 * D : (CACHE == 1 ? D : D / 2);
-    const unsigned token = (unsigned)A.Hkv * ROW;      // bytes between the rows of a page
-    const uint64_t page_bytes = (uint64_t)token * (unsigned)A.page;
+    constexpr int ROW = row_bytes<CACHE, D>();
+    const Rows<ROW> rows(A, W);
     const int lane_at = W.kvh * ROW + kg * (CACHE == 0 ? 16 : ROW / 4), scale_at = W.kvh * (D / 32) + kg * (D / 4) / 32;
     const char *kb = A.k + lane_at, *vb = A.v + lane_at;
     const unsigned char *ks = CACHE ? A.k_scales + scale_at : nullptr, *vs = CACHE ? A.v_scales + scale_at : nullptr;
-    struct Place {
-        int entry, line;                               // of the table, and row within the page
-    };
-    auto look_up = [&](int key) {
-        const int r = min(key, W.end - 1);             // (behind the end: the last row again)
-        const int pg = (int)(__umulhi((unsigned)r << 1, A.page_magic) >> A.page_shift);
-        return Place{W.table[pg], r - pg * A.page};
-    };
-    auto place = [&](const Place& p) {
-        const unsigned at = (unsigned)min(max(p.entry, 0), A.last_page);
-        return (int64_t)(at * page_bytes + (uint64_t)token * (unsigned)p.line);
-    };
     constexpr int STEP = 32 * kWaves;
     const float rest = K::kGrowth / A.scale2;
     int key = W.begin + 32 * wave;
     Row<CACHE, D> kx, ky, vx, vy;
-    Place px{}, py{};
+    typename Rows<ROW>::Place px{}, py{};
     if (key < W.end) {
-        px = look_up(key + n16);
-        py = look_up(key + 16 + n16);
-        const int64_t x = place(px), y = place(py);
+        px = rows.look_up(key + n16);
+        py = rows.look_up(key + 16 + n16);
+        const int64_t x = rows.place(px), y = rows.place(py);
         kx.load(kb, ks, x);
         ky.load(kb, ks, y);
         vx.load(vb, vs, x);
         vy.load(vb, vs, y);
-        px = look_up(key + STEP + n16);
-        py = look_up(key + STEP + 16 + n16);
+        px = rows.look_up(key + STEP + n16);
+        py = rows.look_up(key + STEP + 16 + n16);
     }
     for (; key < W.end; key += STEP) {
-        const int64_t x = place(px), y = place(py);    // of the next step
-        px = look_up(key + 2 * STEP + n16);
-        py = look_up(key + 2 * STEP + 16 + n16);
+        const int64_t x = rows.place(px), y = rows.place(py);    // of the next step
+        px = rows.look_up(key + 2 * STEP + n16);
+        py = rows.look_up(key + 2 * STEP + 16 + n16);
         dfx4 sx[NC], sy[NC];
 #pragma unroll
         for (int b = 0; b < NC; ++b) sx[b] = sy[b] = dfx4{0.f, 0.f, 0.f, 0.f};
@@ -334,7 +356,7 @@ __device__ __forceinline__ void attend(const SharedArgs& A, const Task& W, Share
         asm volatile("" ::: "memory");
     }
 #pragma unroll
-    for (int b = 0; b < NC; ++b) m[b] *= A.scale2;     // (what saw no keys: the lowest number, or -infinity)
+    for (int b = 0; b < NC; ++b) m[b] = m[b] * A.scale2 - kShift;   // (probabilities are 2^(logit - that) now)
     __syncthreads();                                   // (all waves have read their values)
     constexpr int DT = D / 16;
     const int qi = tid >> 4, d0 = (tid & 15) * DT;
@@ -373,13 +395,294 @@ __device__ __forceinline__ void attend(const SharedArgs& A, const Task& W, Share
 #pragma unroll
             for (int d = 0; d < DT; ++d) out[d] = (elem)(o[d] * inv);
             if (A.lse && (tid & 15) == 0)
-                A.lse[hq] = Lq == 0.f ? -INFINITY : (most - kShift + __builtin_amdgcn_logf(Lq)) * 0.6931471805599453f;
+                A.lse[hq] = Lq == 0.f ? -INFINITY : (most + __builtin_amdgcn_logf(Lq)) * 0.6931471805599453f;
         } else {
             float* pa = A.part_acc + (hq * A.slots + W.slot) * D + d0;
 #pragma unroll
             for (int d = 0; d < DT; ++d) pa[d] = o[d];
             if ((tid & 15) == 0) A.part_ml[hq * A.slots + W.slot] = make_float2(most, Lq);
         }
+    }
+}
+
+typedef __attribute__((ext_vector_type(8))) short frag;          // an operand's eight elements
+typedef __attribute__((ext_vector_type(16))) float fx16;
+__device__ __forceinline__ fx16 mma32(dec_bf16, frag a, frag b, fx16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(dbf16x8, a), __builtin_bit_cast(dbf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ fx16 mma32(dec_f16, frag a, frag b, fx16 c) {
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(df16x8, a), __builtin_bit_cast(df16x8, b), c, 0, 0, 0);
+}
+
+// LDS of a workgroup that meets a prefix's rows with 64 or 128 query heads: two tiles each of keys and values, and behind the loop the
+// waves' sums.
+constexpr int kKeys = 64;      // keys of a tile
+template <int D> union Wide {
+    struct {
+        char k[2][kKeys * 2 * D], v[2][kKeys * 2 * D];
+    } tile;
+    struct {
+        float acc[kWaves][32][D], m[kWaves][32], l[kWaves][32];
+    } sum;
+};
+
+// A lane's part of a tile on its way from the pool to LDS.  Plain rows go there by themselves, 16 bytes a lane at a time; codes pass
+// through registers, a block of 32 of a key and a value row per thread (heads of 64: of one of them).
+template <typename T, int CACHE, int D> struct Fetch;
+template <typename T, int D> struct Fetch<T, 0, D> {
+    static constexpr int PIECES = D / 8, RPL = 64 / PIECES, PER = kKeys / (RPL * kWaves);   // 16-byte pieces of a row; rows of a load; loads
+    typedef typename Rows<2 * D>::Place Place;
+    const char *kb, *vb;
+    int first;                                        // row of the lane's first load
+    Place p[PER];
+    __device__ __forceinline__ Fetch(const SharedArgs& A, const Task& W, int wave, int lane) {
+        first = wave * RPL + lane / PIECES;           // (rows of the others have the same places)
+        kb = A.k + W.kvh * (2 * D) + ((lane % PIECES) ^ (first & (PIECES - 1))) * 16;
+        vb = A.v + W.kvh * (2 * D) + place_of<D>(first, lane % PIECES) * 16;
+    }
+    __device__ __forceinline__ void look_up(const Rows<2 * D>& rows, int key) {
+#pragma unroll
+        for (int i = 0; i < PER; ++i) p[i] = rows.look_up(key + i * RPL * kWaves + first);
+    }
+    __device__ __forceinline__ void start(const Rows<2 * D>& rows, char* k, char* v, int wave) {
+        typedef __attribute__((address_space(1))) void* from;
+        typedef __attribute__((address_space(3))) void* to;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const int64_t at = rows.place(p[i]);
+            __builtin_amdgcn_global_load_lds((from)(kb + at), (to)(k + (i * kWaves + wave) * 1024), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((from)(vb + at), (to)(v + (i * kWaves + wave) * 1024), 16, 0, 0);
+        }
+    }
+    // (such loads write no register that the compiler would wait for, and a barrier alone does not wait)
+    __device__ __forceinline__ void finish(char*, char*) { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+};
+template <typename T, int CACHE, int D> struct Fetch {
+    static constexpr int ROW = row_bytes<CACHE, D>(), BLOCKS = D / 32, N = D == 128 ? 2 : 1, W4 = CACHE == 1 ? 8 : 4;   // N: blocks of a thread; its words
+    typedef typename Rows<ROW>::Place Place;
+    int key, block, tensor;
+    const char* base[N];
+    const unsigned char* scales[N];
+    Place p;
+    unsigned w[N][W4], s[N];
+    __device__ __forceinline__ Fetch(const SharedArgs& A, const Task& W, int wave, int lane) {
+        const int tid = wave * 64 + lane;
+        tensor = N == 2 ? 0 : tid / (kKeys * BLOCKS);
+        key = tid / BLOCKS % kKeys;
+        block = tid % BLOCKS;
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            base[n] = (tensor + n == 0 ? A.k : A.v) + W.kvh * ROW + block * (ROW / BLOCKS);
+            scales[n] = (tensor + n == 0 ? A.k_scales : A.v_scales) + W.kvh * BLOCKS + block;
+        }
+    }
+    __device__ __forceinline__ void look_up(const Rows<ROW>& rows, int first) { p = rows.look_up(first + key); }
+    __device__ __forceinline__ void start(const Rows<ROW>& rows, char*, char*, int) {
+        const int64_t at = rows.place(p);
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+#pragma unroll
+            for (int i = 0; i < W4 / 4; ++i) {
+                const uint4 x = *reinterpret_cast<const uint4*>(base[n] + at + 16 * i);
+                w[n][4 * i] = x.x;
+                w[n][4 * i + 1] = x.y;
+                w[n][4 * i + 2] = x.z;
+                w[n][4 * i + 3] = x.w;
+            }
+            s[n] = scales[n][at >> (CACHE == 1 ? 5 : 4)];
+        }
+    }
+    __device__ __forceinline__ void finish(char* k, char* v) {
+#pragma unroll
+        for (int n = 0; n < N; ++n) {
+            const bool is_k = tensor + n == 0;
+            char* to = (is_k ? k : v) + key * (2 * D);
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const int piece = 4 * block + c, at = is_k ? piece ^ (key & (D / 8 - 1)) : place_of<D>(key, piece);
+                *reinterpret_cast<uint4*>(to + at * 16) = values_of<CACHE>(w[n] + c * (W4 / 4), s[n]);
+            }
+        }
+    }
+};
+
+// attend for up to 32 RB query heads in products of 32x32x16: lane l = 32 h + n supplies row or column n and contraction elements 8 h .. +7; register
+// r of lane l is row 8 (r / 4) + 4 h + r % 4, column n.  RB waves have 32 query heads each, and each of the 4 / RB such sets every other block
+// of 32 keys; all share the tiles in LDS.  The probabilities of a lane, 16 keys of one query head a block, enter the last product as they are (contraction
+// element e stands for key 8 (e / 4) + 4 h + e % 4 of 16), rounded to its type once, or, fp16 queries over codes, whose products are in bfloat16, in two parts.
+template <typename T, int CACHE, int D, int RB>
+__device__ __forceinline__ void attend_wide(const SharedArgs& A, const Task& W, Wide<D>& s) {
+    typedef kind<T, CACHE> K;
+    typedef typename K::mat M;
+    constexpr int KS = kWaves / RB;                   // waves that share the keys
+    constexpr int NQ = D / 16, ND = D / 32;           // products along a head; blocks of 32 output elements
+    constexpr bool kF16 = CACHE == 0 && std::is_same<T, dec_f16>::value;
+    // exponent that probabilities are raised by, and the most that a lane's 16 may sum up to before its maximum is moved
+    constexpr float kShift = kF16 ? 7.f : 0.f, kMost = kF16 ? 32768.f : 1048576.f;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int n32 = lane & 31, h2 = lane >> 5, rb = wave % RB, ks = wave / RB;
+    auto head_of = [&](int row) { return ((int64_t)W.b0 + row / A.g) * A.Hq + (int64_t)W.kvh * A.g + row % A.g; };
+    const bool busy = W.row0 + 32 * rb < W.rows;      // the wave has query heads at all
+
+    frag qf[NQ][K::kQ];
+    {
+        const int row = min(W.row0 + 32 * rb + n32, W.rows - 1);      // (behind the last: it again, and nothing is stored)
+        const char* q = A.q + head_of(row) * (2 * D) + 16 * h2;
+#pragma unroll
+        for (int c = 0; c < NQ; ++c) {
+            uint4 x[K::kQ];
+            query_operands<T, CACHE>(*reinterpret_cast<const uint4*>(q + 32 * c), x);
+#pragma unroll
+            for (int i = 0; i < K::kQ; ++i) qf[c][i] = __builtin_bit_cast(frag, x[i]);
+        }
+    }
+    float m = -3.4028235e38f, lsum = 0.f;             // (finite: logits of -infinity have probability 0 and not NaN)
+    fx16 acc[ND];
+#pragma unroll
+    for (int i = 0; i < ND; ++i)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) acc[i][r] = 0.f;
+
+    const Rows<row_bytes<CACHE, D>()> rows(A, W);
+    Fetch<T, CACHE, D> fetch(A, W, wave, lane);
+    // a lane's places in a tile: its pieces of key row n32, and of the first value row that it transposes
+    const int vr = 4 * h2 + (lane & 15) / 4;
+    const unsigned k_at = n32 * (2 * D) + ((h2 ^ (n32 & (D / 8 - 1))) * 16);
+    const unsigned v_at = vr * (2 * D) + place_of<D>(vr, 2 * ((lane >> 4) & 1) + (lane & 3) / 2) * 16 + (lane & 1) * 8;
+    constexpr unsigned kTurn = D == 128 ? 32 : 0;     // (what rows 8 further down differ by)
+
+    auto probabilities = [&](const fx16& x, float* e, float* sum) {
+        const float shift = kShift - m;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) e[r] = __builtin_fmaf(x[r], A.scale2, shift);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) e[r] = __builtin_amdgcn_exp2f(e[r]);
+        sum[0] = e[0];
+        sum[1] = e[1];
+#pragma unroll
+        for (int r = 2; r < 16; ++r) sum[r & 1] += e[r];
+    };
+    auto block = [&](int key, const char* sk, const char* sv) {
+        fx16 x;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) x[r] = 0.f;
+#pragma unroll
+        for (int c = 0; c < NQ; ++c) {
+            const frag kf = *reinterpret_cast<const frag*>(sk + (k_at ^ (unsigned)(c * 32)));
+#pragma unroll
+            for (int i = 0; i < K::kQ; ++i) x = mma32(M{}, kf, qf[c][i], x);
+        }
+        if (key + 32 > W.end) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (key + 8 * (r / 4) + 4 * h2 + r % 4 >= W.end) x[r] = -INFINITY;
+        }
+        float e[16], sum[2];
+        probabilities(x, e, sum);
+        // A row's maximum is looked for, and its sums moved to it, only when they outgrow kMost.  (A row's two lanes have other halves of the keys.)
+        const float both = sum[0] + sum[1];
+        if (__any(both > kMost)) {
+            float big = x[0];
+#pragma unroll
+            for (int r = 1; r < 16; ++r) big = fmaxf(big, x[r]);
+            const float others = other_half(both), top = fmaxf(big, other_half(big)) * A.scale2;
+            const float mn = both > kMost || others > kMost ? fmaxf(m, top) : m;
+            const float alpha = __builtin_amdgcn_exp2f(m - mn);
+            m = mn;
+            lsum *= alpha;
+#pragma unroll
+            for (int i = 0; i < ND; ++i)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) acc[i][r] *= alpha;
+            probabilities(x, e, sum);
+        }
+        lsum += sum[0] + sum[1];
+        frag pf[2][K::kQ];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            if constexpr (K::kQ == 1) {
+                typedef __attribute__((ext_vector_type(8))) typename std::conditional<kF16, _Float16, __bf16>::type rounded;
+                rounded y;
+#pragma unroll
+                for (int r = 0; r < 8; ++r) y[r] = (typename std::conditional<kF16, _Float16, __bf16>::type)e[8 * j + r];
+                pf[j][0] = __builtin_bit_cast(frag, y);
+            } else {
+                unsigned hi[4], lo[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) split2(dec_bf16{}, e[8 * j + 2 * r], e[8 * j + 2 * r + 1], hi[r], lo[r]);
+                pf[j][0] = __builtin_bit_cast(frag, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+                pf[j][K::kQ - 1] = __builtin_bit_cast(frag, make_uint4(lo[0], lo[1], lo[2], lo[3]));
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+            for (int i = 0; i < ND; ++i) {
+                const unsigned at = (v_at ^ (unsigned)(i * 64)) + 16 * j * (2 * D);
+                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)((lds_char)sv + at));
+                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)((lds_char)sv + (at ^ kTurn) + 8 * (2 * D)));
+                const frag vf = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+#pragma unroll
+                for (int n = 0; n < K::kQ; ++n) acc[i] = mma32(M{}, vf, pf[j][n], acc[i]);
+            }
+    };
+    const int tiles = (W.end - W.begin + kKeys - 1) / kKeys;
+    fetch.look_up(rows, W.begin);
+    fetch.start(rows, s.tile.k[0], s.tile.v[0], wave);
+    fetch.look_up(rows, W.begin + kKeys);
+    fetch.finish(s.tile.k[0], s.tile.v[0]);
+    __syncthreads();
+    auto tile = [&](int t, int now) {
+        const int key = W.begin + t * kKeys;
+        char *k_now = s.tile.k[now], *v_now = s.tile.v[now], *k_next = s.tile.k[now ^ 1], *v_next = s.tile.v[now ^ 1];
+        if (t + 1 < tiles) {
+            fetch.start(rows, k_next, v_next, wave);
+            fetch.look_up(rows, key + 2 * kKeys);
+        }
+        if (busy) {
+#pragma unroll
+            for (int i = 0; i < 2 / KS; ++i) {
+                const int b = KS == 1 ? i : ks;
+                if (key + 32 * b < W.end) block(key + 32 * b, k_now + 32 * b * (2 * D), v_now + 32 * b * (2 * D));
+            }
+        }
+        if (t + 1 < tiles) fetch.finish(k_next, v_next);
+        __syncthreads();                              // the next tiles have arrived, these have been read
+    };
+    for (int t = 0; t < tiles; t += 2) {
+        tile(t, 0);
+        if (t + 1 < tiles) tile(t + 1, 1);
+    }
+    // The waves' sums (four floats permuted, so that the rows of a write meet all banks), and the answer, 16 bytes of a row a lane.
+    auto at = [&](int w, int line, int four) { return reinterpret_cast<float4*>(&s.sum.acc[w][line][0]) + (four ^ (line & (D / 4 - 1))); };
+    const float l = lsum + other_half(lsum);
+#pragma unroll
+    for (int i = 0; i < ND; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            *at(wave, n32, 8 * i + 2 * r + h2) = make_float4(acc[i][4 * r], acc[i][4 * r + 1], acc[i][4 * r + 2], acc[i][4 * r + 3]);
+    if (h2 == 0) {
+        s.sum.m[wave][n32] = m - kShift;              // (probabilities are 2^(logit - that) now)
+        s.sum.l[wave][n32] = l;
+    }
+    __syncthreads();
+    constexpr int PER = D / 4;                        // threads of a row
+    for (int line = tid / PER; line < 32 * RB; line += kWaves * 64 / PER) {
+        const int row = W.row0 + line;
+        if (row >= W.rows) break;
+        const int w = line / 32, n = line % 32, four = tid % PER;
+        float4 o = *at(w, n, four);
+        float M = s.sum.m[w][n], L = s.sum.l[w][n];
+        if constexpr (KS == 2) {
+            const float M1 = s.sum.m[w + RB][n], top = fmaxf(M, M1), f0 = __builtin_amdgcn_exp2f(M - top), f1 = __builtin_amdgcn_exp2f(M1 - top);
+            const float4 o1 = *at(w + RB, n, four);
+            o = make_float4(o.x * f0 + o1.x * f1, o.y * f0 + o1.y * f1, o.z * f0 + o1.z * f1, o.w * f0 + o1.w * f1);
+            L = L * f0 + s.sum.l[w + RB][n] * f1;
+            M = top;
+        }
+        const int64_t to = head_of(row) * A.slots + W.slot;
+        *reinterpret_cast<float4*>(A.part_acc + to * D + four * 4) = o;
+        if (four == 0) A.part_ml[to] = make_float2(M, L);
     }
 }
 
@@ -455,14 +758,20 @@ __global__ __launch_bounds__(kWaves * 64, D == 64 ? 4 : 3) void cached_attn(cons
     if (own_task<false>(A, blockIdx.x, W)) attend<T, CACHE, D, 1>(A, W, s);
 }
 
-template <typename T, int CACHE, int D, int NC>
-__global__ __launch_bounds__(kWaves * 64, NC == 1 ? (D == 64 ? 4 : 3) : (NC == 2 || D == 64 ? 2 : 1)) void shared_attn(const SharedArgs A) {
-    __shared__ __align__(256) Shared<D> s;
+// R: query heads of a tile.
+template <typename T, int CACHE, int D, int R>
+__global__ __launch_bounds__(kWaves * 64, R == 16 ? (D == 64 ? 4 : 3) : 2) void shared_attn(const SharedArgs A) {
+    constexpr bool kWide = R > 32;
+    __shared__ __align__(256) union {
+        Shared<D> own;
+        typename std::conditional<kWide, Wide<D>, Shared<D>>::type prefix;
+    } s;
     Task W;
     if (blockIdx.x >= A.prefix_groups) {
-        if (own_task<true>(A, blockIdx.x - A.prefix_groups, W)) attend<T, CACHE, D, 1>(A, W, s);
-    } else if (prefix_task<16 * NC>(A, blockIdx.x, threadIdx.x & 63, W)) {
-        attend<T, CACHE, D, NC>(A, W, s);
+        if (own_task<true>(A, blockIdx.x - A.prefix_groups, W)) attend<T, CACHE, D, 1>(A, W, s.own);
+    } else if (prefix_task<R>(A, blockIdx.x, threadIdx.x & 63, W)) {
+        if constexpr (kWide) attend_wide<T, CACHE, D, R / 32>(A, W, s.prefix);
+        else attend<T, CACHE, D, R / 16>(A, W, s.prefix);
     }
 }
 
@@ -471,7 +780,6 @@ template <typename T, int CACHE, int D, bool SHARED>
 __global__ __launch_bounds__(kWaves * 64) void cached_join(const SharedArgs A) {
     typedef typename kind<T, CACHE>::elem elem;
     constexpr int E = D / 64, BATCH = 8;
-    constexpr float kShift = kind<T, CACHE>::kShift;
     const int64_t hq = blockIdx.x;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, b = (int)(hq / A.Hq);
     const int S = clamped(A.lens[b], A.max_len);
@@ -531,9 +839,12 @@ __global__ __launch_bounds__(kWaves * 64) void cached_join(const SharedArgs A) {
     if (threadIdx.x < D) {
         const int d = threadIdx.x;
         const float y = s_o[0][d] + s_o[1][d] + s_o[2][d] + s_o[3][d];
-        reinterpret_cast<elem*>(A.out)[hq * D + d] = (elem)(Lq == 0.f ? 0.f : y / Lq);
+        float z = Lq == 0.f ? 0.f : y / Lq;
+        // (probabilities that were rounded up can carry a mean of numbers near fp16's largest past it; infinities stay)
+        if (CACHE == 0 && std::is_same<T, dec_f16>::value && __builtin_fabsf(z) < INFINITY) z = __builtin_amdgcn_fmed3f(z, -65504.f, 65504.f);
+        reinterpret_cast<elem*>(A.out)[hq * D + d] = (elem)z;
     }
-    if (A.lse && threadIdx.x == 0) A.lse[hq] = Lq == 0.f ? -INFINITY : (M - kShift + __builtin_amdgcn_logf(Lq)) * 0.6931471805599453f;
+    if (A.lse && threadIdx.x == 0) A.lse[hq] = Lq == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(Lq)) * 0.6931471805599453f;
 }
 
 }  // namespace
@@ -552,10 +863,11 @@ SharedPlan shared_plan(int B, int G, int Hq, int Hkv, int D, int64_t max_prefix,
     P.least = P.nchunk == 1 || pairs > 128 ? 512 : (pairs > 64 ? 256 : 128);
     if (G > 0) {
         const int64_t rows = ((int64_t)B * g + G - 1) / G;    // of a group, on the average
-        P.columns = rows <= 16 ? 16 : (rows <= 32 ? 32 : 64);
+        P.columns = rows <= 16 ? 16 : (rows <= 32 ? 32 : (rows <= 64 ? 64 : 128));
         P.tiles = (int)(G + (int64_t)B * g / P.columns);
         const int64_t units = (int64_t)P.tiles * Hkv;
-        P.prefix_chunks = (int)std::max<int64_t>(1, std::min<int64_t>({256, (max_prefix + 127) / 128, (1024 + units - 1) / units}));
+        const int64_t most = P.columns <= 32 ? 1024 : 512;
+        P.prefix_chunks = (int)std::max<int64_t>(1, std::min<int64_t>({256, (max_prefix + 127) / 128, (most + units - 1) / units}));
         P.prefix_least = 128;
     }
     P.slots = P.prefix_chunks + P.nchunk;
@@ -600,9 +912,10 @@ hipError_t launch_shared(int dtype, int cache, int D, SharedArgs A, void* worksp
             }
             return;
         }
-        if (P.columns == 16) hipLaunchKernelGGL((shared_attn<T, C, DD, 1>), grid, block, 0, st, A);
-        else if (P.columns == 32) hipLaunchKernelGGL((shared_attn<T, C, DD, 2>), grid, block, 0, st, A);
-        else hipLaunchKernelGGL((shared_attn<T, C, DD, 4>), grid, block, 0, st, A);
+        if (P.columns == 16) hipLaunchKernelGGL((shared_attn<T, C, DD, 16>), grid, block, 0, st, A);
+        else if (P.columns == 32) hipLaunchKernelGGL((shared_attn<T, C, DD, 32>), grid, block, 0, st, A);
+        else if (P.columns == 64) hipLaunchKernelGGL((shared_attn<T, C, DD, 64>), grid, block, 0, st, A);
+        else hipLaunchKernelGGL((shared_attn<T, C, DD, 128>), grid, block, 0, st, A);
         hipLaunchKernelGGL((cached_join<T, C, DD, true>), heads, block, 0, st, A);
     };
     auto of = [&](auto t, auto c) {

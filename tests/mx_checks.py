@@ -7,7 +7,9 @@ between two codes, which no random input here does, or on a border exactly, wher
 Attention, with the names of serve_checks.py: keys and values are exact bfloat16 numbers in the products and fp16 queries two bfloat16 parts
 whose sum is exact, so logits sum up to 2 D products:  d = 2 (2 D + 4) w reach + 2^-20;  probabilities are two bfloat16 parts by
 truncation, c = 2^-14, except for plain fp16 pages, c = 2^-20 (fp16 parts of 2^15 p; what is below 2^-29 of the largest loses up to 2^-39 of
-that: n 2^-39 more);  joining m partial sums adds m roundings, m <= n:  |got - want| <= u |want| + (c + 2 d + 3 n w) spread.
+that: n 2^-39 more);  joining m partial sums adds m roundings, m <= n:  |got - want| <= u |want| + (c + 2 d + 3 n w) spread.  Prefixes that more than 32 query heads
+of a group meet have their probabilities rounded once, as in the attention over prompts: c = u there (fp16 ones are taken 2^7 times as large, those
+that are subnormal then lose up to 2^-32 of the largest each: n 2^-32 more), but for fp16 queries over codes.
 """
 import numpy as np
 import torch
@@ -16,7 +18,7 @@ from oracle import mx_oracle as orc
 from serve_checks import W24, half_step, num, pool
 
 
-def check_step(got, got_lse, want, want_lse, spread, reach, n, dtype, plain=False):
+def check_step(got, got_lse, want, want_lse, spread, reach, n, dtype, plain=False, rounded=False):
     """got [B, Hq, D], got_lse [B, Hq] tensors (or None), rows that see nothing have want_lse = -inf; n: rows seen at most."""
     some = np.isfinite(want_lse[:, 0])
     got = num(got)
@@ -24,6 +26,8 @@ def check_step(got, got_lse, want, want_lse, spread, reach, n, dtype, plain=Fals
     assert (got[~some] == 0).all()
     D = want.shape[-1]
     c = 2.0 ** -20 + n * 2.0 ** -39 if plain and dtype == torch.float16 else 2.0 ** -14
+    if rounded and (plain or dtype == torch.bfloat16):
+        c = half_step(dtype) + n * 2.0 ** -32
     d = 2 * (2 * D + 4) * W24 * reach + 2.0 ** -20
     bound = half_step(dtype) * np.abs(want) + (c + 2 * d[..., None] + 3 * n * W24) * spread + 1e-30
     if dtype == torch.float16:

@@ -47,7 +47,8 @@ def check(s, kind, out, lse):
     cu = cpu("cu_groups")
     pl, ln = np.clip(cpu("prefix_lens"), 0, s["max_prefix"]), np.clip(cpu("lens"), 0, s["max_len"])
     want = orc.decode_shared(num(s["q"]), k, v, cpu("prefix_table"), pl, cpu("block_table"), ln, list(zip(cu[:-1], cu[1:])))
-    check_step(out, lse, *want, int(pl.max() + ln.max()) + 1, s["q"].dtype, plain=kind == "plain")
+    check_step(out, lse, *want, int(pl.max() + ln.max()) + 1, s["q"].dtype, plain=kind == "plain",
+               rounded=s["q"].shape[0] * s["q"].shape[1] // s["k_pages"].shape[2] > 32 * len(pl))
 
 
 CASES = [   # prefixes, groups, lens, page, Hq, Hkv, D, dtype, kind, before
@@ -79,11 +80,26 @@ def test_step_matches_oracle(snapkv, n):
 
 
 @pytest.mark.parametrize("kind", ["plain", "fp8", "fp4"])
-@pytest.mark.parametrize("members", [1, 3, 4, 5, 8, 9, 16, 17, 31])
+@pytest.mark.parametrize("members", [1, 3, 4, 5, 8, 9, 16, 17, 31, 32, 33, 65])
 def test_tiles_of_query_heads(snapkv, members, kind):
     """Group sizes around whole tiles, four query heads to a KV head; a prefix that ends inside a step, a page and a share."""
     s = build(seeded(70 + members), [389], [members], [members % 5] * members, 16, 4, 1, 128, torch.bfloat16, kind, room=600)
     check(s, kind, *run(snapkv, s))
+
+
+@pytest.mark.parametrize("kind", ["plain", "fp8", "fp4"])
+@pytest.mark.parametrize("members", [3, 9, 20, 40])
+def test_tiles_of_query_heads_of_64_elements(snapkv, members, kind):
+    s = build(seeded(170 + members), [643], [members], [1 + members % 4] * members, 24, 8, 2, 64, torch.float16, kind)
+    check(s, kind, *run(snapkv, s))
+
+
+@pytest.mark.parametrize("P", [1, 31, 32, 33, 63, 64, 65, 127, 128, 129, 191, 1000])
+@pytest.mark.parametrize("members", [10, 20])
+def test_short_prefixes_of_many(snapkv, members, P):
+    """Prefixes that end inside a tile and a block of 32 keys, met by tiles of 64 and of 128 query heads."""
+    s = build(seeded(200 + P), [P], [members], [1] * members, 16, 8, 2, 128, torch.bfloat16, "plain")
+    check(s, "plain", *run(snapkv, s))
 
 
 def test_one_group_without_offsets(snapkv):
@@ -133,6 +149,44 @@ def test_nan_stays_with_those_who_see_it(snapkv):
     torch.cuda.synchronize()
     bad[:3, 2:] = True
     assert got[0][bad].isnan().all() and torch.equal(got[0][~bad], want[0][~bad])
+
+
+@pytest.mark.parametrize("members", [12, 30])
+def test_nan_stays_with_those_who_see_it_in_wide_tiles(snapkv, members):
+    s = build(seeded(183), [300, 300], [members, members], [20] * (2 * members), 16, 4, 2, 128, torch.bfloat16, "plain")
+    s["q"].mul_(2)
+    want = run(snapkv, s)
+    s["q"][1, 2, 5] = float("nan")
+    got = run(snapkv, s)
+    torch.cuda.synchronize()
+    bad = torch.zeros((2 * members, 4), dtype=torch.bool, device="cuda")
+    bad[1, 2] = True
+    assert got[0][bad].isnan().all() and torch.equal(got[0][~bad], want[0][~bad]) and torch.equal(got[1][~bad], want[1][~bad])
+    s["v_pages"][s["prefix_table"][0, 2].long(), 3, 1, 70] = float("inf")   # one element of a value of the first prefix, KV head 1
+    got = run(snapkv, s)
+    torch.cuda.synchronize()
+    assert torch.equal(got[1][~bad], want[1][~bad])
+    bad[:members, 2:] = True
+    assert torch.equal(got[0][~bad], want[0][~bad])
+    seen = got[0][:members, 2:].clone()
+    assert (seen[..., 70].isinf() | seen[..., 70].isnan()).all()
+    seen[..., 70] = want[0][:members, 2:, 70]
+    keep = torch.ones((members, 2), dtype=torch.bool, device="cuda")
+    keep[1, 0] = False
+    assert torch.equal(seen[keep], want[0][:members, 2:][keep])
+    s["k_pages"][s["prefix_table"][1, 18].long(), 11, 0] = float("nan")     # the last row of the second prefix, KV head 0
+    got = run(snapkv, s)
+    torch.cuda.synchronize()
+    assert got[0][members:, :2].isnan().all() and torch.equal(got[0][:members, :2], want[0][:members, :2]) and torch.equal(got[0][members:, 2:], want[0][members:, 2:])
+
+
+def test_fp16_values_near_the_largest(snapkv):
+    """A mean of finite numbers is finite."""
+    s = build(seeded(184), [400], [12], [0] * 12, 16, 8, 2, 64, torch.float16, "plain")
+    s["v_pages"].fill_(65504.0)
+    out, _ = run(snapkv, s)
+    torch.cuda.synchronize()
+    assert out.isfinite().all() and (out.float() >= 65504 * (1 - 2.0 ** -9)).all()
 
 
 def test_a_prefix_shared_is_the_prefix_of_each(snapkv):
