@@ -10,7 +10,7 @@
 //
 // MFMA layout (16x16x32): lane l = 16 kg + n supplies row or column n and contraction elements 8 kg .. +7 of an operand; accumulator
 // register r of lane l is row 4 kg + r, column n.  Which element of a head is which contraction element is free, as long as
-// queries and keys agree: a lane has those that lie in its 16-byte loads (element_of).
+// queries and keys agree: a lane has those that lie side by side in a row of codes (element_of).
 //
 //   logits^T = K Q^T, 32 keys a step, 16 after 16: a lane gets keys 4 kg .. +3 of both.  out^T = V^T P^T with P in two parts:
 //     contraction elements 8 kg .. +7 are those keys, so P never moves.  V goes through LDS, its rows' 16-byte pieces permuted,
@@ -64,65 +64,23 @@ template <int CACHE, int D> __device__ __forceinline__ constexpr int element_of(
 
 typedef __attribute__((ext_vector_type(2))) __bf16 dbf16x2;
 
-// Eight values of codes (8 bits: two words, 4 bits: one) under a scale byte, as bfloat16 numbers.
-template <int CACHE> __device__ __forceinline__ uint4 values_of(const unsigned* w, unsigned s) {
+// Eight values of codes (of 8 bits: both words, of 4: the first) under a scale byte, as bfloat16 numbers.
+template <int CACHE> __device__ __forceinline__ uint4 values_of(unsigned w0, unsigned w1, unsigned s) {
     const float u = __uint_as_float(s << 23);
     if constexpr (CACHE == 1)
-        return make_uint4(__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[0], u, false)),
-                          __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[0], u, true)),
-                          __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[1], u, false)),
-                          __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w[1], u, true)));
+        return make_uint4(__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, u, false)),
+                          __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w0, u, true)),
+                          __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, u, false)),
+                          __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w1, u, true)));
     else
-        return make_uint4(__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[0], u, 0)),
-                          __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[0], u, 1)),
-                          __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[0], u, 2)),
-                          __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w[0], u, 3)));
+        return make_uint4(__builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w0, u, 0)),
+                          __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w0, u, 1)),
+                          __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w0, u, 2)),
+                          __builtin_bit_cast(unsigned, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w0, u, 3)));
 }
 
-// A lane's part of a row as it lies in memory, and its operands.
-template <int CACHE, int D> struct Row;
-template <int D> struct Row<0, D> {
-    uint4 w[D / 32];
-    // base, scales: the lane's part of the pool's first row; at: the row's place in bytes.
-    __device__ __forceinline__ void load(const char* base, const unsigned char*, int64_t at) {
-#pragma unroll
-        for (int c = 0; c < D / 32; ++c) w[c] = *reinterpret_cast<const uint4*>(base + at + 64 * c);
-    }
-    __device__ __forceinline__ uint4 operand(int c) const { return w[c]; }
-};
-template <int D> struct Row<1, D> {
-    unsigned w[D / 16], s;
-    __device__ __forceinline__ void load(const char* base, const unsigned char* scales, int64_t at) {
-#pragma unroll
-        for (int c = 0; c < D / 64; ++c) {
-            const uint4 x = *reinterpret_cast<const uint4*>(base + at + 16 * c);
-            w[4 * c] = x.x;
-            w[4 * c + 1] = x.y;
-            w[4 * c + 2] = x.z;
-            w[4 * c + 3] = x.w;
-        }
-        s = scales[at >> 5];
-    }
-    __device__ __forceinline__ uint4 operand(int c) const { return values_of<1>(w + 2 * c, s); }
-};
-template <int D> struct Row<2, D> {
-    unsigned w[D / 32], s;
-    __device__ __forceinline__ void load(const char* base, const unsigned char* scales, int64_t at) {
-        if constexpr (D == 128) {
-            const uint4 x = *reinterpret_cast<const uint4*>(base + at);
-            w[0] = x.x;
-            w[1] = x.y;
-            w[2] = x.z;
-            w[3] = x.w;
-        } else {
-            const uint2 x = *reinterpret_cast<const uint2*>(base + at);
-            w[0] = x.x;
-            w[1] = x.y;
-        }
-        s = scales[at >> 4];
-    }
-    __device__ __forceinline__ uint4 operand(int c) const { return values_of<2>(w + c, s); }
-};
+// Bytes of a row of codes or elements.
+template <int CACHE, int D> constexpr int row_bytes() { return CACHE == 0 ? 2 * D : (CACHE == 1 ? D : D / 2); }
 
 // Eight of a query's elements as one operand, or the two operands whose sum they are (11 bits: the high part has 8).
 template <typename T, int CACHE> __device__ __forceinline__ void query_operands(uint4 x, uint4* q) {
@@ -145,9 +103,6 @@ struct Task {
     const int32_t* table;
     int begin, end, slot;
 };
-
-// Bytes of a row of codes or elements.
-template <int CACHE, int D> constexpr int row_bytes() { return CACHE == 0 ? 2 * D : (CACHE == 1 ? D : D / 2); }
 
 // Where a key's row lies, in bytes of codes or elements of the pool (the row's scales lie a 32nd of that behind theirs, a 16th for 4-bit codes).
 // The table is read some time before the place is used.
@@ -173,21 +128,110 @@ template <int ROW> struct Rows {
     }
 };
 
-// LDS of a workgroup: the waves' values of a step, and behind the loop their sums.
+// LDS of a workgroup: a step's rows, scales and places of each wave, and behind the loop their sums.
 template <int D> union Shared {
-    char v[kWaves][32 * 2 * D];
+    struct {
+        char rows[32 * 2 * D];
+        unsigned char scales[32 * (D / 32)];
+        int64_t places[32];
+    } wave[kWaves];
     struct {
         float acc[kWaves][16][D + 4], m[kWaves][16], l[kWaves][16];
     } sum;
 };
 typedef __attribute__((ext_vector_type(4))) short s16x4;
+typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
 typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
 typedef __attribute__((address_space(3))) char* lds_char;
 
-// Which of its row's 16-byte places holds a piece: the rows that a read meets are in different banks, and those that a write does.
-template <int D> __device__ __forceinline__ int place_of(int row, int piece) {
-    return piece ^ (D == 128 ? (row & 3) << 2 | (row >> 2 & 3) : (row & 1) << 2 | (row >> 1 & 3));
+// Which of its row's 16-byte places in LDS holds a piece of a value row (the four rows of a transposing read are in different banks, and those
+// of a write), and of a key row (those of eight lanes that read one piece each are).
+// (Both permutations turn bits of the place by bits of the row: what rows apart by a multiple of a lane's rows differ by is a constant.)
+template <int D> __device__ __forceinline__ constexpr int place_of(int row, int piece) {
+    return piece ^ ((row & 3) << 1 | (D == 128 ? (row >> 2 & 1) << 3 | (row >> 3 & 1) : row >> 2 & 1));
 }
+template <int ROW> __device__ __forceinline__ constexpr int key_place_of(int row, int piece) {
+    constexpr int PIECES = ROW / 16;
+    return piece ^ (row / (PIECES < 8 ? 8 / PIECES : 1) & (PIECES - 1));
+}
+
+// 32 rows on their way from the pool through a wave's registers to its LDS: neighbouring lanes have neighbouring 16 bytes, which costs the
+// least of the look-ups that the first cache does (8 x 16000 rows of 4 bits, 32 heads: 176 us with a row's pieces 16 lanes apart, as products take them).
+template <int CACHE, int D> struct Stage {
+    static constexpr int ROW = row_bytes<CACHE, D>(), LPR = ROW / 16, RPI = 64 / LPR, N = 32 / RPI, NB = D / 32;   // lanes of a row; rows of a load; loads; blocks of a row
+    u32x4 w[N];
+    unsigned s[CACHE ? N : 1];
+    // base, scales: the lane's part of the pool's first row
+    __device__ __forceinline__ void load(const char* base, const unsigned char* scales, const int64_t* at) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            w[i] = *reinterpret_cast<const u32x4*>(base + at[i]);
+            if constexpr (CACHE != 0) s[i] = scales[at[i] >> (CACHE == 1 ? 5 : 4)];
+        }
+    }
+    // A lane's places in LDS: of its first key's codes or elements, its first value's first piece.
+    static __device__ __forceinline__ unsigned key_at(int lane) { return lane / LPR * ROW + key_place_of<ROW>(lane / LPR, lane % LPR) * 16; }
+    static __device__ __forceinline__ unsigned value_at(int lane) { return lane / LPR * (2 * D) + place_of<D>(lane / LPR, lane % LPR * P) * 16; }
+    static constexpr int P = D / 8 / LPR;              // pieces of a lane's values
+    __device__ __forceinline__ void store_keys(char* rows, unsigned at, unsigned char* scales, int lane) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            *reinterpret_cast<u32x4*>(rows + (at ^ (unsigned)(key_place_of<ROW>(i * RPI, 0) * 16)) + i * RPI * ROW) = w[i];
+            if constexpr (CACHE != 0) scales[(i * RPI + lane / LPR) * NB + lane % LPR / (LPR / NB)] = (unsigned char)s[i];
+        }
+    }
+    __device__ __forceinline__ void store_values(char* rows, unsigned at) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            auto put = [&](int c, uint4 y) __attribute__((always_inline)) {
+                *reinterpret_cast<uint4*>(rows + (at ^ (unsigned)(place_of<D>(i * RPI, c) * 16)) + i * RPI * (2 * D)) = y;
+            };
+            if constexpr (CACHE == 0) {
+                put(0, make_uint4(w[i].x, w[i].y, w[i].z, w[i].w));
+            } else if constexpr (CACHE == 1) {
+                put(0, values_of<1>(w[i].x, w[i].y, s[i]));
+                put(1, values_of<1>(w[i].z, w[i].w, s[i]));
+            } else {
+                put(0, values_of<2>(w[i].x, 0, s[i]));
+                put(1, values_of<2>(w[i].y, 0, s[i]));
+                put(2, values_of<2>(w[i].z, 0, s[i]));
+                put(3, values_of<2>(w[i].w, 0, s[i]));
+            }
+        }
+    }
+};
+// A lane's part of a key row, as the products take it: lane group kg has the elements element_of.
+template <int CACHE, int D> struct Key {
+    static constexpr int ROW = row_bytes<CACHE, D>(), WORDS = ROW / 16;
+    unsigned w[WORDS], s;
+    static __device__ __forceinline__ unsigned at(int row, int kg) {       // of the first piece
+        return row * ROW + key_place_of<ROW>(row, CACHE == 0 ? kg : (WORDS >= 4 ? kg * (WORDS / 4) : kg / 2)) * 16 + (WORDS >= 4 ? 0 : (kg & 1) * 8);
+    }
+    // row: 0, or 16 for the row as many further on, which has the same permutation
+    __device__ __forceinline__ void read(const char* rows, unsigned at, const unsigned char* scales, int row) {
+#pragma unroll
+        for (int i = 0; i < (WORDS + 3) / 4; ++i) {
+            const char* p = rows + (at ^ (unsigned)(i * (CACHE == 0 ? 64 : 16))) + row * ROW;
+            if constexpr (WORDS >= 4) {
+                const u32x4 x = *reinterpret_cast<const u32x4*>(p);
+                w[4 * i] = x.x;
+                w[4 * i + 1] = x.y;
+                w[4 * i + 2] = x.z;
+                w[4 * i + 3] = x.w;
+            } else {
+                const uint2 x = *reinterpret_cast<const uint2*>(p);
+                w[0] = x.x;
+                w[1] = x.y;
+            }
+        }
+        if constexpr (CACHE != 0) s = scales[row * (D / 32)];
+    }
+    __device__ __forceinline__ uint4 operand(int c) const {
+        if constexpr (CACHE == 0) return make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
+        else if constexpr (CACHE == 1) return values_of<1>(w[2 * c], w[2 * c + 1], s);
+        else return values_of<2>(w[c], 0, s);
+    }
+};
 
 // The largest x of the four lanes that have a query's keys.
 __device__ __forceinline__ float across_groups(float x) {
@@ -227,9 +271,12 @@ __device__ __forceinline__ void attend(const SharedArgs& A, const Task& W, Share
             query_operands<T, CACHE>(x, qf[b][c]);
         }
     }
-    char* const sv = s.v[wave];
+    char* const sv = s.wave[wave].rows;
+    unsigned char* const sc = s.wave[wave].scales;
+    int64_t* const places = s.wave[wave].places;
     const int tr = 4 * kg + (n16 >> 2);                // row and place of the lane's first transposing read
-    const unsigned tr_at = tr * (2 * D) + place_of<D>(tr, (n16 & 3) >> 1) * 16 + (n16 & 1) * 8;
+    unsigned tr_at = tr * (2 * D) + place_of<D>(tr, (n16 & 3) >> 1) * 16 + (n16 & 1) * 8;
+    unsigned key_at = Stage<CACHE, D>::key_at(lane), value_at = Stage<CACHE, D>::value_at(lane), operand_at = Key<CACHE, D>::at(n16, kg);
     float m[NC], lsum[NC];
     dfx4 acc[NC][NB];
 #pragma unroll
@@ -239,31 +286,45 @@ __device__ __forceinline__ void attend(const SharedArgs& A, const Task& W, Share
 #pragma unroll
         for (int i = 0; i < NB; ++i) acc[b][i] = dfx4{0.f, 0.f, 0.f, 0.f};
     }
-    constexpr int ROW = row_bytes<CACHE, D>();
+    typedef Stage<CACHE, D> Rows32;
+    constexpr int ROW = Rows32::ROW, LPR = Rows32::LPR, STEP = 32 * kWaves;
     const Rows<ROW> rows(A, W);
-    const int lane_at = W.kvh * ROW + kg * (CACHE == 0 ? 16 : ROW / 4), scale_at = W.kvh * (D / 32) + kg * (D / 4) / 32;
+    const int lane_at = W.kvh * ROW + lane % LPR * 16, scale_at = W.kvh * (D / 32) + lane % LPR / (CACHE ? LPR / (D / 32) : 1);
     const char *kb = A.k + lane_at, *vb = A.v + lane_at;
     const unsigned char *ks = CACHE ? A.k_scales + scale_at : nullptr, *vs = CACHE ? A.v_scales + scale_at : nullptr;
-    constexpr int STEP = 32 * kWaves;
+    Rows32 kr, vr;
+    typename Rows<ROW>::Place p{};
+    // Places of a step's rows: lane l finds that of row l % 32, and gets those of the rows it loads.
+    auto exchange = [&](int64_t* at) {
+        places[lane & 31] = rows.place(p);
+        asm volatile("" ::: "memory");                 // (a wave's LDS operations are done in order)
+#pragma unroll
+        for (int i = 0; i < Rows32::N; ++i) at[i] = places[i * Rows32::RPI + lane / LPR];
+        asm volatile("" ::: "memory");
+    };
     const float rest = K::kGrowth / A.scale2;
     int key = W.begin + 32 * wave;
-    Row<CACHE, D> kx, ky, vx, vy;
-    typename Rows<ROW>::Place px{}, py{};
     if (key < W.end) {
-        px = rows.look_up(key + n16);
-        py = rows.look_up(key + 16 + n16);
-        const int64_t x = rows.place(px), y = rows.place(py);
-        kx.load(kb, ks, x);
-        ky.load(kb, ks, y);
-        vx.load(vb, vs, x);
-        vy.load(vb, vs, y);
-        px = rows.look_up(key + STEP + n16);
-        py = rows.look_up(key + STEP + 16 + n16);
+        p = rows.look_up(key + (lane & 31));
+        int64_t at[Rows32::N];
+        exchange(at);
+        kr.load(kb, ks, at);
+        vr.load(vb, vs, at);
+        p = rows.look_up(key + STEP + (lane & 31));
     }
     for (; key < W.end; key += STEP) {
-        const int64_t x = rows.place(px), y = rows.place(py);    // of the next step
-        px = rows.look_up(key + 2 * STEP + n16);
-        py = rows.look_up(key + 2 * STEP + 16 + n16);
+        int64_t at[Rows32::N];                         // of the next step
+        exchange(at);
+        p = rows.look_up(key + 2 * STEP + (lane & 31));
+        Key<CACHE, D> kx, ky;
+        // (sums of a place and a constant, made once in front of the loop, would take more registers than there are)
+        asm volatile("" : "+v"(tr_at), "+v"(key_at), "+v"(value_at), "+v"(operand_at));
+        kr.store_keys(sv, key_at, sc, lane);
+        asm volatile("" ::: "memory");
+        const unsigned char* own = sc + n16 * (D / 32) + kg * (D / 4) / 32;
+        kx.read(sv, operand_at, own, 0);
+        ky.read(sv, operand_at, own, 16);
+        kr.load(kb, ks, at);
         dfx4 sx[NC], sy[NC];
 #pragma unroll
         for (int b = 0; b < NC; ++b) sx[b] = sy[b] = dfx4{0.f, 0.f, 0.f, 0.f};
@@ -278,10 +339,6 @@ __device__ __forceinline__ void attend(const SharedArgs& A, const Task& W, Share
                     sy[b] = mma(M{}, oy, qf[b][c][i], sy[b]);
                 }
         }
-        __builtin_amdgcn_sched_barrier(0);             // (the next keys come into these registers)
-        kx.load(kb, ks, x);
-        ky.load(kb, ks, y);
-        __builtin_amdgcn_sched_barrier(0);
         if (key + 32 > W.end) {                        // the last step
             const int k0 = key + 4 * kg;
 #pragma unroll
@@ -331,21 +388,15 @@ __device__ __forceinline__ void attend(const SharedArgs& A, const Task& W, Share
             split2(M{}, e[4], e[5], ph[b].z, pl[b].z);
             split2(M{}, e[6], e[7], ph[b].w, pl[b].w);
         }
-#pragma unroll
-        for (int c = 0; c < NP; ++c) {
-            const int to = n16 * (2 * D) + place_of<D>(n16, element_of<CACHE, D>(kg, c, 0) / 8) * 16;
-            *reinterpret_cast<uint4*>(sv + to) = vx.operand(c);
-            *reinterpret_cast<uint4*>(sv + 16 * (2 * D) + to) = vy.operand(c);
-        }
-        __builtin_amdgcn_sched_barrier(0);             // (as the next values)
-        vx.load(vb, vs, x);
-        vy.load(vb, vs, y);
-        asm volatile("" ::: "memory");                 // (a wave's LDS operations are done in order)
+        asm volatile("" ::: "memory");
+        vr.store_values(sv, value_at);
+        asm volatile("" ::: "memory");
+        vr.load(vb, vs, at);
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
-            const lds_char at = (lds_char)sv + (tr_at ^ (unsigned)(i * 32));
-            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)at);
-            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(at + 16 * 2 * D));
+            const lds_char from = (lds_char)sv + (tr_at ^ (unsigned)(i * 32));
+            const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)from);
+            const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(from + 16 * 2 * D));
             const uint4 vt = __builtin_bit_cast(uint4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
 #pragma unroll
             for (int b = 0; b < NC; ++b) {
@@ -500,7 +551,7 @@ template <typename T, int CACHE, int D> struct Fetch {
 #pragma unroll
             for (int c = 0; c < 4; ++c) {
                 const int piece = 4 * block + c, at = is_k ? piece ^ (key & (D / 8 - 1)) : place_of<D>(key, piece);
-                *reinterpret_cast<uint4*>(to + at * 16) = values_of<CACHE>(w[n] + c * (W4 / 4), s[n]);
+                *reinterpret_cast<uint4*>(to + at * 16) = values_of<CACHE>(w[n][c * (W4 / 4)], w[n][c * (W4 / 4) + (W4 / 4 - 1)], s[n]);
             }
         }
     }
@@ -549,7 +600,7 @@ __device__ __forceinline__ void attend_wide(const SharedArgs& A, const Task& W, 
     const int vr = 4 * h2 + (lane & 15) / 4;
     const unsigned k_at = n32 * (2 * D) + ((h2 ^ (n32 & (D / 8 - 1))) * 16);
     const unsigned v_at = vr * (2 * D) + place_of<D>(vr, 2 * ((lane >> 4) & 1) + (lane & 3) / 2) * 16 + (lane & 1) * 8;
-    constexpr unsigned kTurn = D == 128 ? 32 : 0;     // (what rows 8 further down differ by)
+    constexpr unsigned kTurn = D == 128 ? 16 : 0;     // (what rows 8 further down differ by)
 
     auto probabilities = [&](const fx16& x, float* e, float* sum) {
         const float shift = kShift - m;
