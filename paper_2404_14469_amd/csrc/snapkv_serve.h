@@ -80,7 +80,8 @@ struct SharedArgs {
     int nchunk, least, prefix_chunks, prefix_least;  // shares of a sequence or prefix at most, and keys of the shortest
     int tiles;                                       // places of a prefix's query heads, all groups together
     int slots;                                       // partials of a query head: the prefix's, then its own
-    int places;                                      // of workgroups, per sequence and KV head
+    int places;                                      // of workgroups, per sequence and set of KV heads
+    int head_shift;                                  // 2^head_shift KV heads in a set, which a workgroup of an own share takes together
     bool by_xcd, prefix_by_xcd;                      // how the workgroups of own and of prefixes' shares are dealt out
     unsigned prefix_groups;                          // workgroups for prefixes, which come first
     unsigned page_magic;                             // r / page = (2 r * page_magic >> 32) >> page_shift, r < 2^31

@@ -97,9 +97,10 @@ template <typename T, int CACHE> __device__ __forceinline__ void query_operands(
 }
 
 // What a workgroup has to do: keys begin .. end - 1 of the rows that `table` names, for the query heads row0 .. of rows of them,
-// sequence by sequence from b0 on, that read KV head kvh; its answer is partial `slot` of theirs, or (slot < 0) the whole.
+// sequence by sequence from b0 on, that read KV head kvh (or, a wave each and so fewer waves a head, that and the next 2^shift - 1); its answer is
+// partial `slot` of theirs, or (slot < 0) the whole.
 struct Task {
-    int b0, row0, rows, kvh;
+    int b0, row0, rows, kvh, shift;
     const int32_t* table;
     int begin, end, slot;
 };
@@ -128,19 +129,20 @@ template <int ROW> struct Rows {
     }
 };
 
-// LDS of a workgroup: a step's rows, scales and places of each wave, and behind the loop their sums.
+// LDS of a workgroup: a step's rows and places of each wave, the scales of 128 keys and values of all its KV heads, and behind the loop the waves' sums.
 template <int D> union Shared {
     struct {
-        char rows[32 * 2 * D];
-        unsigned char scales[32 * (D / 32)];
-        int64_t places[32];
-    } wave[kWaves];
+        char rows[kWaves][32 * 2 * D];
+        int64_t places[kWaves][32];
+        unsigned char scales[32 * kWaves * 2 * 4 * (D / 32)];
+    } step;
     struct {
         float acc[kWaves][16][D + 4], m[kWaves][16], l[kWaves][16];
     } sum;
 };
 typedef __attribute__((ext_vector_type(4))) short s16x4;
 typedef __attribute__((ext_vector_type(4))) unsigned u32x4;
+typedef __attribute__((ext_vector_type(2))) unsigned u32x2;
 typedef __attribute__((address_space(3))) s16x4* lds_s16x4;
 typedef __attribute__((address_space(3))) char* lds_char;
 
@@ -160,27 +162,24 @@ template <int ROW> __device__ __forceinline__ constexpr int key_place_of(int row
 template <int CACHE, int D> struct Stage {
     static constexpr int ROW = row_bytes<CACHE, D>(), LPR = ROW / 16, RPI = 64 / LPR, N = 32 / RPI, NB = D / 32;   // lanes of a row; rows of a load; loads; blocks of a row
     u32x4 w[N];
-    unsigned s[CACHE ? N : 1];
-    // base, scales: the lane's part of the pool's first row
-    __device__ __forceinline__ void load(const char* base, const unsigned char* scales, const int64_t* at) {
+    // base: the lane's part of the pool's first row
+    __device__ __forceinline__ void load(const char* base, const int64_t* at) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            w[i] = *reinterpret_cast<const u32x4*>(base + at[i]);
-            if constexpr (CACHE != 0) s[i] = scales[at[i] >> (CACHE == 1 ? 5 : 4)];
-        }
+        for (int i = 0; i < N; ++i) w[i] = *reinterpret_cast<const u32x4*>(base + at[i]);
     }
     // A lane's places in LDS: of its first key's codes or elements, its first value's first piece.
     static __device__ __forceinline__ unsigned key_at(int lane) { return lane / LPR * ROW + key_place_of<ROW>(lane / LPR, lane % LPR) * 16; }
     static __device__ __forceinline__ unsigned value_at(int lane) { return lane / LPR * (2 * D) + place_of<D>(lane / LPR, lane % LPR * P) * 16; }
     static constexpr int P = D / 8 / LPR;              // pieces of a lane's values
-    __device__ __forceinline__ void store_keys(char* rows, unsigned at, unsigned char* scales, int lane) const {
+    __device__ __forceinline__ void store_keys(char* rows, unsigned at) const {
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            *reinterpret_cast<u32x4*>(rows + (at ^ (unsigned)(key_place_of<ROW>(i * RPI, 0) * 16)) + i * RPI * ROW) = w[i];
-            if constexpr (CACHE != 0) scales[(i * RPI + lane / LPR) * NB + lane % LPR / (LPR / NB)] = (unsigned char)s[i];
-        }
+        for (int i = 0; i < N; ++i) *reinterpret_cast<u32x4*>(rows + (at ^ (unsigned)(key_place_of<ROW>(i * RPI, 0) * 16)) + i * RPI * ROW) = w[i];
     }
-    __device__ __forceinline__ void store_values(char* rows, unsigned at) const {
+    // scales: of the lane's first row, `apart` bytes from one row's to the next's.
+    __device__ __forceinline__ void store_values(char* rows, unsigned at, const unsigned char* scales, int apart) const {
+        unsigned s[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) s[i] = CACHE ? scales[i * RPI * apart] : 0;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             auto put = [&](int c, uint4 y) __attribute__((always_inline)) {
@@ -208,7 +207,7 @@ template <int CACHE, int D> struct Key {
         return row * ROW + key_place_of<ROW>(row, CACHE == 0 ? kg : (WORDS >= 4 ? kg * (WORDS / 4) : kg / 2)) * 16 + (WORDS >= 4 ? 0 : (kg & 1) * 8);
     }
     // row: 0, or 16 for the row as many further on, which has the same permutation
-    __device__ __forceinline__ void read(const char* rows, unsigned at, const unsigned char* scales, int row) {
+    __device__ __forceinline__ void read(const char* rows, unsigned at, int row) {
 #pragma unroll
         for (int i = 0; i < (WORDS + 3) / 4; ++i) {
             const char* p = rows + (at ^ (unsigned)(i * (CACHE == 0 ? 64 : 16))) + row * ROW;
@@ -224,7 +223,6 @@ template <int CACHE, int D> struct Key {
                 w[1] = x.y;
             }
         }
-        if constexpr (CACHE != 0) s = scales[row * (D / 32)];
     }
     __device__ __forceinline__ uint4 operand(int c) const {
         if constexpr (CACHE == 0) return make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
@@ -257,13 +255,14 @@ __device__ __forceinline__ void attend(const SharedArgs& A, const Task& W, Share
     constexpr float kShift = K::kShift;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n16 = lane & 15, kg = lane >> 4;
-    auto head_of = [&](int row) { return ((int64_t)W.b0 + row / A.g) * A.Hq + (int64_t)W.kvh * A.g + row % A.g; };
+    const int heads = 1 << W.shift, kvh = W.kvh + (wave & (heads - 1)), part = wave >> W.shift;
+    auto head_of = [&](int row, int kvh) { return ((int64_t)W.b0 + row / A.g) * A.Hq + (int64_t)kvh * A.g + row % A.g; };
 
     uint4 qf[NC][NP][K::kQ];
 #pragma unroll
     for (int b = 0; b < NC; ++b) {
         const int row = W.row0 + 16 * b + n16;
-        const char* q = A.q + (row < W.rows ? head_of(row) : 0) * (2 * D);
+        const char* q = A.q + (row < W.rows ? head_of(row, kvh) : 0) * (2 * D);
 #pragma unroll
         for (int c = 0; c < NP; ++c) {
             uint4 x = make_uint4(0, 0, 0, 0);
@@ -271,9 +270,8 @@ __device__ __forceinline__ void attend(const SharedArgs& A, const Task& W, Share
             query_operands<T, CACHE>(x, qf[b][c]);
         }
     }
-    char* const sv = s.wave[wave].rows;
-    unsigned char* const sc = s.wave[wave].scales;
-    int64_t* const places = s.wave[wave].places;
+    char* const sv = s.step.rows[wave];
+    int64_t* const places = s.step.places[wave];
     const int tr = 4 * kg + (n16 >> 2);                // row and place of the lane's first transposing read
     unsigned tr_at = tr * (2 * D) + place_of<D>(tr, (n16 & 3) >> 1) * 16 + (n16 & 1) * 8;
     unsigned key_at = Stage<CACHE, D>::key_at(lane), value_at = Stage<CACHE, D>::value_at(lane), operand_at = Key<CACHE, D>::at(n16, kg);
@@ -287,44 +285,93 @@ __device__ __forceinline__ void attend(const SharedArgs& A, const Task& W, Share
         for (int i = 0; i < NB; ++i) acc[b][i] = dfx4{0.f, 0.f, 0.f, 0.f};
     }
     typedef Stage<CACHE, D> Rows32;
-    constexpr int ROW = Rows32::ROW, LPR = Rows32::LPR, STEP = 32 * kWaves;
+    constexpr int ROW = Rows32::ROW, LPR = Rows32::LPR;
+    const int STEP = 32 * kWaves >> W.shift;
     const Rows<ROW> rows(A, W);
-    const int lane_at = W.kvh * ROW + lane % LPR * 16, scale_at = W.kvh * (D / 32) + lane % LPR / (CACHE ? LPR / (D / 32) : 1);
+    const int lane_at = kvh * ROW + lane % LPR * 16;
     const char *kb = A.k + lane_at, *vb = A.v + lane_at;
-    const unsigned char *ks = CACHE ? A.k_scales + scale_at : nullptr, *vs = CACHE ? A.v_scales + scale_at : nullptr;
     Rows32 kr, vr;
     typename Rows<ROW>::Place p{};
     // Places of a step's rows: lane l finds that of row l % 32, and gets those of the rows it loads.
-    auto exchange = [&](int64_t* at) {
+    auto store_places = [&]() {
         places[lane & 31] = rows.place(p);
         asm volatile("" ::: "memory");                 // (a wave's LDS operations are done in order)
+    };
+    auto load_from = [&](Rows32& r, const char* base) {
+        int64_t at[Rows32::N];
 #pragma unroll
         for (int i = 0; i < Rows32::N; ++i) at[i] = places[i * Rows32::RPI + lane / LPR];
         asm volatile("" ::: "memory");
+        r.load(base, at);
+        __builtin_amdgcn_sched_barrier(0);
     };
     const float rest = K::kGrowth / A.scale2;
-    int key = W.begin + 32 * wave;
-    if (key < W.end) {
+    // Scales of 128 rows at a time: a lane fetches those of all the workgroup's KV heads of one key or value row at once (a line of the first cache
+    // has up to 32 heads' scales; fetched by every head for itself they cost as much as the codes), and LDS hands them out.
+    // With one KV head the rows that a wave fetches scales of are those it meets, and nothing is to be waited for.
+    constexpr int NS = D / 32;
+    const int apart = 2 * (NS << W.shift);             // bytes from a row's scales to the next's: keys', values'
+    unsigned char* const mine = s.step.scales + (32 * wave + (lane & 31)) * apart + (lane >> 5) * (apart / 2);
+    const unsigned char* const sb = CACHE ? (lane < 32 ? A.k_scales : A.v_scales) + W.kvh * NS : nullptr;
+    u32x4 sr{};
+    typename Rows<ROW>::Place sp{};
+    auto load_scales = [&]() {
+        const unsigned char* from = sb + (rows.place(sp) >> (CACHE == 1 ? 5 : 4));
+        if (apart == 32) sr = *reinterpret_cast<const u32x4*>(from);
+        else if (apart == 16) sr.xy = *reinterpret_cast<const u32x2*>(from);
+        else if (apart == 8) sr.x = *reinterpret_cast<const unsigned*>(from);
+        else sr.x = *reinterpret_cast<const unsigned short*>(from);
+    };
+    auto store_scales = [&]() {
+        if (apart == 32) *reinterpret_cast<u32x4*>(mine) = sr;
+        else if (apart == 16) *reinterpret_cast<u32x2*>(mine) = sr.xy;
+        else if (apart == 8) *reinterpret_cast<unsigned*>(mine) = sr.x;
+        else *reinterpret_cast<unsigned short*>(mine) = (unsigned short)sr.x;
+    };
+    int key = W.begin + 32 * part, block = W.begin + 32 * wave + (lane & 31);
+    // (waves that share scales take the same number of steps)
+    const int stop = CACHE != 0 && W.shift > 0 ? W.end + 32 * part : W.end;
+    if (key < stop) {
         p = rows.look_up(key + (lane & 31));
-        int64_t at[Rows32::N];
-        exchange(at);
-        kr.load(kb, ks, at);
-        vr.load(vb, vs, at);
+        if constexpr (CACHE != 0) {
+            sp = rows.look_up(block);
+            load_scales();
+            sp = rows.look_up(block + 32 * kWaves);
+        }
+        store_places();
+        // (loads are waited for in their order: the same as in the loop, or its waits are longer)
         p = rows.look_up(key + STEP + (lane & 31));
+        __builtin_amdgcn_sched_barrier(0);
+        load_from(kr, kb);
+        load_from(vr, vb);
     }
-    for (; key < W.end; key += STEP) {
-        int64_t at[Rows32::N];                         // of the next step
-        exchange(at);
+    for (int round = 0; key < stop; key += STEP, ++round) {
+        const int among = round & (heads - 1);         // of the steps that 128 rows are
+        if (CACHE != 0 && among == 0) {
+            if (W.shift > 0) __syncthreads();          // (the ones before have been read)
+            store_scales();
+            if (W.shift > 0) __syncthreads();
+            block += 32 * kWaves;
+            load_scales();
+            sp = rows.look_up(block + 32 * kWaves);
+        }
+        store_places();                                // of the next step
         p = rows.look_up(key + 2 * STEP + (lane & 31));
+        __builtin_amdgcn_sched_barrier(0);
         Key<CACHE, D> kx, ky;
         // (sums of a place and a constant, made once in front of the loop, would take more registers than there are)
         asm volatile("" : "+v"(tr_at), "+v"(key_at), "+v"(value_at), "+v"(operand_at));
-        kr.store_keys(sv, key_at, sc, lane);
+        kr.store_keys(sv, key_at);
         asm volatile("" ::: "memory");
-        const unsigned char* own = sc + n16 * (D / 32) + kg * (D / 4) / 32;
-        kx.read(sv, operand_at, own, 0);
-        ky.read(sv, operand_at, own, 16);
-        kr.load(kb, ks, at);
+        kx.read(sv, operand_at, 0);
+        ky.read(sv, operand_at, 16);
+        const unsigned char* const scales = s.step.scales + (among * STEP + 32 * part) * apart + (wave & (heads - 1)) * NS;
+        if constexpr (CACHE != 0) {
+            const unsigned char* own = scales + n16 * apart + kg * (D / 4) / 32;
+            kx.s = own[0];
+            ky.s = own[16 * apart];
+        }
+        load_from(kr, kb);
         dfx4 sx[NC], sy[NC];
 #pragma unroll
         for (int b = 0; b < NC; ++b) sx[b] = sy[b] = dfx4{0.f, 0.f, 0.f, 0.f};
@@ -389,9 +436,9 @@ __device__ __forceinline__ void attend(const SharedArgs& A, const Task& W, Share
             split2(M{}, e[6], e[7], ph[b].w, pl[b].w);
         }
         asm volatile("" ::: "memory");
-        vr.store_values(sv, value_at);
+        vr.store_values(sv, value_at, scales + apart / 2 + lane / LPR * apart + lane % LPR / (CACHE ? LPR / NS : 1), apart);
         asm volatile("" ::: "memory");
-        vr.load(vb, vs, at);
+        load_from(vr, vb);
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
             const lds_char from = (lds_char)sv + (tr_at ^ (unsigned)(i * 32));
@@ -424,34 +471,35 @@ __device__ __forceinline__ void attend(const SharedArgs& A, const Task& W, Share
             s.sum.l[wave][n16] = lsum[b];
         }
         __syncthreads();
-        const int row = W.row0 + 16 * b + qi;
-        if (row >= W.rows) continue;
-        float most = s.sum.m[0][qi];
+        // 16 threads an item: a query head of one of the KV heads
+        const int here = min(16, W.rows - W.row0 - 16 * b);
+        for (int item = qi; item < heads * here; item += 16) {
+            const int head = item / here, n = item - head * here, row = W.row0 + 16 * b + n;
+            float most = s.sum.m[head][n];
+            for (int w = head + heads; w < kWaves; w += heads) most = fmaxf(most, s.sum.m[w][n]);
+            float Lq = 0.f, o[DT];
 #pragma unroll
-        for (int w = 1; w < kWaves; ++w) most = fmaxf(most, s.sum.m[w][qi]);
-        float Lq = 0.f, o[DT];
+            for (int d = 0; d < DT; ++d) o[d] = 0.f;
+            for (int w = head; w < kWaves; w += heads) {
+                const float f = __builtin_amdgcn_exp2f(s.sum.m[w][n] - most);
+                Lq += s.sum.l[w][n] * f;
 #pragma unroll
-        for (int d = 0; d < DT; ++d) o[d] = 0.f;
+                for (int d = 0; d < DT; ++d) o[d] += s.sum.acc[w][n][d0 + d] * f;
+            }
+            const int64_t hq = head_of(row, W.kvh + head);
+            if (W.slot < 0) {
+                const float inv = Lq == 0.f ? 0.f : 1.f / Lq;      // (no rows; a sum that is NaN makes the row's answer NaN)
+                elem* out = reinterpret_cast<elem*>(A.out) + hq * D + d0;
 #pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            const float f = __builtin_amdgcn_exp2f(s.sum.m[w][qi] - most);
-            Lq += s.sum.l[w][qi] * f;
+                for (int d = 0; d < DT; ++d) out[d] = (elem)(o[d] * inv);
+                if (A.lse && (tid & 15) == 0)
+                    A.lse[hq] = Lq == 0.f ? -INFINITY : (most + __builtin_amdgcn_logf(Lq)) * 0.6931471805599453f;
+            } else {
+                float* pa = A.part_acc + (hq * A.slots + W.slot) * D + d0;
 #pragma unroll
-            for (int d = 0; d < DT; ++d) o[d] += s.sum.acc[w][qi][d0 + d] * f;
-        }
-        const int64_t hq = head_of(row);
-        if (W.slot < 0) {
-            const float inv = Lq == 0.f ? 0.f : 1.f / Lq;      // (no rows; a sum that is NaN makes the row's answer NaN)
-            elem* out = reinterpret_cast<elem*>(A.out) + hq * D + d0;
-#pragma unroll
-            for (int d = 0; d < DT; ++d) out[d] = (elem)(o[d] * inv);
-            if (A.lse && (tid & 15) == 0)
-                A.lse[hq] = Lq == 0.f ? -INFINITY : (most + __builtin_amdgcn_logf(Lq)) * 0.6931471805599453f;
-        } else {
-            float* pa = A.part_acc + (hq * A.slots + W.slot) * D + d0;
-#pragma unroll
-            for (int d = 0; d < DT; ++d) pa[d] = o[d];
-            if ((tid & 15) == 0) A.part_ml[hq * A.slots + W.slot] = make_float2(most, Lq);
+                for (int d = 0; d < DT; ++d) pa[d] = o[d];
+                if ((tid & 15) == 0) A.part_ml[hq * A.slots + W.slot] = make_float2(most, Lq);
+            }
         }
     }
 }
@@ -485,24 +533,27 @@ template <typename T, int D> struct Fetch<T, 0, D> {
     typedef typename Rows<2 * D>::Place Place;
     const char *kb, *vb;
     int first;                                        // row of the lane's first load
-    Place p[PER];
+    Place pk[PER], pv[PER];
     __device__ __forceinline__ Fetch(const SharedArgs& A, const Task& W, int wave, int lane) {
         first = wave * RPL + lane / PIECES;           // (rows of the others have the same places)
         kb = A.k + W.kvh * (2 * D) + ((lane % PIECES) ^ (first & (PIECES - 1))) * 16;
         vb = A.v + W.kvh * (2 * D) + place_of<D>(first, lane % PIECES) * 16;
     }
-    __device__ __forceinline__ void look_up(const Rows<2 * D>& rows, int key) {
+    // Keys from row k on, values from row v on.
+    __device__ __forceinline__ void look_up(const Rows<2 * D>& rows, int k, int v) {
 #pragma unroll
-        for (int i = 0; i < PER; ++i) p[i] = rows.look_up(key + i * RPL * kWaves + first);
+        for (int i = 0; i < PER; ++i) {
+            pk[i] = rows.look_up(k + i * RPL * kWaves + first);
+            pv[i] = rows.look_up(v + i * RPL * kWaves + first);
+        }
     }
     __device__ __forceinline__ void start(const Rows<2 * D>& rows, char* k, char* v, int wave) {
         typedef __attribute__((address_space(1))) void* from;
         typedef __attribute__((address_space(3))) void* to;
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            const int64_t at = rows.place(p[i]);
-            __builtin_amdgcn_global_load_lds((from)(kb + at), (to)(k + (i * kWaves + wave) * 1024), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((from)(vb + at), (to)(v + (i * kWaves + wave) * 1024), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((from)(kb + rows.place(pk[i])), (to)(k + (i * kWaves + wave) * 1024), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((from)(vb + rows.place(pv[i])), (to)(v + (i * kWaves + wave) * 1024), 16, 0, 0);
         }
     }
     // (such loads write no register that the compiler would wait for, and a barrier alone does not wait)
@@ -514,7 +565,7 @@ template <typename T, int CACHE, int D> struct Fetch {
     int key, block, tensor;
     const char* base[N];
     const unsigned char* scales[N];
-    Place p;
+    Place p[N];
     unsigned w[N][W4], s[N];
     __device__ __forceinline__ Fetch(const SharedArgs& A, const Task& W, int wave, int lane) {
         const int tid = wave * 64 + lane;
@@ -527,11 +578,14 @@ template <typename T, int CACHE, int D> struct Fetch {
             scales[n] = (tensor + n == 0 ? A.k_scales : A.v_scales) + W.kvh * BLOCKS + block;
         }
     }
-    __device__ __forceinline__ void look_up(const Rows<ROW>& rows, int first) { p = rows.look_up(first + key); }
+    __device__ __forceinline__ void look_up(const Rows<ROW>& rows, int k, int v) {
+#pragma unroll
+        for (int n = 0; n < N; ++n) p[n] = rows.look_up((tensor + n == 0 ? k : v) + key);
+    }
     __device__ __forceinline__ void start(const Rows<ROW>& rows, char*, char*, int) {
-        const int64_t at = rows.place(p);
 #pragma unroll
         for (int n = 0; n < N; ++n) {
+            const int64_t at = rows.place(p[n]);
 #pragma unroll
             for (int i = 0; i < W4 / 4; ++i) {
                 const uint4 x = *reinterpret_cast<const uint4*>(base[n] + at + 16 * i);
@@ -602,7 +656,7 @@ __device__ __forceinline__ void attend_wide(const SharedArgs& A, const Task& W, 
     const unsigned v_at = vr * (2 * D) + place_of<D>(vr, 2 * ((lane >> 4) & 1) + (lane & 3) / 2) * 16 + (lane & 1) * 8;
     constexpr unsigned kTurn = D == 128 ? 16 : 0;     // (what rows 8 further down differ by)
 
-    auto probabilities = [&](const fx16& x, float* e, float* sum) {
+    auto probabilities = [&](const fx16& x, float* e, float* sum) __attribute__((always_inline)) {
         const float shift = kShift - m;
 #pragma unroll
         for (int r = 0; r < 16; ++r) e[r] = __builtin_fmaf(x[r], A.scale2, shift);
@@ -613,21 +667,37 @@ __device__ __forceinline__ void attend_wide(const SharedArgs& A, const Task& W, 
 #pragma unroll
         for (int r = 2; r < 16; ++r) sum[r & 1] += e[r];
     };
-    auto block = [&](int key, const char* sk, const char* sv) {
-        fx16 x;
+    auto k_frag = [&](const char* sk, int c) __attribute__((always_inline)) { return *reinterpret_cast<const frag*>(sk + (k_at ^ (unsigned)(c * 32))); };
+    auto v_frag = [&](const char* sv, int n) __attribute__((always_inline)) {      // 32 columns n % ND of 16 keys n / ND
+        const unsigned at = (v_at ^ (unsigned)(n % ND * 64)) + n / ND * 16 * (2 * D);
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)((lds_char)sv + at));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)((lds_char)sv + (at ^ kTurn) + 8 * (2 * D)));
+        return __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+    };
+    fx16 x;                                           // logits of the wave's next block of keys
+    auto product = [&](frag kf, int c) __attribute__((always_inline)) {
+        fx16 z;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) x[r] = 0.f;
+        for (int r = 0; r < 16; ++r) z[r] = 0.f;
 #pragma unroll
-        for (int c = 0; c < NQ; ++c) {
-            const frag kf = *reinterpret_cast<const frag*>(sk + (k_at ^ (unsigned)(c * 32)));
+        for (int i = 0; i < K::kQ; ++i) x = mma32(M{}, kf, qf[c][i], c == 0 && i == 0 ? z : x);
+    };
+    auto hide = [&](int key) __attribute__((always_inline)) {                      // logits of keys behind the end
+        if (key + 32 <= W.end) return;
+        asm volatile("");                             // (a branch: 32 instructions otherwise)
 #pragma unroll
-            for (int i = 0; i < K::kQ; ++i) x = mma32(M{}, kf, qf[c][i], x);
-        }
-        if (key + 32 > W.end) {
+        for (int r = 0; r < 16; ++r)
+            if (key + 8 * (r / 4) + 4 * h2 + r % 4 >= W.end) x[r] = -INFINITY;
+    };
+    // The softmax of the block whose logits are there, which only vector instructions do, then the products of the wave's next block's logits and
+    // of this one's part of the output, which only matrix instructions do: the other wave of the SIMD is in the other half
+    // meanwhile, and goes second.  Operands are read from LDS AHEAD products before their own.
+    constexpr int NV = 2 * ND, AHEAD = 3;
+    auto pass = [&](int next, const char* sk, const char* sv) __attribute__((always_inline)) {
+        frag kf[NQ], vf[NV], pf[2][K::kQ];
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-                if (key + 8 * (r / 4) + 4 * h2 + r % 4 >= W.end) x[r] = -INFINITY;
-        }
+        for (int i = 0; i < AHEAD; ++i) kf[i] = k_frag(sk, i);
+        __builtin_amdgcn_sched_barrier(0);
         float e[16], sum[2];
         probabilities(x, e, sum);
         // A row's maximum is looked for, and its sums moved to it, only when they outgrow kMost.  (A row's two lanes have other halves of the keys.)
@@ -648,14 +718,13 @@ __device__ __forceinline__ void attend_wide(const SharedArgs& A, const Task& W, 
             probabilities(x, e, sum);
         }
         lsum += sum[0] + sum[1];
-        frag pf[2][K::kQ];
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
             if constexpr (K::kQ == 1) {
-                typedef __attribute__((ext_vector_type(8))) typename std::conditional<kF16, _Float16, __bf16>::type rounded;
-                rounded y;
+                typedef typename std::conditional<kF16, _Float16, __bf16>::type elem;
+                __attribute__((ext_vector_type(8))) elem y;
 #pragma unroll
-                for (int r = 0; r < 8; ++r) y[r] = (typename std::conditional<kF16, _Float16, __bf16>::type)e[8 * j + r];
+                for (int r = 0; r < 8; ++r) y[r] = (elem)e[8 * j + r];
                 pf[j][0] = __builtin_bit_cast(frag, y);
             } else {
                 unsigned hi[4], lo[4];
@@ -665,36 +734,56 @@ __device__ __forceinline__ void attend_wide(const SharedArgs& A, const Task& W, 
                 pf[j][K::kQ - 1] = __builtin_bit_cast(frag, make_uint4(lo[0], lo[1], lo[2], lo[3]));
             }
         }
+        __builtin_amdgcn_s_setprio(1);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
+        for (int i = 0; i < NQ; ++i) {
+            if (i + AHEAD < NQ) kf[i + AHEAD] = k_frag(sk, i + AHEAD);
+            else vf[i + AHEAD - NQ] = v_frag(sv, i + AHEAD - NQ);
+            product(kf[i], i);
+            __builtin_amdgcn_sched_barrier(0);
+        }
 #pragma unroll
-            for (int i = 0; i < ND; ++i) {
-                const unsigned at = (v_at ^ (unsigned)(i * 64)) + 16 * j * (2 * D);
-                const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)((lds_char)sv + at));
-                const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)((lds_char)sv + (at ^ kTurn) + 8 * (2 * D)));
-                const frag vf = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+        for (int i = 0; i < NV; ++i) {
+            if (i + AHEAD < NV) vf[i + AHEAD] = v_frag(sv, i + AHEAD);
 #pragma unroll
-                for (int n = 0; n < K::kQ; ++n) acc[i] = mma32(M{}, vf, pf[j][n], acc[i]);
-            }
+            for (int n = 0; n < K::kQ; ++n) acc[i % ND] = mma32(M{}, vf[i], pf[i / ND][n], acc[i % ND]);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        __builtin_amdgcn_s_setprio(0);
+        hide(next);
     };
+    // Keys are a block of every wave set ahead of values: tile t of V is keys 64 t on, that of K keys 64 t + EARLY on, whose logits are taken meanwhile.
+    // The next tiles arrive in the other two buffers.
+    constexpr int EARLY = 32 * KS;
     const int tiles = (W.end - W.begin + kKeys - 1) / kKeys;
-    fetch.look_up(rows, W.begin);
+    fetch.look_up(rows, W.begin, W.begin);
+    fetch.start(rows, s.tile.k[1], s.tile.v[0], wave);
+    fetch.look_up(rows, W.begin + EARLY, W.begin);
+    fetch.finish(s.tile.k[1], s.tile.v[0]);
     fetch.start(rows, s.tile.k[0], s.tile.v[0], wave);
-    fetch.look_up(rows, W.begin + kKeys);
+    fetch.look_up(rows, W.begin + kKeys + EARLY, W.begin + kKeys);
+    __syncthreads();
+    if (busy) {
+        const char* sk = s.tile.k[1] + (KS == 1 ? 0 : ks) * 32 * (2 * D);
+#pragma unroll
+        for (int i = 0; i < NQ; ++i) product(k_frag(sk, i), i);
+        hide(W.begin + (KS == 1 ? 0 : ks) * 32);
+    }
     fetch.finish(s.tile.k[0], s.tile.v[0]);
     __syncthreads();
-    auto tile = [&](int t, int now) {
+    auto tile = [&](int t, int now) __attribute__((always_inline)) {
         const int key = W.begin + t * kKeys;
         char *k_now = s.tile.k[now], *v_now = s.tile.v[now], *k_next = s.tile.k[now ^ 1], *v_next = s.tile.v[now ^ 1];
         if (t + 1 < tiles) {
             fetch.start(rows, k_next, v_next, wave);
-            fetch.look_up(rows, key + 2 * kKeys);
+            fetch.look_up(rows, key + 2 * kKeys + EARLY, key + 2 * kKeys);
         }
         if (busy) {
 #pragma unroll
             for (int i = 0; i < 2 / KS; ++i) {
                 const int b = KS == 1 ? i : ks;
-                if (key + 32 * b < W.end) block(key + 32 * b, k_now + 32 * b * (2 * D), v_now + 32 * b * (2 * D));
+                if (key + 32 * b < W.end) pass(key + 32 * b + EARLY, k_now + 32 * b * (2 * D), v_now + 32 * b * (2 * D));
             }
         }
         if (t + 1 < tiles) fetch.finish(k_next, v_next);
@@ -738,14 +827,16 @@ __device__ __forceinline__ void attend_wide(const SharedArgs& A, const Task& W, 
 }
 
 // The share of a sequence's own rows that workgroup i of those for them takes; false: none.
-template <bool SHARED> __device__ __forceinline__ bool own_task(const SharedArgs& A, unsigned i, Task& W) {
+template <int CACHE, bool SHARED> __device__ __forceinline__ bool own_task(const SharedArgs& A, unsigned i, Task& W) {
     // A share's heads run on one XCD (workgroup i runs on XCD i % 8), which then reads whole lines of all heads; a sequence has
     // an odd number of places, so that the first shares, which are all that short sequences have, do not meet on a few XCDs.
-    W.kvh = i % A.Hkv;
-    int chunk = i / A.Hkv;
+    const int shift = CACHE ? A.head_shift : 0, sets = A.Hkv >> shift;
+    W.shift = shift;
+    W.kvh = (i % sets) << shift;
+    int chunk = i / sets;
     if (A.by_xcd) {
-        W.kvh = i / 8 % A.Hkv;
-        chunk = i / (8 * A.Hkv) * 8 + i % 8;
+        W.kvh = (i / 8 % sets) << shift;
+        chunk = i / (8 * sets) * 8 + i % 8;
     }
     W.b0 = chunk / A.places;
     chunk %= A.places;
@@ -774,8 +865,12 @@ template <int R> __device__ __forceinline__ bool prefix_task(const SharedArgs& A
         chunk = i / (8 * units) * 8 + i % 8;
         j = i / 8 % units;
     }
-    const int tile = j % A.tiles;
+    // (from one head and share to the next the tiles are turned: places without a tile would else meet on a few of the chip's parts, which
+    // get workgroups in turn whether they return at once or not)
+    const unsigned unit = (A.prefix_by_xcd ? i / 8 : i) / A.tiles;
+    const int tile = (j + unit + unit / 4) % A.tiles;
     W.kvh = j / A.tiles;
+    W.shift = 0;
     if (chunk >= A.prefix_chunks) return false;
     auto at = [&](int i) { return A.cu ? clamped(A.cu[i], A.B) : (i == 0 ? 0 : A.B); };
     auto first = [&](int i) { return i + (int)((int64_t)at(i) * A.g / R); };
@@ -806,7 +901,7 @@ template <typename T, int CACHE, int D>
 __global__ __launch_bounds__(kWaves * 64, D == 64 ? 4 : 3) void cached_attn(const SharedArgs A) {
     __shared__ __align__(256) Shared<D> s;
     Task W;
-    if (own_task<false>(A, blockIdx.x, W)) attend<T, CACHE, D, 1>(A, W, s);
+    if (own_task<CACHE, false>(A, blockIdx.x, W)) attend<T, CACHE, D, 1>(A, W, s);
 }
 
 // R: query heads of a tile.
@@ -819,20 +914,21 @@ __global__ __launch_bounds__(kWaves * 64, R == 16 ? (D == 64 ? 4 : 3) : 2) void 
     } s;
     Task W;
     if (blockIdx.x >= A.prefix_groups) {
-        if (own_task<true>(A, blockIdx.x - A.prefix_groups, W)) attend<T, CACHE, D, 1>(A, W, s.own);
+        if (own_task<CACHE, true>(A, blockIdx.x - A.prefix_groups, W)) attend<T, CACHE, D, 1>(A, W, s.own);
     } else if (prefix_task<R>(A, blockIdx.x, threadIdx.x & 63, W)) {
         if constexpr (kWide) attend_wide<T, CACHE, D, R / 32>(A, W, s.prefix);
         else attend<T, CACHE, D, R / 16>(A, W, s.prefix);
     }
 }
 
-// Joins the partials of a query head: a workgroup for each, its waves a quarter of them, eight outputs in flight at a time.
+// Joins the partials of a query head: a workgroup for each, a part of its threads every 8th (heads of 64: 16th) partial, four elements a thread, eight in
+// flight at a time, the first ones before the largest maximum is known.
 template <typename T, int CACHE, int D, bool SHARED>
-__global__ __launch_bounds__(kWaves * 64) void cached_join(const SharedArgs A) {
+__global__ __launch_bounds__(256) void cached_join(const SharedArgs A) {
     typedef typename kind<T, CACHE>::elem elem;
-    constexpr int E = D / 64, BATCH = 8;
+    constexpr int LANES = D / 4, PARTS = 256 / LANES, BATCH = 8;
     const int64_t hq = blockIdx.x;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, b = (int)(hq / A.Hq);
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, b = (int)(hq / A.Hq), part = tid / LANES;
     const int S = clamped(A.lens[b], A.max_len);
     const int share = share_of(S, A.nchunk, A.least);
     int n = (S + share - 1) / share, before = 0;
@@ -852,71 +948,89 @@ __global__ __launch_bounds__(kWaves * 64) void cached_join(const SharedArgs A) {
     } else if (n <= 1) {
         return;
     }
-    auto slot = [&](int i) { return i < before ? i : A.prefix_chunks + (i - before); };
     const float2* ml = A.part_ml + hq * A.slots;
-    const float* pa = A.part_acc + hq * A.slots * D + lane * E;
+    const float* pa = A.part_acc + hq * A.slots * D + tid % LANES * 4;
+    float2 p[BATCH];
+    float4 x[BATCH];
+    auto fetch = [&](int first) {
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            const int at = first + i * PARTS + part, s = at < before ? at : A.prefix_chunks + (at - before);
+            p[i] = make_float2(-3.4028235e38f, 0.f);
+            x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (at < n) {
+                p[i] = ml[s];
+                x[i] = *reinterpret_cast<const float4*>(pa + (int64_t)s * D);
+            }
+        }
+    };
+    fetch(0);
     float M = -3.4028235e38f;
-    for (int i = lane; i < n; i += 64) M = fmaxf(M, ml[slot(i)].x);
+#pragma unroll
+    for (int i = 0; i < BATCH; ++i) M = fmaxf(M, p[i].x);
+    for (int i = PARTS * BATCH + tid; i < n; i += 256) M = fmaxf(M, ml[i < before ? i : A.prefix_chunks + (i - before)].x);
 #pragma unroll
     for (int d = 32; d >= 1; d >>= 1) M = fmaxf(M, __shfl_xor(M, d));
-    float Lq = 0.f, o[E];
-#pragma unroll
-    for (int e = 0; e < E; ++e) o[e] = 0.f;
-    for (int i0 = wave * BATCH; i0 < n; i0 += kWaves * BATCH) {
-        float2 p[BATCH];
-        float x[BATCH][E];
-#pragma unroll
-        for (int i = 0; i < BATCH; ++i) {
-            const int64_t c = slot(i0 + i < n ? i0 + i : n - 1);
-            p[i] = ml[c];
-#pragma unroll
-            for (int e = 0; e < E; ++e) x[i][e] = pa[c * D + e];
-        }
+    __shared__ float s_m[kWaves], s_l[PARTS], s_o[PARTS][D];
+    if (lane == 0) s_m[wave] = M;
+    __syncthreads();
+    M = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
+    float Lq = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int first = 0;;) {
 #pragma unroll
         for (int i = 0; i < BATCH; ++i) {
-            if (i0 + i >= n) break;
             const float f = __builtin_amdgcn_exp2f(p[i].x - M);
             Lq += p[i].y * f;
-#pragma unroll
-            for (int e = 0; e < E; ++e) o[e] += x[i][e] * f;
+            o = make_float4(o.x + x[i].x * f, o.y + x[i].y * f, o.z + x[i].z * f, o.w + x[i].w * f);
         }
+        first += PARTS * BATCH;
+        if (first >= n) break;
+        fetch(first);
     }
-    __shared__ float s_o[kWaves][D], s_l[kWaves];
-#pragma unroll
-    for (int e = 0; e < E; ++e) s_o[wave][lane * E + e] = o[e];
-    if (lane == 0) s_l[wave] = Lq;
+    *reinterpret_cast<float4*>(&s_o[part][tid % LANES * 4]) = o;
+    if (tid % LANES == 0) s_l[part] = Lq;
     __syncthreads();
-    Lq = s_l[0] + s_l[1] + s_l[2] + s_l[3];
-    if (threadIdx.x < D) {
-        const int d = threadIdx.x;
-        const float y = s_o[0][d] + s_o[1][d] + s_o[2][d] + s_o[3][d];
-        float z = Lq == 0.f ? 0.f : y / Lq;
-        // (probabilities that were rounded up can carry a mean of numbers near fp16's largest past it; infinities stay)
-        if (CACHE == 0 && std::is_same<T, dec_f16>::value && __builtin_fabsf(z) < INFINITY) z = __builtin_amdgcn_fmed3f(z, -65504.f, 65504.f);
-        reinterpret_cast<elem*>(A.out)[hq * D + d] = (elem)z;
+    if (tid >= D) return;
+    float y = 0.f;
+    Lq = 0.f;
+#pragma unroll
+    for (int i = 0; i < PARTS; ++i) {
+        y += s_o[i][tid];
+        Lq += s_l[i];
     }
-    if (A.lse && threadIdx.x == 0) A.lse[hq] = Lq == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(Lq)) * 0.6931471805599453f;
+    y = Lq == 0.f ? 0.f : y / Lq;
+    // (probabilities that were rounded up can carry a mean of numbers near fp16's largest past it; infinities stay)
+    if (CACHE == 0 && std::is_same<T, dec_f16>::value && __builtin_fabsf(y) < INFINITY) y = __builtin_amdgcn_fmed3f(y, -65504.f, 65504.f);
+    reinterpret_cast<elem*>(A.out)[hq * D + tid] = (elem)y;
+    if (A.lse && tid == 0) A.lse[hq] = Lq == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(Lq)) * 0.6931471805599453f;
 }
 
 }  // namespace
 
-// Shares of a sequence's own rows: as many as give 1024 workgroups if all sequences are as long as they may be, of 128 to 1024 keys (512 where
-// even those give 2048 workgroups), but no more than give 16384 workgroups, or seven; a sequence of up to 512 rows is not cut.  Shares of a prefix: as
+// Sequences that can be long or many (keys of all KV heads, from here on) have shares of at most 512 keys, and, over codes, workgroups that
+// take four KV heads together, a wave each (or two): one fetch of scales for all, and whole lines of 4-bit codes.  Microseconds with one / two / four
+// heads: 8 x 16000 rows, 32 heads, 4 bits 152 / 129 / 126, 8 bits 215 / 197 / 193; 131072 rows, 8 heads, 4 bits 43 / 39 / 40, 8 bits 70 / 65 / 61; 32
+// sequences of 1 to 16384 rows, 8 heads, 8 bits 73 / 71 / 70.  Fewer keys: 8 x 4000 rows of 4 bits, 8 heads 16.8 / 17.8 / 20.9, 2 x 30000 22.4 / 22.0 / 24.5.
+constexpr int64_t kManyKeys = 1 << 20;
+
+// Shares of a sequence's own rows: as many as give 1024 workgroups if all sequences are as long as they may be, of 128 to 1024 keys,
+// but no more than give 16384 workgroups, or seven; a sequence of up to 512 rows is not cut.  Shares of a prefix: as
 // many as give 1024 workgroups with all tiles and KV heads, of 128 keys at least, no more than 256.
 SharedPlan shared_plan(int B, int G, int Hq, int Hkv, int D, int64_t max_prefix, int64_t max_len) {
     SharedPlan P{};
     const int g = Hq / Hkv;
     const int64_t pairs = (int64_t)B * Hkv, keys = pairs * max_len;
     int64_t chunk = std::max<int64_t>(128, (keys / 1024 + 127) / 128 * 128);
-    chunk = std::min<int64_t>(chunk, keys >= 2048 * 1024 ? 512 : 1024);
+    chunk = std::min<int64_t>(chunk, keys >= kManyKeys ? 512 : 1024);
     if (max_len <= 512) chunk = 512;
     P.nchunk = (int)std::min((max_len + chunk - 1) / chunk, std::max<int64_t>(7, 16384 / pairs));
     P.least = P.nchunk == 1 || pairs > 128 ? 512 : (pairs > 64 ? 256 : 128);
     if (G > 0) {
         const int64_t rows = ((int64_t)B * g + G - 1) / G;    // of a group, on the average
         P.columns = rows <= 16 ? 16 : (rows <= 32 ? 32 : (rows <= 64 ? 64 : 128));
-        P.tiles = (int)(G + (int64_t)B * g / P.columns);
-        const int64_t units = (int64_t)P.tiles * Hkv;
+        P.tiles = (int)(G - 1 + ((int64_t)B * g + P.columns - 1) / P.columns);
+        const int64_t units = (rows + P.columns - 1) / P.columns * G * Hkv;   // (as many tiles as groups of the average size have)
         const int64_t most = P.columns <= 32 ? 1024 : 512;
         P.prefix_chunks = (int)std::max<int64_t>(1, std::min<int64_t>({256, (max_prefix + 127) / 128, (most + units - 1) / units}));
         P.prefix_least = 128;
@@ -946,13 +1060,14 @@ hipError_t launch_shared(int dtype, int cache, int D, SharedArgs A, void* worksp
     A.scale2 = (float)(1.4426950408889634 / std::sqrt((double)D));
     A.part_acc = static_cast<float*>(workspace);
     A.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + P.acc_bytes);
+    A.head_shift = cache != 0 && (int64_t)A.B * A.Hkv * A.max_len >= kManyKeys ? (A.Hkv % 4 == 0 ? 2 : (A.Hkv % 2 == 0 ? 1 : 0)) : 0;
     A.by_xcd = (int64_t)P.nchunk * A.B >= 8;
     A.places = A.by_xcd ? P.nchunk | 1 : P.nchunk;
     int64_t units = (int64_t)A.places * A.B;
     if (A.by_xcd) units = (units + 7) / 8 * 8;
     A.prefix_by_xcd = P.prefix_chunks >= 8;
     A.prefix_groups = (unsigned)((A.prefix_by_xcd ? (P.prefix_chunks + 7) / 8 * 8 : P.prefix_chunks) * (int64_t)P.tiles * A.Hkv);
-    const dim3 grid((unsigned)(A.prefix_groups + units * A.Hkv)), block(kWaves * 64), heads((unsigned)((int64_t)A.B * A.Hq));
+    const dim3 grid((unsigned)(A.prefix_groups + units * (A.Hkv >> A.head_shift))), block(kWaves * 64), heads((unsigned)((int64_t)A.B * A.Hq));
     auto form = [&](auto t, auto c, auto d) {
         typedef decltype(t) T;
         constexpr int C = decltype(c)::value, DD = decltype(d)::value;
