@@ -516,13 +516,20 @@ __device__ __forceinline__ fx16 mma32(dec_f16, frag a, frag b, fx16 c) {
 // LDS of a workgroup that meets a prefix's rows with 64 or 128 query heads: two tiles each of keys and values, and behind the loop the
 // waves' sums.
 constexpr int kKeys = 64;      // keys of a tile
-template <int D> union Wide {
-    struct {
-        char k[2][kKeys * 2 * D], v[2][kKeys * 2 * D];
-    } tile;
-    struct {
-        float acc[kWaves][32][D], m[kWaves][32], l[kWaves][32];
-    } sum;
+constexpr int kPlaces = 4 * kKeys;
+template <int D> struct Wide {
+    union {
+        struct {
+            char k[2][kKeys * 2 * D], v[2][kKeys * 2 * D];
+        } tile;
+        float acc[kWaves][32][D];
+    };
+    union {
+        int64_t places[kPlaces];                      // of the rows around the tiles: row r's is number r % kPlaces
+        struct {
+            float m[kWaves][32], l[kWaves][32];
+        } sum;
+    };
 };
 
 // A lane's part of a tile on its way from the pool to LDS.  Plain rows go there by themselves, 16 bytes a lane at a time; codes pass
@@ -530,30 +537,27 @@ template <int D> union Wide {
 template <typename T, int CACHE, int D> struct Fetch;
 template <typename T, int D> struct Fetch<T, 0, D> {
     static constexpr int PIECES = D / 8, RPL = 64 / PIECES, PER = kKeys / (RPL * kWaves);   // 16-byte pieces of a row; rows of a load; loads
-    typedef typename Rows<2 * D>::Place Place;
     const char *kb, *vb;
     int first;                                        // row of the lane's first load
-    Place pk[PER], pv[PER];
     __device__ __forceinline__ Fetch(const SharedArgs& A, const Task& W, int wave, int lane) {
         first = wave * RPL + lane / PIECES;           // (rows of the others have the same places)
         kb = A.k + W.kvh * (2 * D) + ((lane % PIECES) ^ (first & (PIECES - 1))) * 16;
         vb = A.v + W.kvh * (2 * D) + place_of<D>(first, lane % PIECES) * 16;
     }
-    // Keys from row k on, values from row v on.
-    __device__ __forceinline__ void look_up(const Rows<2 * D>& rows, int k, int v) {
-#pragma unroll
-        for (int i = 0; i < PER; ++i) {
-            pk[i] = rows.look_up(k + i * RPL * kWaves + first);
-            pv[i] = rows.look_up(v + i * RPL * kWaves + first);
-        }
-    }
-    __device__ __forceinline__ void start(const Rows<2 * D>& rows, char* k, char* v, int wave) {
+    // Keys of rows from k on, values of rows from v on.
+    __device__ __forceinline__ void start(const int64_t* places, int k, int v, char* to_k, char* to_v, int wave) {
         typedef __attribute__((address_space(1))) void* from;
         typedef __attribute__((address_space(3))) void* to;
+        int64_t pk[PER], pv[PER];
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            __builtin_amdgcn_global_load_lds((from)(kb + rows.place(pk[i])), (to)(k + (i * kWaves + wave) * 1024), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((from)(vb + rows.place(pv[i])), (to)(v + (i * kWaves + wave) * 1024), 16, 0, 0);
+            pk[i] = places[(k + i * RPL * kWaves + first) & (kPlaces - 1)];
+            pv[i] = places[(v + i * RPL * kWaves + first) & (kPlaces - 1)];
+        }
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            __builtin_amdgcn_global_load_lds((from)(kb + pk[i]), (to)(to_k + (i * kWaves + wave) * 1024), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((from)(vb + pv[i]), (to)(to_v + (i * kWaves + wave) * 1024), 16, 0, 0);
         }
     }
     // (such loads write no register that the compiler would wait for, and a barrier alone does not wait)
@@ -561,11 +565,9 @@ template <typename T, int D> struct Fetch<T, 0, D> {
 };
 template <typename T, int CACHE, int D> struct Fetch {
     static constexpr int ROW = row_bytes<CACHE, D>(), BLOCKS = D / 32, N = D == 128 ? 2 : 1, W4 = CACHE == 1 ? 8 : 4;   // N: blocks of a thread; its words
-    typedef typename Rows<ROW>::Place Place;
     int key, block, tensor;
     const char* base[N];
     const unsigned char* scales[N];
-    Place p[N];
     unsigned w[N][W4], s[N];
     __device__ __forceinline__ Fetch(const SharedArgs& A, const Task& W, int wave, int lane) {
         const int tid = wave * 64 + lane;
@@ -578,14 +580,10 @@ template <typename T, int CACHE, int D> struct Fetch {
             scales[n] = (tensor + n == 0 ? A.k_scales : A.v_scales) + W.kvh * BLOCKS + block;
         }
     }
-    __device__ __forceinline__ void look_up(const Rows<ROW>& rows, int k, int v) {
-#pragma unroll
-        for (int n = 0; n < N; ++n) p[n] = rows.look_up((tensor + n == 0 ? k : v) + key);
-    }
-    __device__ __forceinline__ void start(const Rows<ROW>& rows, char*, char*, int) {
+    __device__ __forceinline__ void start(const int64_t* places, int k, int v, char*, char*, int) {
 #pragma unroll
         for (int n = 0; n < N; ++n) {
-            const int64_t at = rows.place(p[n]);
+            const int64_t at = places[((tensor + n == 0 ? k : v) + key) & (kPlaces - 1)];
 #pragma unroll
             for (int i = 0; i < W4 / 4; ++i) {
                 const uint4 x = *reinterpret_cast<const uint4*>(base[n] + at + 16 * i);
@@ -757,12 +755,14 @@ __device__ __forceinline__ void attend_wide(const SharedArgs& A, const Task& W, 
     // The next tiles arrive in the other two buffers.
     constexpr int EARLY = 32 * KS;
     const int tiles = (W.end - W.begin + kKeys - 1) / kKeys;
-    fetch.look_up(rows, W.begin, W.begin);
-    fetch.start(rows, s.tile.k[1], s.tile.v[0], wave);
-    fetch.look_up(rows, W.begin + EARLY, W.begin);
+    // Places: a thread finds one of the first 256 rows, and 64 more for every tile, two tiles ahead, are shared out to the waves (the page is looked
+    // up yet a tile before).  A lane that looked up the rows it loads did as much for that as for the softmax.
+    s.places[(W.begin + tid) & (kPlaces - 1)] = rows.place(rows.look_up(W.begin + tid));
+    auto page = rows.look_up(W.begin + 4 * kKeys + 16 * wave + (lane & 15));
+    __syncthreads();
+    fetch.start(s.places, W.begin, W.begin, s.tile.k[1], s.tile.v[0], wave);
     fetch.finish(s.tile.k[1], s.tile.v[0]);
-    fetch.start(rows, s.tile.k[0], s.tile.v[0], wave);
-    fetch.look_up(rows, W.begin + kKeys + EARLY, W.begin + kKeys);
+    fetch.start(s.places, W.begin + EARLY, W.begin, s.tile.k[0], s.tile.v[0], wave);
     __syncthreads();
     if (busy) {
         const char* sk = s.tile.k[1] + (KS == 1 ? 0 : ks) * 32 * (2 * D);
@@ -776,8 +776,10 @@ __device__ __forceinline__ void attend_wide(const SharedArgs& A, const Task& W, 
         const int key = W.begin + t * kKeys;
         char *k_now = s.tile.k[now], *v_now = s.tile.v[now], *k_next = s.tile.k[now ^ 1], *v_next = s.tile.v[now ^ 1];
         if (t + 1 < tiles) {
-            fetch.start(rows, k_next, v_next, wave);
-            fetch.look_up(rows, key + 2 * kKeys + EARLY, key + 2 * kKeys);
+            fetch.start(s.places, key + kKeys + EARLY, key + kKeys, k_next, v_next, wave);
+            // (rows of tile t + 4 take the places of those of tile t, which all have read)
+            s.places[(key + 4 * kKeys + 16 * wave + (lane & 15)) & (kPlaces - 1)] = rows.place(page);
+            page = rows.look_up(key + 5 * kKeys + 16 * wave + (lane & 15));
         }
         if (busy) {
 #pragma unroll
@@ -794,7 +796,7 @@ __device__ __forceinline__ void attend_wide(const SharedArgs& A, const Task& W, 
         if (t + 1 < tiles) tile(t + 1, 1);
     }
     // The waves' sums (four floats permuted, so that the rows of a write meet all banks), and the answer, 16 bytes of a row a lane.
-    auto at = [&](int w, int line, int four) { return reinterpret_cast<float4*>(&s.sum.acc[w][line][0]) + (four ^ (line & (D / 4 - 1))); };
+    auto at = [&](int w, int line, int four) { return reinterpret_cast<float4*>(&s.acc[w][line][0]) + (four ^ (line & (D / 4 - 1))); };
     const float l = lsum + other_half(lsum);
 #pragma unroll
     for (int i = 0; i < ND; ++i)
