@@ -566,18 +566,20 @@ def _device_of(t: torch.Tensor, name: str) -> int:
     return device
 
 
-def _cache_of(k_pages, k_scales, v_pages, v_scales, Hkv: int, D: int) -> int:
-    """Which codes microscaled pages hold, by their width."""
-    pages, page_size, Hp, width = pool = k_pages.shape
-    if v_pages.shape != pool or Hp != Hkv or width not in (D, D // 2) or k_scales.shape != (pages, page_size, Hkv, D // 32) or \
-            v_scales.shape != k_scales.shape:
-        raise ValueError("microscaled pages must be codes [num_pages, page_size, Hkv, D] or [.., D / 2] and scales [.., D / 32]")
-    return CACHE_FP8 if width == D else CACHE_FP4
-
-
-def _append_args(k, v, block_table, starts, cu_seqlens, positions, cos, sin, interleaved, q, q_out, k_out):
-    """The device, and the C arguments of an append before its pages and behind them."""
+def snapkv_append_paged(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
+                        block_table: torch.Tensor, starts: torch.Tensor, cu_seqlens: Optional[torch.Tensor] = None,
+                        positions: Optional[torch.Tensor] = None, cos: Optional[torch.Tensor] = None,
+                        sin: Optional[torch.Tensor] = None, interleaved: bool = False, q: Optional[torch.Tensor] = None,
+                        q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, stream=None) -> None:
+    """k, v [T,Hkv,D] (views with contiguous rows) go into k_pages/v_pages [num_pages, page_size, Hkv, D] behind
+    block_table [B, columns] int32, sequence b's from row starts[b] on; cu_seqlens [B+1] int32, or None: a token per
+    sequence.  With cos/sin [positions, rot_dim/2] float32 the keys, and q [T,Hq,D] -> q_out, are rotated by positions [T]
+    int32 (None: the rows); k_out [T,Hkv,D]: the rotated keys once more."""
+    lib = load()
     T, Hkv, D = rows = k.shape
+    num_pages, page_size, Hp, Dp = pool = k_pages.shape
+    if v.shape != rows or Hp != Hkv or Dp != D or v_pages.shape != pool:
+        raise ValueError("k, v, k_pages and v_pages disagree on their shapes")
     if block_table.ndim != 2:
         raise ValueError("block_table must be [B, columns]")
     B, columns = block_table.shape
@@ -606,33 +608,47 @@ def _append_args(k, v, block_table, starts, cu_seqlens, positions, cos, sin, int
     qp, qr, qh = _rows(q, "q", dt, dev, T, Hq, D) if Hq else none
     op, orow, oh = _rows(q_out, "q_out", dt, dev, T, Hq, D) if Hq else none
     cp, cr, ch = _rows(k_out, "k_out", dt, dev, T, Hkv, D) if k_out is not None else none
-    before = (_dtype_code(k), qp, kp, vp, _at(cu_seqlens, "cu_seqlens", i32, dev) if cu_seqlens is not None else None,
-              _at(starts, "starts", i32, dev), _at(positions, "positions", i32, dev) if positions is not None else None, T, B,
-              Hq, Hkv, D, qr, qh, kr, kh, vr, vh,
-              _at(cos, "cos", torch.float32, dev) if cos is not None else None,
-              _at(sin, "sin", torch.float32, dev) if cos is not None else None, P, 2 * half, 1 if interleaved else 0)
-    return dev, before, (op, orow, oh, cp, cr, ch)
-
-
-def snapkv_append_paged(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
-                        block_table: torch.Tensor, starts: torch.Tensor, cu_seqlens: Optional[torch.Tensor] = None,
-                        positions: Optional[torch.Tensor] = None, cos: Optional[torch.Tensor] = None,
-                        sin: Optional[torch.Tensor] = None, interleaved: bool = False, q: Optional[torch.Tensor] = None,
-                        q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None, stream=None) -> None:
-    """k, v [T,Hkv,D] (views with contiguous rows) go into k_pages/v_pages [num_pages, page_size, Hkv, D] behind
-    block_table [B, columns] int32, sequence b's from row starts[b] on; cu_seqlens [B+1] int32, or None: a token per
-    sequence.  With cos/sin [positions, rot_dim/2] float32 the keys, and q [T,Hq,D] -> q_out, are rotated by positions [T]
-    int32 (None: the rows); k_out [T,Hkv,D]: the rotated keys once more."""
-    lib = load()
-    T, Hkv, D = rows = k.shape
-    num_pages, page_size, Hp, Dp = pool = k_pages.shape
-    if v.shape != rows or Hp != Hkv or Dp != D or v_pages.shape != pool:
-        raise ValueError("k, v, k_pages and v_pages disagree on their shapes")
-    dev, before, after = _append_args(k, v, block_table, starts, cu_seqlens, positions, cos, sin, interleaved, q, q_out, k_out)
     _check(lib.snapkv_append_paged(
-        *before, _at(k_pages, "k_pages", k.dtype, dev), _at(v_pages, "v_pages", k.dtype, dev),
-        _at(block_table, "block_table", torch.int32, dev), block_table.shape[1], num_pages, page_size, *after,
-        _stream_on(dev, stream)))
+        _dtype_code(k), qp, kp, vp, _at(cu_seqlens, "cu_seqlens", i32, dev) if cu_seqlens is not None else None,
+        _at(starts, "starts", i32, dev), _at(positions, "positions", i32, dev) if positions is not None else None, T, B,
+        Hq, Hkv, D, qr, qh, kr, kh, vr, vh,
+        _at(cos, "cos", torch.float32, dev) if cos is not None else None, _at(sin, "sin", torch.float32, dev) if cos is not None else None,
+        P, 2 * half, 1 if interleaved else 0,
+        _at(k_pages, "k_pages", dt, dev), _at(v_pages, "v_pages", dt, dev), _at(block_table, "block_table", i32, dev),
+        columns, num_pages, page_size, op, orow, oh, cp, cr, ch, _stream_on(dev, stream)))
+
+
+# The steps over microscaled pages and shared prefixes: argument checks and marshalling are compiled (csrc/snapkv_steps.cpp).  Microseconds of host
+# time, with them in Python / so: 8 tokens appended and their rows read back (two calls) 21.4 / 9.1, one token over 2113 rows 12.3 / 7.8, two users of a
+# prefix 13.1 / 8.1; the kernels of these calls take 7 to 9.
+_steps_module = None
+
+
+def _steps():
+    global _steps_module
+    if _steps_module is None:
+        load()
+        if not os.path.exists(os.path.join(_PKG, "_steps.so")):
+            raise FileNotFoundError(
+                f"{os.path.join(_PKG, '_steps.so')} is missing: build it with `python -m paper_2404_14469_amd.build` "
+                "(there is no CPU fallback)")
+        from . import _steps as module
+        _steps_module = module
+    return _steps_module
+
+
+def _stream_of(t: torch.Tensor, stream) -> int:
+    """The stream of a call on this tensor's device, which the call refuses if it is not the current one."""
+    if stream is not None:
+        return _stream(stream) or 0
+    return (_raw_stream(t.get_device()) if _raw_stream is not None else _stream(None) or 0) if t.is_cuda else 0
+
+
+def _stream_of_step(t: torch.Tensor, stream, workspace) -> int:
+    st = _stream_of(t, stream)
+    if stream is not None and workspace is None and t.is_cuda and st != (_stream(None) or 0):
+        raise ValueError("a step on another stream than the current one needs a workspace of the caller's")
+    return st
 
 
 def snapkv_append_paged_mx(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tensor, k_scales: torch.Tensor, v_pages: torch.Tensor,
@@ -643,17 +659,8 @@ def snapkv_append_paged_mx(k: torch.Tensor, v: torch.Tensor, k_pages: torch.Tens
                            k_out: Optional[torch.Tensor] = None, stream=None) -> None:
     """snapkv_append_paged into microscaled pages, all uint8: codes k_pages/v_pages [num_pages, page_size, Hkv, D] (e4m3) or
     [.., D/2] (e2m1, two to a byte) and k_scales/v_scales [num_pages, page_size, Hkv, D/32]."""
-    lib = load()
-    T, Hkv, D = k.shape
-    if v.shape != k.shape:
-        raise ValueError("k and v disagree on their shapes")
-    cache, u8 = _cache_of(k_pages, k_scales, v_pages, v_scales, Hkv, D), torch.uint8
-    dev, before, after = _append_args(k, v, block_table, starts, cu_seqlens, positions, cos, sin, interleaved, q, q_out, k_out)
-    num_pages, page_size = k_pages.shape[:2]
-    _check(lib.snapkv_append_paged_mx(
-        before[0], cache, *before[1:], _at(k_pages, "k_pages", u8, dev), _at(k_scales, "k_scales", u8, dev),
-        _at(v_pages, "v_pages", u8, dev), _at(v_scales, "v_scales", u8, dev), _at(block_table, "block_table", torch.int32, dev),
-        block_table.shape[1], num_pages, page_size, *after, _stream_on(dev, stream)))
+    _check(_steps().append_paged_mx(k, v, k_pages, k_scales, v_pages, v_scales, block_table, starts, cu_seqlens, positions, cos, sin,
+                                    interleaved, q, q_out, k_out, _stream_of(k, stream)))
 
 
 def snapkv_read_paged_mx(k_pages: torch.Tensor, k_scales: torch.Tensor, v_pages: torch.Tensor, v_scales: torch.Tensor,
@@ -661,25 +668,7 @@ def snapkv_read_paged_mx(k_pages: torch.Tensor, k_scales: torch.Tensor, v_pages:
                          cu_seqlens: Optional[torch.Tensor] = None, stream=None) -> None:
     """Rows of microscaled pages (as for snapkv_append_paged_mx) -> k_out, v_out [T,Hkv,D] (views with contiguous rows, e.g. of
     head-major storage): sequence b's from row starts[b] on, packed by cu_seqlens [B+1] int32 (None: one row per sequence)."""
-    lib = load()
-    T, Hkv, D = k_out.shape
-    if v_out.shape != k_out.shape or v_out.dtype is not k_out.dtype:
-        raise ValueError("k_out and v_out disagree on their shapes or types")
-    cache, u8, i32 = _cache_of(k_pages, k_scales, v_pages, v_scales, Hkv, D), torch.uint8, torch.int32
-    if block_table.ndim != 2:
-        raise ValueError("block_table must be [B, columns]")
-    B, columns = block_table.shape
-    if starts.shape != (B,) or (cu_seqlens is not None and cu_seqlens.shape != (B + 1,)):
-        raise ValueError("starts must be [B] and cu_seqlens [B + 1]")
-    num_pages, page_size = k_pages.shape[:2]
-    dev, dt = _device_of(k_out, "k_out"), k_out.dtype
-    kp, kr, kh = _rows(k_out, "k_out", dt, dev, T, Hkv, D)
-    vp, vr, vh = _rows(v_out, "v_out", dt, dev, T, Hkv, D)
-    _check(lib.snapkv_read_paged_mx(
-        _dtype_code(k_out), cache, _at(k_pages, "k_pages", u8, dev), _at(k_scales, "k_scales", u8, dev),
-        _at(v_pages, "v_pages", u8, dev), _at(v_scales, "v_scales", u8, dev), _at(block_table, "block_table", i32, dev), columns,
-        num_pages, page_size, _at(cu_seqlens, "cu_seqlens", i32, dev) if cu_seqlens is not None else None,
-        _at(starts, "starts", i32, dev), T, B, Hkv, D, kp, kr, kh, vp, vr, vh, _stream_on(dev, stream)))
+    _check(_steps().read_paged_mx(k_pages, k_scales, v_pages, v_scales, block_table, starts, k_out, v_out, cu_seqlens, _stream_of(k_out, stream)))
 
 
 def snapkv_prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, cu_seqlens: torch.Tensor, out: torch.Tensor,
@@ -755,43 +744,14 @@ def snapkv_decode_shared_workspace_bytes(B: int, G: int, Hq: int, Hkv: int, D: i
     return int(load().snapkv_decode_shared_workspace_bytes(B, G, Hq, Hkv, D, max_prefix, max_len))
 
 
-def _step_workspace(workspace, need, q, dev: int, stream):
-    """Address and size of a step's workspace, the stream, and what owns the memory (None given: need() bytes for this call)."""
-    st = _stream_on(dev, stream)
-    if workspace is not None:
-        return _at(workspace, "workspace", torch.uint8, dev), workspace.numel(), st, workspace
-    if stream is not None and st != _stream(None):
-        raise ValueError("a step on another stream than the current one needs a workspace of the caller's")
-    size = need()
-    if not size:
-        return None, 0, st, None
-    workspace = torch.empty(size, dtype=torch.uint8, device=q.device)
-    return workspace.data_ptr(), size, st, workspace
-
-
 def snapkv_decode_attention_paged_mx(q: torch.Tensor, k_pages: torch.Tensor, k_scales: torch.Tensor, v_pages: torch.Tensor,
                                      v_scales: torch.Tensor, block_table: torch.Tensor, lens: torch.Tensor, max_len: int,
                                      out: torch.Tensor, out_lse: Optional[torch.Tensor] = None,
                                      workspace: Optional[torch.Tensor] = None, stream=None) -> None:
     """snapkv_decode_attention_paged over microscaled pages (as for snapkv_append_paged_mx); q and out bf16 or fp16.  `workspace`: of
     snapkv_decode_paged_mx_workspace_bytes, or None, as there."""
-    lib = load()
-    max_len = int(max_len)
-    B, Hq, D = q.shape
-    num_pages, page_size, Hkv = k_pages.shape[:3]
-    cache, u8, i32 = _cache_of(k_pages, k_scales, v_pages, v_scales, Hkv, D), torch.uint8, torch.int32
-    if block_table.ndim != 2 or block_table.shape[0] != B or lens.shape != (B,):
-        raise ValueError("block_table must be [B, columns] and lens [B]")
-    if out.shape != (B, Hq, D) or (out_lse is not None and out_lse.shape != (B, Hq)):
-        raise ValueError("out must be [B, Hq, D] and out_lse [B, Hq]")
-    dev, dt = _device_of(q, "q"), q.dtype
-    ins = (_at(q, "q", dt, dev), _at(k_pages, "k_pages", u8, dev), _at(k_scales, "k_scales", u8, dev),
-           _at(v_pages, "v_pages", u8, dev), _at(v_scales, "v_scales", u8, dev), _at(block_table, "block_table", i32, dev),
-           block_table.shape[1], num_pages, page_size, _at(lens, "lens", i32, dev))
-    outs = (_at(out, "out", dt, dev), _at(out_lse, "out_lse", torch.float32, dev) if out_lse is not None else None)
-    ws, size, st, _owner = _step_workspace(
-        workspace, lambda: snapkv_decode_paged_mx_workspace_bytes(B, Hq, Hkv, D, max_len), q, dev, stream)
-    _check(lib.snapkv_decode_attention_paged_mx(_dtype_code(q), cache, *ins, max_len, B, Hq, Hkv, D, *outs, ws, size, st))
+    _check(_steps().decode_attention_paged_mx(q, k_pages, k_scales, v_pages, v_scales, block_table, lens, int(max_len), out, out_lse,
+                                              workspace, _stream_of_step(q, stream, workspace)))
 
 
 def snapkv_decode_attention_shared(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, prefix_table: torch.Tensor,
@@ -805,36 +765,8 @@ def snapkv_decode_attention_shared(q: torch.Tensor, k_pages: torch.Tensor, v_pag
     most max_len) behind block_table [B, columns].  q, out [B,Hq,D] bf16 or fp16; pages of q's type or, with k_scales and
     v_scales, microscaled ones (as for snapkv_append_paged_mx).  `workspace`: of snapkv_decode_shared_workspace_bytes; None:
     allocated by torch for this call, on the current stream."""
-    lib = load()
-    max_prefix, max_len = int(max_prefix), int(max_len)
-    B, Hq, D = q.shape
-    num_pages, page_size, Hkv, width = pool = k_pages.shape
-    i32, cache, kind = torch.int32, CACHE_PLAIN, q.dtype
-    if k_scales is not None or v_scales is not None:
-        if k_scales is None or v_scales is None:
-            raise ValueError("k_scales and v_scales must both be given")
-        cache, kind = _cache_of(k_pages, k_scales, v_pages, v_scales, Hkv, D), torch.uint8
-    elif width != D or v_pages.shape != pool:
-        raise ValueError("q, k_pages and v_pages disagree on their shapes")
-    if prefix_table.ndim != 2:
-        raise ValueError("prefix_table must be [G, columns]")
-    G = prefix_table.shape[0]
-    if prefix_lens.shape != (G,) or (cu_groups is not None and cu_groups.shape != (G + 1,)) or (cu_groups is None and G != 1):
-        raise ValueError("prefix_lens must be [G] and cu_groups [G + 1] (None: one group)")
-    if block_table.ndim != 2 or block_table.shape[0] != B or lens.shape != (B,):
-        raise ValueError("block_table must be [B, columns] and lens [B]")
-    if out.shape != (B, Hq, D) or (out_lse is not None and out_lse.shape != (B, Hq)):
-        raise ValueError("out must be [B, Hq, D] and out_lse [B, Hq]")
-    dev, dt = _device_of(q, "q"), q.dtype
-    ks, vs = (_at(k_scales, "k_scales", kind, dev), _at(v_scales, "v_scales", kind, dev)) if cache else (None, None)
-    ins = (_at(q, "q", dt, dev), _at(k_pages, "k_pages", kind, dev), ks, _at(v_pages, "v_pages", kind, dev), vs, num_pages, page_size,
-           _at(cu_groups, "cu_groups", i32, dev) if cu_groups is not None else None, G,
-           _at(prefix_table, "prefix_table", i32, dev), prefix_table.shape[1], _at(prefix_lens, "prefix_lens", i32, dev), max_prefix,
-           _at(block_table, "block_table", i32, dev), block_table.shape[1], _at(lens, "lens", i32, dev), max_len)
-    outs = (_at(out, "out", dt, dev), _at(out_lse, "out_lse", torch.float32, dev) if out_lse is not None else None)
-    ws, size, st, _owner = _step_workspace(
-        workspace, lambda: snapkv_decode_shared_workspace_bytes(B, G, Hq, Hkv, D, max_prefix, max_len), q, dev, stream)
-    _check(lib.snapkv_decode_attention_shared(_dtype_code(q), cache, *ins, B, Hq, Hkv, D, *outs, ws, size, st))
+    _check(_steps().decode_attention_shared(q, k_pages, v_pages, prefix_table, prefix_lens, int(max_prefix), block_table, lens, int(max_len),
+                                            out, out_lse, cu_groups, k_scales, v_scales, workspace, _stream_of_step(q, stream, workspace)))
 
 
 def compress(q_win, k, v, pool_kind: int, p: int, C: int, stream=None

@@ -1,4 +1,4 @@
-"""Builds libsnapkv.so for gfx950 in-tree with hipcc (cross-compiles without a GPU)."""
+"""Builds libsnapkv.so for gfx950 in-tree with hipcc (cross-compiles without a GPU), and the compiled part of the binding."""
 from __future__ import annotations
 
 import os
@@ -8,6 +8,7 @@ import sys
 PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
 LIB = os.path.join(PKG, "libsnapkv.so")
+STEPS = os.path.join(PKG, "_steps.so")   # argument checks and calls of some entries (csrc/snapkv_steps.cpp): host code against torch's headers
 SOURCES = ["snapkv_api.hip", "snapkv_geom.hip", "snapkv_fused.hip", "snapkv_wide.hip", "snapkv_select.hip", "snapkv_topk.hip",
            "snapkv_decode.hip", "snapkv_hitrate.hip", "snapkv_append.hip", "snapkv_prompt.hip", "snapkv_paged.hip", "snapkv_mx.hip",
            "snapkv_shared.hip"]
@@ -16,6 +17,18 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
          "-Wall", "-Wno-unused-command-line-argument"]
+
+
+def steps_command() -> list:
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+    lib = os.path.join(os.path.dirname(torch.__file__), "lib")
+    return ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+            *("-I" + p for p in [*cpp_extension.include_paths(), sysconfig.get_paths()["include"]]),
+            os.path.join(CSRC, "snapkv_steps.cpp"), "-o", STEPS, "-L" + lib, "-ltorch_python", "-ltorch_cpu", "-lc10", "-L" + PKG, "-lsnapkv",
+            "-Wl,-rpath,$ORIGIN"]
 
 
 def build_library(verbose: bool = False) -> str:
@@ -38,6 +51,7 @@ def build_library(verbose: bool = False) -> str:
             print(text, flush=True)
     link = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs]
     subprocess.check_call(link)
+    subprocess.check_call(steps_command())
     return LIB
 
 
