@@ -208,44 +208,41 @@ __global__ __launch_bounds__(256) void append_mx(const AppendArgs A) {
     }
 }
 
-// N values of one piece from their codes, times 2^(byte - 127).
-template <int N> __device__ __forceinline__ void load_values(mx<1>, const char* row, int at, float unit, float* y) {
-    unsigned w[N / 4];
-    if constexpr (N == 8) {
-        const uint2 x = *reinterpret_cast<const uint2*>(row + at);
-        w[0] = x.x;
-        w[1] = x.y;
-    } else {
-        w[0] = *reinterpret_cast<const unsigned*>(row + at);
-    }
-#pragma unroll
-    for (int i = 0; i < N / 4; ++i) {
-        const fx2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[i], unit, false), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w[i], unit, true);
-        y[4 * i] = a.x;
-        y[4 * i + 1] = a.y;
-        y[4 * i + 2] = b.x;
-        y[4 * i + 3] = b.y;
-    }
+// One piece's codes as they lie in a row, and the N values that they stand for, times 2^(byte - 127).
+template <int CACHE, int N> struct codes_of;
+template <> struct codes_of<1, 8> { typedef uint2 type; };
+template <> struct codes_of<1, 4> { typedef unsigned type; };
+template <> struct codes_of<2, 8> { typedef unsigned type; };
+template <> struct codes_of<2, 4> { typedef unsigned short type; };
+__device__ __forceinline__ void four_values(unsigned w, float unit, float* y) {
+    const fx2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, unit, false), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(w, unit, true);
+    y[0] = a.x;
+    y[1] = a.y;
+    y[2] = b.x;
+    y[3] = b.y;
 }
-template <int N> __device__ __forceinline__ void load_values(mx<2>, const char* row, int at, float unit, float* y) {
-    unsigned w;
-    if constexpr (N == 8) w = *reinterpret_cast<const unsigned*>(row + at / 2);
-    else w = *reinterpret_cast<const unsigned short*>(row + at / 2);
-    fx2 x[4];
-    x[0] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 0);
-    x[1] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 1);
-    if constexpr (N == 8) {
-        x[2] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 2);
-        x[3] = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 3);
-    }
-#pragma unroll
-    for (int i = 0; i < N / 2; ++i) {
-        y[2 * i] = x[i].x;
-        y[2 * i + 1] = x[i].y;
-    }
+__device__ __forceinline__ void values(mx<1>, uint2 w, float unit, float* y) {
+    four_values(w.x, unit, y);
+    four_values(w.y, unit, y + 4);
+}
+__device__ __forceinline__ void values(mx<1>, unsigned w, float unit, float* y) { four_values(w, unit, y); }
+__device__ __forceinline__ void values(mx<2>, unsigned short w, float unit, float* y) {
+    const fx2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 1);
+    y[0] = a.x;
+    y[1] = a.y;
+    y[2] = b.x;
+    y[3] = b.y;
+}
+__device__ __forceinline__ void values(mx<2>, unsigned w, float unit, float* y) {
+    values(mx<2>{}, (unsigned short)w, unit, y);
+    const fx2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 2), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, unit, 3);
+    y[4] = a.x;
+    y[5] = a.y;
+    y[6] = b.x;
+    y[7] = b.y;
 }
 
-// A wave takes a token, a lane one piece of a head at a time.
+// A wave takes a token, a lane one piece of a head at a time, and of four heads before the first is stored.
 template <typename T, int CACHE, int D>
 __global__ __launch_bounds__(256) void read_mx(const AppendArgs A) {
     typedef piece_of<T> piece;
@@ -269,18 +266,30 @@ __global__ __launch_bounds__(256) void read_mx(const AppendArgs A) {
     if (page < 0 || page >= A.pages) return;
     const int64_t slot = page * A.page + (row - pg * A.page);
     const int c = lane % P;
-    for (int h = part * HW + lane / P; h < 2 * A.Hkv; h += A.parts * HW) {
-        const bool is_k = h < A.Hkv;
-        const int hh = is_k ? h : h - A.Hkv;
-        const int64_t at = slot * A.Hkv + hh;
-        const unsigned s = (is_k ? A.k_scales : A.v_scales)[at * (D / 32) + c * N / 32];
-        float y[N];
-        load_values<N>(mx<CACHE>{}, (is_k ? A.k_pages : A.v_pages) + at * ROW, c * N, __uint_as_float(s << 23), y);
-        piece x;
+    constexpr int BATCH = 4;
+    for (int h0 = part * HW + lane / P; h0 < 2 * A.Hkv; h0 += A.parts * HW * BATCH) {
+        typename codes_of<CACHE, N>::type w[BATCH];
+        unsigned s[BATCH];
 #pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = (typename T::elem)y[i];
-        char* o = is_k ? A.k_out + t * A.ko_rs + hh * A.ko_hs : A.v_out + t * A.vo_rs + hh * A.vo_hs;
-        reinterpret_cast<piece*>(o)[c] = x;
+        for (int i = 0; i < BATCH; ++i) {
+            const int h = min(h0 + i * A.parts * HW, 2 * A.Hkv - 1);           // (behind the last: it again, and nothing is stored)
+            const bool is_k = h < A.Hkv;
+            const int64_t at = slot * A.Hkv + (is_k ? h : h - A.Hkv);
+            s[i] = (is_k ? A.k_scales : A.v_scales)[at * (D / 32) + c * N / 32];
+            w[i] = *reinterpret_cast<const typename codes_of<CACHE, N>::type*>((is_k ? A.k_pages : A.v_pages) + at * ROW + c * N * ROW / D);
+        }
+#pragma unroll
+        for (int i = 0; i < BATCH; ++i) {
+            const int h = h0 + i * A.parts * HW;
+            if (h >= 2 * A.Hkv) break;
+            float y[N];
+            values(mx<CACHE>{}, w[i], __uint_as_float(s[i] << 23), y);
+            piece x;
+#pragma unroll
+            for (int e = 0; e < N; ++e) x[e] = (typename T::elem)y[e];
+            char* o = h < A.Hkv ? A.k_out + t * A.ko_rs + h * A.ko_hs : A.v_out + t * A.vo_rs + (h - A.Hkv) * A.vo_hs;
+            reinterpret_cast<piece*>(o)[c] = x;
+        }
     }
 }
 
