@@ -159,13 +159,18 @@ template <int ROW> __device__ __forceinline__ constexpr int key_place_of(int row
 
 // 32 rows on their way from the pool through a wave's registers to its LDS: neighbouring lanes have neighbouring 16 bytes, which costs the
 // least of the look-ups that the first cache does (8 x 16000 rows of 4 bits, 32 heads: 176 us with a row's pieces 16 lanes apart, as products take them).
-template <int CACHE, int D> struct Stage {
+// PAST: past the caches' lasting part, for rows that are whole lines and met once (8-bit rows: 8 x 16000, 32 heads 193 us without, 170 with, 6.3 TB/s; 32 sequences
+// of 1 to 16384, 8 heads 70 / 61.5; of 4 bits, two heads' rows to a line, 125 / 136).
+template <int CACHE, int D, bool PAST> struct Stage {
     static constexpr int ROW = row_bytes<CACHE, D>(), LPR = ROW / 16, RPI = 64 / LPR, N = 32 / RPI, NB = D / 32;   // lanes of a row; rows of a load; loads; blocks of a row
     u32x4 w[N];
     // base: the lane's part of the pool's first row
     __device__ __forceinline__ void load(const char* base, const int64_t* at) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) w[i] = *reinterpret_cast<const u32x4*>(base + at[i]);
+        for (int i = 0; i < N; ++i) {
+            if constexpr (PAST) w[i] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(base + at[i]));
+            else w[i] = *reinterpret_cast<const u32x4*>(base + at[i]);
+        }
     }
     // A lane's places in LDS: of its first key's codes or elements, its first value's first piece.
     static __device__ __forceinline__ unsigned key_at(int lane) { return lane / LPR * ROW + key_place_of<ROW>(lane / LPR, lane % LPR) * 16; }
@@ -245,7 +250,7 @@ __device__ __forceinline__ float other_half(float x) {
     return __uint_as_float((threadIdx.x & 32) ? y[0] : y[1]);
 }
 
-template <typename T, int CACHE, int D, int NC>
+template <typename T, int CACHE, int D, int NC, bool PAST = false>
 __device__ __forceinline__ void attend(const SharedArgs& A, const Task& W, Shared<D>& s) {
     typedef kind<T, CACHE> K;
     typedef typename K::mat M;
@@ -274,7 +279,7 @@ __device__ __forceinline__ void attend(const SharedArgs& A, const Task& W, Share
     int64_t* const places = s.step.places[wave];
     const int tr = 4 * kg + (n16 >> 2);                // row and place of the lane's first transposing read
     unsigned tr_at = tr * (2 * D) + place_of<D>(tr, (n16 & 3) >> 1) * 16 + (n16 & 1) * 8;
-    unsigned key_at = Stage<CACHE, D>::key_at(lane), value_at = Stage<CACHE, D>::value_at(lane), operand_at = Key<CACHE, D>::at(n16, kg);
+    unsigned key_at = Stage<CACHE, D, PAST>::key_at(lane), value_at = Stage<CACHE, D, PAST>::value_at(lane), operand_at = Key<CACHE, D>::at(n16, kg);
     float m[NC], lsum[NC];
     dfx4 acc[NC][NB];
 #pragma unroll
@@ -284,7 +289,7 @@ __device__ __forceinline__ void attend(const SharedArgs& A, const Task& W, Share
 #pragma unroll
         for (int i = 0; i < NB; ++i) acc[b][i] = dfx4{0.f, 0.f, 0.f, 0.f};
     }
-    typedef Stage<CACHE, D> Rows32;
+    typedef Stage<CACHE, D, PAST> Rows32;
     constexpr int ROW = Rows32::ROW, LPR = Rows32::LPR;
     const int STEP = 32 * kWaves >> W.shift;
     const Rows<ROW> rows(A, W);
@@ -532,6 +537,9 @@ template <int D> struct Wide {
     };
 };
 
+// Rows of long prefixes go past the caches' lasting part (plain 131071 rows, 8 heads, 16 users 119 us without, 107 with; 64 users of 32749 rows 91 / 87).
+constexpr int kPast = 2;       // (of a load into LDS: the bit for that)
+
 // A lane's part of a tile on its way from the pool to LDS.  Plain rows go there by themselves, 16 bytes a lane at a time; codes pass
 // through registers, a block of 32 of a key and a value row per thread (heads of 64: of one of them).
 template <typename T, int CACHE, int D> struct Fetch;
@@ -556,8 +564,8 @@ template <typename T, int D> struct Fetch<T, 0, D> {
         }
 #pragma unroll
         for (int i = 0; i < PER; ++i) {
-            __builtin_amdgcn_global_load_lds((from)(kb + pk[i]), (to)(to_k + (i * kWaves + wave) * 1024), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((from)(vb + pv[i]), (to)(to_v + (i * kWaves + wave) * 1024), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((from)(kb + pk[i]), (to)(to_k + (i * kWaves + wave) * 1024), 16, 0, kPast);
+            __builtin_amdgcn_global_load_lds((from)(vb + pv[i]), (to)(to_v + (i * kWaves + wave) * 1024), 16, 0, kPast);
         }
     }
     // (such loads write no register that the compiler would wait for, and a barrier alone does not wait)
@@ -586,7 +594,9 @@ template <typename T, int CACHE, int D> struct Fetch {
             const int64_t at = places[((tensor + n == 0 ? k : v) + key) & (kPlaces - 1)];
 #pragma unroll
             for (int i = 0; i < W4 / 4; ++i) {
-                const uint4 x = *reinterpret_cast<const uint4*>(base[n] + at + 16 * i);
+                u32x4 x;              // (4 bits: a block is all that a thread loads of its row; the halves of one of 8 bits would be fetched twice)
+                if constexpr (CACHE == 2) x = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(base[n] + at));
+                else x = *reinterpret_cast<const u32x4*>(base[n] + at + 16 * i);
                 w[n][4 * i] = x.x;
                 w[n][4 * i + 1] = x.y;
                 w[n][4 * i + 2] = x.z;
@@ -899,11 +909,11 @@ template <int R> __device__ __forceinline__ bool prefix_task(const SharedArgs& A
     return true;
 }
 
-template <typename T, int CACHE, int D>
+template <typename T, int CACHE, int D, bool PAST>
 __global__ __launch_bounds__(kWaves * 64, D == 64 ? 4 : 3) void cached_attn(const SharedArgs A) {
     __shared__ __align__(256) Shared<D> s;
     Task W;
-    if (own_task<CACHE, false>(A, blockIdx.x, W)) attend<T, CACHE, D, 1>(A, W, s);
+    if (own_task<CACHE, false>(A, blockIdx.x, W)) attend<T, CACHE, D, 1, PAST>(A, W, s);
 }
 
 // R: query heads of a tile.
@@ -916,19 +926,19 @@ __global__ __launch_bounds__(kWaves * 64, R == 16 ? (D == 64 ? 4 : 3) : 2) void 
     } s;
     Task W;
     if (blockIdx.x >= A.prefix_groups) {
-        if (own_task<CACHE, true>(A, blockIdx.x - A.prefix_groups, W)) attend<T, CACHE, D, 1>(A, W, s.own);
+        if (own_task<CACHE, true>(A, blockIdx.x - A.prefix_groups, W)) attend<T, CACHE, D, 1, CACHE == 0>(A, W, s.own);
     } else if (prefix_task<R>(A, blockIdx.x, threadIdx.x & 63, W)) {
         if constexpr (kWide) attend_wide<T, CACHE, D, R / 32>(A, W, s.prefix);
         else attend<T, CACHE, D, R / 16>(A, W, s.prefix);
     }
 }
 
-// Joins the partials of a query head: a workgroup for each, a part of its threads every 8th (heads of 64: 16th) partial, four elements a thread, eight in
-// flight at a time, the first ones before the largest maximum is known.
-template <typename T, int CACHE, int D, bool SHARED>
-__global__ __launch_bounds__(256) void cached_join(const SharedArgs A) {
+// Joins the partials of a query head: a workgroup for each, its threads four elements of every 8th (heads of 64: 16th) partial, or, with 1024 threads,
+// of every 32nd (64th), eight in flight at a time, the first ones before the largest maximum is known.
+template <typename T, int CACHE, int D, bool SHARED, int THREADS>
+__global__ __launch_bounds__(THREADS) void cached_join(const SharedArgs A) {
     typedef typename kind<T, CACHE>::elem elem;
-    constexpr int LANES = D / 4, PARTS = 256 / LANES, BATCH = 8;
+    constexpr int LANES = D / 4, PARTS = THREADS / LANES, WAVES = THREADS / 64, BATCH = 8;
     const int64_t hq = blockIdx.x;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, b = (int)(hq / A.Hq), part = tid / LANES;
     const int S = clamped(A.lens[b], A.max_len);
@@ -970,13 +980,14 @@ __global__ __launch_bounds__(256) void cached_join(const SharedArgs A) {
     float M = -3.4028235e38f;
 #pragma unroll
     for (int i = 0; i < BATCH; ++i) M = fmaxf(M, p[i].x);
-    for (int i = PARTS * BATCH + tid; i < n; i += 256) M = fmaxf(M, ml[i < before ? i : A.prefix_chunks + (i - before)].x);
+    for (int i = PARTS * BATCH + tid; i < n; i += THREADS) M = fmaxf(M, ml[i < before ? i : A.prefix_chunks + (i - before)].x);
 #pragma unroll
     for (int d = 32; d >= 1; d >>= 1) M = fmaxf(M, __shfl_xor(M, d));
-    __shared__ float s_m[kWaves], s_l[PARTS], s_o[PARTS][D];
+    __shared__ float s_m[WAVES], s_l[PARTS], s_o[PARTS][D];
     if (lane == 0) s_m[wave] = M;
     __syncthreads();
-    M = fmaxf(fmaxf(s_m[0], s_m[1]), fmaxf(s_m[2], s_m[3]));
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) M = fmaxf(M, s_m[w]);
     float Lq = 0.f;
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int first = 0;;) {
@@ -1062,7 +1073,8 @@ hipError_t launch_shared(int dtype, int cache, int D, SharedArgs A, void* worksp
     A.scale2 = (float)(1.4426950408889634 / std::sqrt((double)D));
     A.part_acc = static_cast<float*>(workspace);
     A.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + P.acc_bytes);
-    A.head_shift = cache != 0 && (int64_t)A.B * A.Hkv * A.max_len >= kManyKeys ? (A.Hkv % 4 == 0 ? 2 : (A.Hkv % 2 == 0 ? 1 : 0)) : 0;
+    const bool many = (int64_t)A.B * A.Hkv * A.max_len >= kManyKeys;
+    A.head_shift = cache != 0 && many ? (A.Hkv % 4 == 0 ? 2 : (A.Hkv % 2 == 0 ? 1 : 0)) : 0;
     A.by_xcd = (int64_t)P.nchunk * A.B >= 8;
     A.places = A.by_xcd ? P.nchunk | 1 : P.nchunk;
     int64_t units = (int64_t)A.places * A.B;
@@ -1070,13 +1082,20 @@ hipError_t launch_shared(int dtype, int cache, int D, SharedArgs A, void* worksp
     A.prefix_by_xcd = P.prefix_chunks >= 8;
     A.prefix_groups = (unsigned)((A.prefix_by_xcd ? (P.prefix_chunks + 7) / 8 * 8 : P.prefix_chunks) * (int64_t)P.tiles * A.Hkv);
     const dim3 grid((unsigned)(A.prefix_groups + units * (A.Hkv >> A.head_shift))), block(kWaves * 64), heads((unsigned)((int64_t)A.B * A.Hq));
+    // (256 partials of 32 heads: a step over 131072 rows of 4 bits 38.7 us with 256 threads a head, 37.6 with 1024; 65 of 512 heads, 131071 rows of 8
+    // bits, 73.3 / 75.7)
+    auto join = [&](auto few, auto many) {
+        if (P.slots > 64 && heads.x <= 128) hipLaunchKernelGGL(many, heads, dim3(1024), 0, st, A);
+        else hipLaunchKernelGGL(few, heads, block, 0, st, A);
+    };
     auto form = [&](auto t, auto c, auto d) {
         typedef decltype(t) T;
         constexpr int C = decltype(c)::value, DD = decltype(d)::value;
         if (A.G == 0) {
             if constexpr (C != 0) {
-                hipLaunchKernelGGL((cached_attn<T, C, DD>), grid, block, 0, st, A);
-                if (P.slots > 1) hipLaunchKernelGGL((cached_join<T, C, DD, false>), heads, block, 0, st, A);
+                if (C == 1 && DD == 128 && many) hipLaunchKernelGGL((cached_attn<T, C, DD, C == 1 && DD == 128>), grid, block, 0, st, A);
+                else hipLaunchKernelGGL((cached_attn<T, C, DD, false>), grid, block, 0, st, A);
+                if (P.slots > 1) join(cached_join<T, C, DD, false, 256>, cached_join<T, C, DD, false, 1024>);
             }
             return;
         }
@@ -1084,7 +1103,7 @@ hipError_t launch_shared(int dtype, int cache, int D, SharedArgs A, void* worksp
         else if (P.columns == 32) hipLaunchKernelGGL((shared_attn<T, C, DD, 32>), grid, block, 0, st, A);
         else if (P.columns == 64) hipLaunchKernelGGL((shared_attn<T, C, DD, 64>), grid, block, 0, st, A);
         else hipLaunchKernelGGL((shared_attn<T, C, DD, 128>), grid, block, 0, st, A);
-        hipLaunchKernelGGL((cached_join<T, C, DD, true>), heads, block, 0, st, A);
+        join(cached_join<T, C, DD, true, 256>, cached_join<T, C, DD, true, 1024>);
     };
     auto of = [&](auto t, auto c) {
         if (D == 128) form(t, c, std::integral_constant<int, 128>{});
