@@ -475,7 +475,7 @@ int snapkv_append_paged_mx(int dtype, int cache, const void* q, const void* k, c
 
 /*
  * Rows of microscaled pages as values of dtype (rounded once; exact in bfloat16, where subnormal and beyond-range values of pages
- * that others wrote may differ, and in float32): what the compression of a prompt and the attention over one take.
+ * that others wrote may differ, and in float32; what a code's rounding took to 2^128 reads as infinity): what the compression of a prompt and the attention over one take.
  * The T rows of B sequences go packed to k_out and v_out [T, Hkv, D] (strides as for the outputs of snapkv_append_paged, rows that
  * overlap are refused): token t of sequence b is its logical row starts[b] + t - cu_seqlens[b] (cu_seqlens NULL: one row
  * per sequence, T == B).  Tokens of no sequence, rows that the table has no column for (or before the first) and table entries outside
@@ -503,7 +503,7 @@ size_t snapkv_decode_paged_mx_workspace_bytes(int B, int Hq, int Hkv, int D, int
 /*
  * The same step for batches whose sequences share prefixes: group i is the sequences cu_groups[i] .. cu_groups[i + 1] - 1, and
  * each of them sees the prefix_lens[i] rows that prefix_table's row i names, then its own lens[b] rows of block_table.  A
- * prefix's rows are read once for all query heads of its group that read them (up to 64 at a time), not once per sequence.
+ * prefix's rows are read once for all query heads of its group that read them (up to 128 at a time), not once per sequence.
  *
  *   cache   SNAPKV_CACHE_PLAIN (pages of dtype; k_scales and v_scales NULL), SNAPKV_CACHE_FP8 or SNAPKV_CACHE_FP4: of prefixes' and own rows,
  *           which lie in one pool of pages
@@ -516,7 +516,9 @@ size_t snapkv_decode_paged_mx_workspace_bytes(int B, int Hq, int Hkv, int D, int
  *   workspace 256-byte aligned, of at least snapkv_decode_shared_workspace_bytes(B, G, Hq, Hkv, D, max_prefix, max_len) bytes, as there
  *           (never 0 for shapes that the step takes)
  *
- * Answers are those of snapkv_decode_attention_paged over prefix and own rows in one table, up to rounding, and repeat bit for bit.
+ * Answers are those of snapkv_decode_attention_paged over prefix and own rows in one table, up to rounding, and repeat bit for bit.  Where
+ * a group has more than 32 query heads to a KV head on the average, probabilities over its prefix are rounded once to dtype before they
+ * meet the values (over codes with fp16 queries: not).
  */
 int snapkv_decode_attention_shared(int dtype, int cache, const void* q, const void* k_pages, const void* k_scales,
                                    const void* v_pages, const void* v_scales, int64_t num_pages, int page_size,

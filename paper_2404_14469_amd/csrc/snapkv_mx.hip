@@ -8,6 +8,10 @@
 // A code jumps at the border between two values, so a key is rotated in 64 bits, where products of its 24 bits at most are
 // exact, and brought to float32 with its last bit set where anything was lost: what is rounded once more from there, to
 // 4 bits or 2, is rounded as the 64-bit value would be.  Queries and the keys' second copy are rotated in float32 and rounded once.
+//
+// Both ways are bound by memory.  65319 tokens of 32 heads in 4 bits: written, with queries rotated, in 471 us (2.46 GB, 5.2 TB/s; a copy
+// reaches 5.1), read back in 258 (1.35 GB, 5.3 TB/s).  32749 rows of 8 heads in 8 bits read back in 31.8 us of a call (203 MB).  Eight rows: 5.0 and 4.0 us,
+// a launch's latency.
 #include "snapkv_sequence.h"
 #include "snapkv_serve.h"
 

@@ -5,8 +5,14 @@
 //
 // j over the rows of the prefix of b's group and then over b's own: one pass with the running maximum and sum of each part, and
 // the parts joined.  A prefix is met by the query heads of all its sequences that read one KV head, as the columns of the same
-// products, so its rows are read once for up to 16 NC of them.  Rows of caches in 8 or 4 bits become bfloat16 numbers
-// (exactly: a code has at most 4 significant bits) between the load and the product; fp16 queries meet them in two bfloat16 parts.
+// products, in tiles of 16, 32, 64 or 128, so its rows are read once for as many of them.  Rows of caches in 8 or 4 bits become
+// bfloat16 numbers (exactly: a code has at most 4 significant bits) between the load and the product; fp16 queries meet them in two
+// bfloat16 parts.  (The matrix instructions that take codes and scales themselves keep about 14 bits of a product's sum: not used.)
+//
+// What bounds it, and what it reaches (us, this card copies at 5.1 TB/s): own rows and small tiles the rows' loads, 16 x 1 to 16384 rows
+// of 8 bits 61 (4.6 TB/s), 8 x 16000 of 4 bits, 32 heads 125 (4.4), 131072 of 8 bits 38 (3.7, of which 4 to 5 are the join); wide tiles
+// loads and products together, 131071 rows of 8 bits for 16 users 77 (70 with the loads alone), 32749 for 64 users and their own 84.
+// One short sequence costs its two launches: 8.9.
 //
 // MFMA layout (16x16x32): lane l = 16 kg + n supplies row or column n and contraction elements 8 kg .. +7 of an operand; accumulator
 // register r of lane l is row 4 kg + r, column n.  Which element of a head is which contraction element is free, as long as
@@ -15,6 +21,9 @@
 //   logits^T = K Q^T, 32 keys a step, 16 after 16: a lane gets keys 4 kg .. +3 of both.  out^T = V^T P^T with P in two parts:
 //     contraction elements 8 kg .. +7 are those keys, so P never moves.  V goes through LDS, its rows' 16-byte pieces permuted,
 //     and comes back by the transposing read (16 lanes read four rows of 16 columns, a lane gets the four of one column).
+//
+// Tiles of 64 and 128 use 32x32x16 and round P once to the products' type (two parts for fp16 queries over codes): there the products
+// count, and a second part would be half as many again.
 #include "snapkv_attn.h"
 #include "snapkv_sequence.h"
 #include "snapkv_serve.h"
