@@ -45,6 +45,21 @@ def test_shared_step_matches_oracle(snapkv, groups, kind):
     check_shared(s, kind, *run_shared(snapkv, s))
 
 
+@pytest.mark.parametrize("room, kind", [(0, "plain"), (300, "plain"), (1200, "plain"), (300, "fp8"), (1200, "fp4")])
+@pytest.mark.parametrize("Hq", [128, 64])
+def test_shares_of_wide_tiles(snapkv, Hq, room, kind):
+    """Tiles of 128 and 64 query heads, their prefixes cut into 32, 24 or 16 shares as own rows may be few, as many or more; the last
+    shares of both prefixes are empty or partial."""
+    lens = [(3 * i) % 11 for i in range(16)]
+    s = build(seeded(1370), [4200, 3001], [8, 8], lens, 16, Hq, 8, 128, torch.bfloat16, kind, room=room)
+    keys, met = 16 * 8 * s["max_len"], 2 * 8 * 4200                # of own rows; of prefixes, one tile to a group and KV head
+    assert (keys < 0.3 * met, keys >= 1.5 * met) == (room == 0, room == 1200)
+    check_shared(s, kind, *run_shared(snapkv, s))
+    out, lse = run_shared(snapkv, s)
+    again, _ = run_shared(snapkv, s, lse=False)
+    assert torch.equal(out, again)
+
+
 def test_a_block_of_nan_reaches_its_own_heads_only(snapkv):
     """Scales of four KV heads are fetched together: a NaN of one head's leaves the others' bits as they are."""
     gen, lens = seeded(1360), [2100] + [500] * 130
