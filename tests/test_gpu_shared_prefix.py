@@ -202,6 +202,30 @@ def test_a_prefix_shared_is_the_prefix_of_each(snapkv):
     assert ((out.double() - want.double()).abs() <= 2.0 ** -7 * want.abs() + 2.0 ** -11).all()
 
 
+@pytest.mark.parametrize("kind", ["plain", "fp8"])
+@pytest.mark.parametrize("members", [3, 24, 60])
+def test_pool_beyond_32_bit_offsets(snapkv, members, kind):
+    """The same rows behind tables whose pages lie at both ends of a pool of over 4 GiB: the same bits, with tiles of 16, 64 and 128."""
+    page, Hkv, D = 128, 16, 128
+    s = build(seeded(87), [900], [members], [5, 130, 1] * (members // 3), page, 2 * Hkv, Hkv, D, torch.bfloat16, kind)
+    want = run(snapkv, s)
+    used = s["k_pages"].shape[0]
+    row = s["k_pages"][0].numel() * s["k_pages"].element_size()
+    pages = (1 << 32) // row + 2 * used
+    moved = torch.arange(used, device="cuda")
+    moved = torch.where(moved % 2 == 0, moved, pages - 1 - moved)
+    big = dict(s)
+    for n in ("k_pages", "v_pages", "k_scales", "v_scales"):
+        if n in s:
+            big[n] = torch.empty((pages,) + s[n].shape[1:], device="cuda", dtype=s[n].dtype)
+            big[n][moved] = s[n]
+    for n in ("prefix_table", "block_table"):
+        big[n] = torch.where(s[n] < used, moved[s[n].clamp(max=used - 1).long()], s[n]).to(torch.int32)
+    assert int(big["prefix_table"][0, :8].max()) * row > 1 << 32 and int(big["prefix_table"][0, :8].min()) < used
+    got = run(snapkv, big)
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+
+
 def test_workspaces_hold_nothing_between_calls(snapkv):
     """A workspace full of NaN, and captured steps of two shapes that share one, replayed with other lengths and groups."""
     gen = seeded(85)
