@@ -1037,8 +1037,8 @@ __global__ __launch_bounds__(THREADS) void cached_join(const SharedArgs A) {
 constexpr int64_t kManyKeys = 1 << 20;
 
 // Shares of a sequence's own rows: as many as give 1024 workgroups if all sequences are as long as they may be, of 128 to 1024 keys,
-// but no more than give 16384 workgroups, or seven; a sequence of up to 512 rows is not cut.  Shares of a prefix: of 128 keys at
-// least, no more than 256, and as many as give 1024 workgroups with all tiles and KV heads; fewer for tiles of 64 or 128 query heads (below).
+// but no more than give 16384 workgroups, or seven; a sequence of up to 512 rows is not cut.  Shares of a prefix, of 128 keys at
+// least and no more than 256: below.
 SharedPlan shared_plan(int B, int G, int Hq, int Hkv, int D, int64_t max_prefix, int64_t max_len) {
     SharedPlan P{};
     const int g = Hq / Hkv;
@@ -1053,15 +1053,23 @@ SharedPlan shared_plan(int B, int G, int Hq, int Hkv, int D, int64_t max_prefix,
         P.columns = rows <= 16 ? 16 : (rows <= 32 ? 32 : (rows <= 64 ? 64 : 128));
         P.tiles = (int)(G - 1 + ((int64_t)B * g + P.columns - 1) / P.columns);
         const int64_t units = (rows + P.columns - 1) / P.columns * G * Hkv;   // (as many tiles as groups of the average size have)
-        // Tiles of 64 or 128: 512 workgroups, two a compute unit, and fewer where the sequences' own rows are many, whose workgroups run beside them.
-        // Own keys over the prefixes' (all as long as they may be, a prefix's once a tile) and microseconds with 256 / 384 / 512 workgroups, 8 KV heads;
-        // the limits 0.3 and 1.5 were set by these: 0.00 (64 users, 32749 rows) 80.5 / 70.4 / 66.2, 0.06 (16 users, 131071 rows of 8 bits) 100 / 88 / 74, 0.24 (the
-        // same) 103 / 91 / 82, 0.49 (64 users, 32749 rows) 84 / 74 / 78, 0.74 (48) 84 / 76 / 79, 0.96 (32) 57 / 58 / 66, 0.98 (64) 91 / 84 / 93, 1.97 (64)
-        // 100 / 110 / 119.  Others, timed afterwards: 0.12 (40 users, 20011 rows) 55 / 52 / 46, 0.40 55.5 / 52.5 / 51.7, 1.41 60.4 / 61.0 / 67.1, 0.63 (2 x 16
-        // users) 88 / 79 / 82, 1.21 (96) 82 / 75 / 85, 2.42 (64, 4 bits) 65 / 67 / 71, and the rule's one loss of weight, 1.07 (2 x 64 users) 78 / 95 / 87.
+        // Shares, for so many workgroups with all tiles and KV heads, are dealt to the 8 XCDs in turn: as many for each, since of 12 four
+        // would get two and four one.  Tiles of 64 or 128 have two workgroups a compute unit and no more, and fewer where the sequences' own
+        // rows are many (own keys over the prefixes', a prefix's once a tile, all as long as they may be).
+        // Microseconds by shares, 8 KV heads.  Tiles of 128: 128 users of 20011 rows 8 / 12 / 16: 94 / 93 / 79; 160 of 16001 8 / 10 / 13 / 16: 97 / 130 / 112 / 104; 256 of
+        // 16001 4 / 6 / 8 / 12 / 16: 171 / 152 / 123 / 154 / 138; 64 of 32749 16 / 24 / 32 with one own row or two: 79 / 71 / 66, with half as many own keys as
+        // prefix keys: 82 / 74 / 78, as many: 86 / 83 / 91, twice: 96 / 107 / 119.  Of 32: 8 users of 32749 32 / 64 / 128: 32.0 / 34.5 / 43.4.  Of 16: 4 of 131071, 8 bits, 32 / 64 / 128: 66 / 69 / 71;
+        // 5 groups of 4, 16001 rows, 8 / 16 / 25: 86 / 76 / 81.  Heads of 64, 20 of them, 3 groups, 8 / 16 / 18: 30.0 / 28.5 / 29.3.  Of 66 sizes of all kinds, many of
+        // which shaped the rule, it is within 6 % of the best count tried at 54, within 8 % at 60; the worst is 20 % (6 groups of 16 users, 12007 rows: 8 shares 96, 6 of
+        // them 80), for a reason that was not found.
         const int64_t met = units * max_prefix;
-        const int64_t most = P.columns <= 32 ? 1024 : (10 * keys < 3 * met ? 512 : (2 * keys < 3 * met ? 384 : 256));
-        P.prefix_chunks = (int)std::max<int64_t>(1, std::min<int64_t>({256, (max_prefix + 127) / 128, (most + units - 1) / units}));
+        const int64_t most = P.columns == 16 ? 512 * (128 / D) : (P.columns == 32 ? 256 * (128 / D) : (20 * keys < 9 * met ? 512 : (2 * keys < 3 * met ? 384 : 256)));
+        int64_t shares = (most + units - 1) / units;
+        if (units < 128) {
+            shares = std::max<int64_t>(8, (most / units + 4) / 8 * 8);
+            while (P.columns > 32 && shares > 8 && shares * units > 512) shares -= 8;
+        }
+        P.prefix_chunks = (int)std::max<int64_t>(1, std::min<int64_t>({256, (max_prefix + 127) / 128, shares}));
         P.prefix_least = 128;
     }
     P.slots = P.prefix_chunks + P.nchunk;
