@@ -60,6 +60,14 @@ def test_shares_of_wide_tiles(snapkv, Hq, room, kind):
     assert torch.equal(out, again)
 
 
+@pytest.mark.parametrize("members", [3, 20])
+def test_prefixes_of_many_kv_heads(snapkv, members):
+    """So many tiles and KV heads (160) that prefixes are cut into a few shares only, with tiles of 16 and of 64 query heads."""
+    groups = [members, members + 1, 1, members, members - 1]
+    s = build(seeded(1380), [700, 129, 1001, 64, 513], groups, [i % 9 for i in range(sum(groups))], 16, 96, 32, 64, torch.bfloat16, "plain")
+    check_shared(s, "plain", *run_shared(snapkv, s))
+
+
 def test_a_block_of_nan_reaches_its_own_heads_only(snapkv):
     """Scales of four KV heads are fetched together: a NaN of one head's leaves the others' bits as they are."""
     gen, lens = seeded(1360), [2100] + [500] * 130
