@@ -518,7 +518,8 @@ size_t snapkv_decode_paged_mx_workspace_bytes(int B, int Hq, int Hkv, int D, int
  *
  * Answers are those of snapkv_decode_attention_paged over prefix and own rows in one table, up to rounding, and repeat bit for bit.  Where
  * a group has more than 32 query heads to a KV head on the average, probabilities over its prefix are rounded once to dtype before they
- * meet the values (over codes with fp16 queries: not).
+ * meet the values (over codes with fp16 queries: not).  Sums are float32: answers are finite where the rows that a sequence sees times their
+ * largest value stay below 2^133.
  */
 int snapkv_decode_attention_shared(int dtype, int cache, const void* q, const void* k_pages, const void* k_scales,
                                    const void* v_pages, const void* v_scales, int64_t num_pages, int page_size,

@@ -50,8 +50,9 @@ template <typename T, int CACHE> struct kind {
     typedef __bf16 elem;
     static constexpr int kQ = 1;                      // parts of a query
     // Probabilities are taken 2^kShift times as large, and relative to a maximum that is moved, and the sums with it, once it is outgrown by
-    // 2^kGrowth.
-    static constexpr float kShift = 0.f, kGrowth = 8.f;
+    // 2^kGrowth.  bf16: values reach from float32's largest to its smallest normal numbers.  2^16 of the largest have a finite sum so (while no maximum
+    // is outgrown, 64 at least), and the smallest, 2^-126, keep 8 bits in a product with the largest probability.
+    static constexpr float kShift = -16.f, kGrowth = 8.f;
 };
 template <> struct kind<dec_f16, 0> {
     typedef dec_f16 mat;
@@ -63,7 +64,7 @@ template <int CACHE> struct kind<dec_f16, CACHE> {
     typedef dec_bf16 mat;
     typedef _Float16 elem;
     static constexpr int kQ = 2;
-    static constexpr float kShift = 0.f, kGrowth = 8.f;
+    static constexpr float kShift = -16.f, kGrowth = 8.f;
 };
 
 // The head's element that is contraction element j of lane group kg in product c.
@@ -639,8 +640,8 @@ __device__ __forceinline__ void attend_wide(const SharedArgs& A, const Task& W, 
     constexpr int KS = kWaves / RB;                   // waves that share the keys
     constexpr int NQ = D / 16, ND = D / 32;           // products along a head; blocks of 32 output elements
     constexpr bool kF16 = CACHE == 0 && std::is_same<T, dec_f16>::value;
-    // exponent that probabilities are raised by, and the most that a lane's 16 may sum up to before its maximum is moved
-    constexpr float kShift = kF16 ? 7.f : 0.f, kMost = kF16 ? 32768.f : 1048576.f;
+    // exponent that probabilities are raised by, and the most that a lane's 16 may sum up to before its maximum is moved: 2^8 or 2^10 above it
+    constexpr float kShift = kF16 ? 7.f : K::kShift, kMost = kF16 ? 32768.f : 0x1p-6f;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int n32 = lane & 31, h2 = lane >> 5, rb = wave % RB, ks = wave / RB;
     auto head_of = [&](int row) { return ((int64_t)W.b0 + row / A.g) * A.Hq + (int64_t)W.kvh * A.g + row % A.g; };
@@ -1022,8 +1023,11 @@ __global__ __launch_bounds__(THREADS) void cached_join(const SharedArgs A) {
         Lq += s_l[i];
     }
     y = Lq == 0.f ? 0.f : y / Lq;
-    // (probabilities that were rounded up can carry a mean of numbers near fp16's largest past it; infinities stay)
-    if (CACHE == 0 && std::is_same<T, dec_f16>::value && __builtin_fabsf(y) < INFINITY) y = __builtin_amdgcn_fmed3f(y, -65504.f, 65504.f);
+    // (probabilities that were rounded up can carry a mean of numbers near the type's largest past it; infinities stay, and over codes means beyond
+    // fp16's range)
+    constexpr bool kHalf = std::is_same<T, dec_f16>::value;
+    constexpr float kLargest = kHalf ? 65504.f : 3.3895314e38f;
+    if (!(kHalf && CACHE != 0) && __builtin_fabsf(y) < INFINITY) y = __builtin_amdgcn_fmed3f(y, -kLargest, kLargest);
     reinterpret_cast<elem*>(A.out)[hq * D + tid] = (elem)y;
     if (A.lse && tid == 0) A.lse[hq] = Lq == 0.f ? -INFINITY : (M + __builtin_amdgcn_logf(Lq)) * 0.6931471805599453f;
 }
