@@ -462,7 +462,7 @@ size_t snapkv_decode_paged_workspace_bytes(int B, int Hq, int Hkv, int D, int64_
  *
  * snapkv_append_paged_mx is snapkv_append_paged into such pages: arguments as there, k_pages and v_pages the codes, k_scales and
  * v_scales the scales (all four 16-byte aligned).  Codes are those of the rotated row before any rounding (what lies beyond
- * float32's range counts as its largest number); q_out and k_out are rotated in float32 and rounded once, to dtype.
+ * float32's range counts as its largest number); q_out is rotated in float32, k_out in 64 bits, and each is rounded once, to dtype.
  */
 int snapkv_append_paged_mx(int dtype, int cache, const void* q, const void* k, const void* v, const int32_t* cu_seqlens,
                            const int32_t* starts, const int32_t* positions, int64_t T, int B, int Hq, int Hkv, int D,

@@ -7,13 +7,16 @@
 //
 // A code jumps at the border between two values, so a key is rotated in 64 bits, where products of its 24 bits at most are
 // exact, and brought to float32 with its last bit set where anything was lost: what is rounded once more from there, to
-// 4 bits or 2, is rounded as the 64-bit value would be.  Queries and the keys' second copy are rotated in float32 and rounded once.
+// 4 bits or 2, is rounded as the 64-bit value would be; so is the keys' second copy in bfloat16 and fp16, and in float32 it is the 64-bit value
+// rounded to nearest.  Queries are rotated in float32 and rounded once.
 //
 // Both ways are bound by memory.  65319 tokens of 32 heads in 4 bits: written, with queries rotated, in 471 us (2.46 GB, 5.2 TB/s; a copy
 // reaches 5.1), read back in 258 (1.35 GB, 5.3 TB/s).  32749 rows of 8 heads in 8 bits read back in 31.8 us of a call (203 MB).  Eight rows: 5.0 and 4.0 us,
 // a launch's latency.
 #include "snapkv_sequence.h"
 #include "snapkv_serve.h"
+
+#include <type_traits>
 
 namespace snapkv {
 namespace {
@@ -146,7 +149,8 @@ __global__ __launch_bounds__(256) void append_mx(const AppendArgs A) {
         const int hh = is_q ? h : (is_k ? h - A.Hq : h - A.Hq - A.Hkv);
         const char* src = is_q ? A.q + t * A.q_rs + hh * A.q_hs : (is_k ? A.k + t * A.k_rs + hh * A.k_hs : A.v + t * A.v_rs + hh * A.v_hs);
         const piece x0 = reinterpret_cast<const piece*>(src)[c0], x1 = reinterpret_cast<const piece*>(src)[c1];
-        float y[2 * N];
+        constexpr bool kSingle = std::is_same<typename T::elem, float>::value;
+        float y[2 * N], copy[kSingle ? 2 * N : 1];    // copy: float32 rows as the keys' second copy has them
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             y[i] = (float)x0[i];
@@ -166,9 +170,13 @@ __global__ __launch_bounds__(256) void append_mx(const AppendArgs A) {
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const int a = INTERLEAVED ? 2 * i : i, c = INTERLEAVED ? 2 * i + 1 : N + i;
-                const double ya = y[a], yc = y[c], dc = cs[i], ds = sn[i];
-                y[a] = to_odd(ya * dc - yc * ds);
-                y[c] = to_odd(yc * dc + ya * ds);
+                const double ya = y[a], yc = y[c], dc = cs[i], ds = sn[i], da = ya * dc - yc * ds, db = yc * dc + ya * ds;
+                y[a] = to_odd(da);
+                y[c] = to_odd(db);
+                if constexpr (kSingle) {
+                    copy[a] = (float)da;
+                    copy[c] = (float)db;
+                }
             }
         }
         if (is_q || (is_k && A.k_out)) {
@@ -177,6 +185,15 @@ __global__ __launch_bounds__(256) void append_mx(const AppendArgs A) {
             for (int i = 0; i < N; ++i) {
                 y0[i] = (typename T::elem)y[i];
                 y1[i] = (typename T::elem)y[N + i];
+            }
+            if constexpr (kSingle) {
+                if (is_k && turn) {
+#pragma unroll
+                    for (int i = 0; i < N; ++i) {
+                        y0[i] = copy[i];
+                        y1[i] = copy[N + i];
+                    }
+                }
             }
             char* o = is_q ? A.q_out + t * A.qo_rs + hh * A.qo_hs : A.k_out + t * A.ko_rs + hh * A.ko_hs;
             store_row<PAST>(reinterpret_cast<piece*>(o) + c0, y0);
