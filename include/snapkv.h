@@ -385,7 +385,7 @@ int snapkv_decode_attention(int dtype, const void* q, const void* k_cache, const
  *   q_out   [T, Hq, D] device, the rotated queries (NULL with Hq = 0);  k_out [T, Hkv, D] device or NULL: the rotated keys
  *           once more, for the attention over the prompt; strides as for the inputs, rows that overlap are refused
  *
- * T < 2^26.  Rows that the table has no column for (or before the first) and table entries outside [0, num_pages) are not
+ * T <= 2^26 - 4.  Rows that the table has no column for (or before the first) and table entries outside [0, num_pages) are not
  * written to pages.  Distinct tokens must not meet in one row of one page.  T = 0 or B = 0 does nothing.  No scratch; calls are independent and
  * may be captured.  Returns SNAPKV_OK or a negative SNAPKV_ERR_* code.
  */

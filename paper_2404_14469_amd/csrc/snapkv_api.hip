@@ -151,6 +151,9 @@ int check_paged_shape(int B, int Hq, int Hkv, int D, int64_t max_len) {
     return SNAPKV_OK;
 }
 
+// Tokens of a call around pages, of which a workgroup of 256 threads takes four: a launch has fewer than 2^32 threads.
+constexpr int64_t kMostTokens = ((int64_t)1 << 26) - 4;
+
 // The checks of snapkv_append_paged and what its kernels take; *empty: there is nothing to do.
 int append_args(int dtype, const void* q, const void* k, const void* v, const int32_t* cu_seqlens, const int32_t* starts,
                 const int32_t* positions, int64_t T, int B, int Hq, int Hkv, int D, int64_t q_row_stride,
@@ -172,7 +175,7 @@ int append_args(int dtype, const void* q, const void* k, const void* v, const in
     if (D != 64 && D != 128) return SNAPKV_ERR_UNSUPPORTED;
     const int e = elem_bytes(dtype);
     if (rot_dim % (32 / e) != 0) return SNAPKV_ERR_UNSUPPORTED;
-    if (T >= (int64_t)1 << 26 || B >= 1 << 24 || Hq + 2 * (int64_t)Hkv > 65535 || num_pages > ((int64_t)1 << 31) ||
+    if (T > kMostTokens || B >= 1 << 24 || Hq + 2 * (int64_t)Hkv > 65535 || num_pages > ((int64_t)1 << 31) ||
         table_columns > ((int64_t)1 << 31) || n_positions > ((int64_t)1 << 31))
         return SNAPKV_ERR_UNSUPPORTED;
     struct { const void* p; int64_t rows, heads; } const t[] = {
@@ -1445,7 +1448,7 @@ int snapkv_read_paged_mx(int dtype, int cache, const void* k_pages, const void* 
     if (!cu_seqlens && T != B) return SNAPKV_ERR_INVALID_ARG;
     if (num_pages < 1 || page_size < 1 || table_columns < 1) return SNAPKV_ERR_INVALID_ARG;
     if (D != 64 && D != 128) return SNAPKV_ERR_UNSUPPORTED;
-    if (T >= (int64_t)1 << 26 || B >= 1 << 24 || 2 * (int64_t)Hkv > 65535 || num_pages > ((int64_t)1 << 31) ||
+    if (T > kMostTokens || B >= 1 << 24 || 2 * (int64_t)Hkv > 65535 || num_pages > ((int64_t)1 << 31) ||
         table_columns > ((int64_t)1 << 31))
         return SNAPKV_ERR_UNSUPPORTED;
     const int e = elem_bytes(dtype);
