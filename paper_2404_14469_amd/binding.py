@@ -630,8 +630,8 @@ def _steps():
         load()
         if not os.path.exists(os.path.join(_PKG, "_steps.so")):
             raise FileNotFoundError(
-                f"{os.path.join(_PKG, '_steps.so')} is missing: build it with `python -m paper_2404_14469_amd.build` "
-                "(there is no CPU fallback)")
+                f"{os.path.join(_PKG, '_steps.so')} is missing: build it with `python -m paper_2404_14469_amd.build` where g++ and the "
+                "headers of torch and Python are (there is no CPU fallback)")
         from . import _steps as module
         _steps_module = module
     return _steps_module

@@ -2,8 +2,10 @@
 from __future__ import annotations
 
 import os
+import shutil
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
@@ -20,8 +22,6 @@ FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-gpu-rdc",
 
 
 def steps_command() -> list:
-    import sysconfig
-
     import torch
     from torch.utils import cpp_extension
     lib = os.path.join(os.path.dirname(torch.__file__), "lib")
@@ -29,6 +29,36 @@ def steps_command() -> list:
             *("-I" + p for p in [*cpp_extension.include_paths(), sysconfig.get_paths()["include"]]),
             os.path.join(CSRC, "snapkv_steps.cpp"), "-o", STEPS, "-L" + lib, "-ltorch_python", "-ltorch_cpu", "-lc10", "-L" + PKG, "-lsnapkv",
             "-Wl,-rpath,$ORIGIN"]
+
+
+def missing_for_steps() -> str:
+    """What the compiled part of the binding needs and this machine lacks ("": nothing)."""
+    if shutil.which("g++") is None:
+        return "g++"
+    try:
+        from torch.utils import cpp_extension
+    except ImportError:
+        return "torch"
+    if not any(os.path.exists(os.path.join(p, "torch", "extension.h")) for p in cpp_extension.include_paths()):
+        return "torch's headers"
+    if not os.path.exists(os.path.join(sysconfig.get_paths()["include"], "Python.h")):
+        return "Python's headers"
+    return ""
+
+
+def build_steps(verbose: bool = False) -> None:
+    """The compiled part of the binding; where the machine lacks what it needs, none, and the calls that it makes say so when they are made."""
+    if os.path.exists(STEPS):
+        os.remove(STEPS)
+    missing = missing_for_steps()
+    if missing:
+        print(f"{STEPS} is not built: {missing} not found; the library is complete without it, the binding lacks the steps over microscaled and shared pages",
+              flush=True)
+        return
+    cmd = steps_command()
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    subprocess.check_call(cmd)
 
 
 def build_library(verbose: bool = False) -> str:
@@ -51,7 +81,7 @@ def build_library(verbose: bool = False) -> str:
             print(text, flush=True)
     link = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB, *objs]
     subprocess.check_call(link)
-    subprocess.check_call(steps_command())
+    build_steps(verbose)
     return LIB
 
 
