@@ -82,8 +82,7 @@ __device__ __forceinline__ float to_odd(double x) {
     return __uint_as_float(u);
 }
 
-// Rows of a call of many tokens go past the caches: nothing reads them before the call ends, and by then most would have been pushed out one
-// by one.  (A prompt of 32749 rows of 8/8 heads read back 43.0 us without, 31.8 with, 6.4 TB/s.)
+// Output rows may go past the caches (launch_append_mx and launch_read_mx say when).
 template <bool PAST, typename P> __device__ __forceinline__ void store_row(P* to, P x) {
     if constexpr (PAST) __builtin_nontemporal_store(x, to);
     else *to = x;
@@ -339,16 +338,27 @@ template <typename F> hipError_t by_form(int dtype, int cache, int D, F form) {
 
 }  // namespace
 
+// Output bytes from which a call's rows go past the caches.  What counts is the call and the one behind it, which reads these rows.  Microseconds past / through
+// the caches.  Append with the attention over the prompts behind it: 1070 MB 4245 / 4265, 819 MB 2983 / 2995, 512 MB 1775 / 1782; 246 MB 869 / 866, 213 MB 534 / 531,
+// 154 MB 458 / 449, 4 MB (8192 tokens of 2/2 heads of 64) 64 / 55: past from about twice the last-level cache's 256 MB on.
+// Read with the compression behind it, into the same rows as before or others in turn: 1070 MB 404 / 420, 537 MB 232 / 237; 459 MB 220 / 211 and 221 / 212, 328 MB
+// 159 / 154 and 161 / 158, 213 MB 94 / 106 and 112 / 104, 154 MB 77 / 76 and 79 / 82, 134 MB (32749 tokens of 8 heads) 84 / 83 and 91 / 87, 32 heads 73 / 71 and 75 / 81;
+// 57 MB 47 / 45 and 46 / 44, 46 MB 45 / 43 and 41 / 40, 25 MB 51.5 / 51.1 and 47.0 / 46.4, 8 MB 31.6 / 31.2.  The read alone: 213 MB 44 / 60, 134 MB 32 / 43, 25 MB
+// 6.9 / 8.9.  So from 64 MB on the pair takes the same within a few percent either way and the read alone less; below, what the read takes less comes back in the
+// compression, which finds no rows in the caches, and more.
+constexpr int64_t kPastAppend = 500000000, kPastRead = 64000000;
+
 hipError_t launch_append_mx(int dtype, int cache, int D, bool interleaved, AppendArgs A, hipStream_t st) {
     const int units = D * (dtype == 1 ? 4 : 2) / 32, per = 64 / units;
     const int heads = A.Hq + 2 * A.Hkv, groups = (heads + per - 1) / per;
     A.parts = A.T < 1024 ? groups : 1;
+    const bool past = A.T * (A.Hq + (A.k_out ? A.Hkv : 0)) * D * (dtype == 1 ? 4 : 2) > kPastAppend;
     const dim3 grid((unsigned)((A.T * A.parts + 3) / 4)), block(256);
     return by_form(dtype, cache, D, [&](auto t, auto c, auto d) {
         typedef decltype(t) T;
         constexpr int C = decltype(c)::value, DD = decltype(d)::value;
         auto launch = [&](auto kern) { hipLaunchKernelGGL(kern, grid, block, 0, st, A); };
-        if (A.parts == 1) launch(interleaved ? append_mx<T, C, DD, true, true> : append_mx<T, C, DD, false, true>);
+        if (past) launch(interleaved ? append_mx<T, C, DD, true, true> : append_mx<T, C, DD, false, true>);
         else launch(interleaved ? append_mx<T, C, DD, true, false> : append_mx<T, C, DD, false, false>);
     });
 }
@@ -357,12 +367,13 @@ hipError_t launch_read_mx(int dtype, int cache, int D, AppendArgs A, hipStream_t
     const int per = 64 * 16 / (D * (dtype == 1 ? 4 : 2));
     const int groups = (2 * A.Hkv + per - 1) / per;
     A.parts = A.T < 1024 ? groups : 1;
+    const bool past = 2 * A.T * A.Hkv * D * (dtype == 1 ? 4 : 2) > kPastRead;
     const dim3 grid((unsigned)((A.T * A.parts + 3) / 4)), block(256);
     return by_form(dtype, cache, D, [&](auto t, auto c, auto d) {
         typedef decltype(t) T;
         constexpr int C = decltype(c)::value, DD = decltype(d)::value;
         auto launch = [&](auto kern) { hipLaunchKernelGGL(kern, grid, block, 0, st, A); };
-        launch(A.parts == 1 ? read_mx<T, C, DD, true> : read_mx<T, C, DD, false>);
+        launch(past ? read_mx<T, C, DD, true> : read_mx<T, C, DD, false>);
     });
 }
 
