@@ -456,7 +456,8 @@ size_t snapkv_decode_paged_workspace_bytes(int B, int Hq, int Hkv, int D, int64_
  * Microscaled pages: the same caches in 8 or 4 bits.  A row of D values lies in blocks of 32; with A a block's largest magnitude and
  * M the largest value of the element type (SNAPKV_CACHE_FP8: e4m3, 448; SNAPKV_CACHE_FP4: e2m1, 6), e is the smallest integer with
  * A <= M 2^e, at least -117; scale byte e + 127; an element's code is the element type's value nearest to x 2^-e, ties to the
- * even code.  A block that holds an infinity or NaN has scale byte 255 and codes of zero and reads as NaN.
+ * even code.  A block that holds an infinity or NaN has scale byte 255 and codes of zero and reads as NaN.  (The OCP specification's conversion takes
+ * floor(log2 A) less the largest code's exponent for e and clips what lies beyond M 2^e; here nothing is clipped.  Pages that it filled read as they stand.)
  *   codes   [num_pages, page_size, Hkv, D] bytes (FP8), or [.., D / 2] with the even element in a byte's low half (FP4)
  *   scales  [num_pages, page_size, Hkv, D / 32] bytes
  *
@@ -491,7 +492,7 @@ int snapkv_read_paged_mx(int dtype, int cache, const void* k_pages, const void* 
 /*
  * snapkv_decode_attention_paged over microscaled pages (cache SNAPKV_CACHE_FP8 or SNAPKV_CACHE_FP4; all four parts of the pages 16-byte aligned):
  * arguments, limits and errors as there; dtype is that of q and out.  Rows below lens that read as NaN give NaN.  The workspace is of at
- * least snapkv_decode_paged_mx_workspace_bytes(B, Hq, Hkv, D, max_len) bytes.
+ * least snapkv_decode_paged_mx_workspace_bytes(B, Hq, Hkv, D, max_len) bytes.  Sums as for snapkv_decode_attention_shared.
  */
 int snapkv_decode_attention_paged_mx(int dtype, int cache, const void* q, const void* k_pages, const void* k_scales,
                                      const void* v_pages, const void* v_scales, const int32_t* block_table,
@@ -503,7 +504,9 @@ size_t snapkv_decode_paged_mx_workspace_bytes(int B, int Hq, int Hkv, int D, int
 /*
  * The same step for batches whose sequences share prefixes: group i is the sequences cu_groups[i] .. cu_groups[i + 1] - 1, and
  * each of them sees the prefix_lens[i] rows that prefix_table's row i names, then its own lens[b] rows of block_table.  A
- * prefix's rows are read once for all query heads of its group that read them (up to 128 at a time), not once per sequence.
+ * prefix's rows are read once for each tile of 16, 32, 64 or 128 query heads of its group that read them, not once per sequence.  Tiles have the
+ * least of these widths that holds a group of the average size, B / G sequences, and prefixes are cut into shares as if each were max_prefix rows long: groups of
+ * very different sizes or prefixes of very different lengths are better met in calls of their own.
  *
  *   cache   SNAPKV_CACHE_PLAIN (pages of dtype; k_scales and v_scales NULL), SNAPKV_CACHE_FP8 or SNAPKV_CACHE_FP4: of prefixes' and own rows,
  *           which lie in one pool of pages
@@ -519,7 +522,7 @@ size_t snapkv_decode_paged_mx_workspace_bytes(int B, int Hq, int Hkv, int D, int
  * Answers are those of snapkv_decode_attention_paged over prefix and own rows in one table, up to rounding, and repeat bit for bit.  Where
  * a group has more than 32 query heads to a KV head on the average, probabilities over its prefix are rounded once to dtype before they
  * meet the values (over codes with fp16 queries: not).  Sums are float32: answers are finite where the rows that a sequence sees times their
- * largest value stay below 2^133.
+ * largest value stay below 2^133.  Plain rows are finite, as there: an infinite value makes the answers of those who see it infinite or NaN.
  */
 int snapkv_decode_attention_shared(int dtype, int cache, const void* q, const void* k_pages, const void* k_scales,
                                    const void* v_pages, const void* v_scales, int64_t num_pages, int page_size,

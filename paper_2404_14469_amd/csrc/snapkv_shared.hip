@@ -5,12 +5,12 @@
 //
 // j over the rows of the prefix of b's group and then over b's own: one pass with the running maximum and sum of each part, and
 // the parts joined.  A prefix is met by the query heads of all its sequences that read one KV head, as the columns of the same
-// products, in tiles of 16, 32, 64 or 128, so its rows are read once for as many of them.  Rows of caches in 8 or 4 bits become
+// products, in tiles of 16, 32, 64 or 128 (one width for all groups, by their average), so its rows are read once for as many of them.  Rows of caches in 8 or 4 bits become
 // bfloat16 numbers (exactly: a code has at most 4 significant bits) between the load and the product; fp16 queries meet them in two
 // bfloat16 parts.  (The matrix instructions that take codes and scales themselves keep about 14 bits of a product's sum: not used.)
 //
-// What bounds it, and what it reaches (us, this card copies at 5.1 TB/s): own rows and small tiles the rows' loads, 16 x 1 to 16384 rows
-// of 8 bits 61 (4.6 TB/s), 8 x 16000 of 4 bits, 32 heads 125 (4.4), 131072 of 8 bits 38 (3.7, of which 4 to 5 are the join); wide tiles
+// What bounds it, and what it reaches (us, this card copies at 5.1 TB/s): own rows and small tiles the rows' loads, 32 x 1 to 16384 rows
+// of 8 bits 61 (4.6 TB/s), 8 x 16000 of 4 bits, 32 heads 125 (4.4), 131072 of 4 bits 38 (3.7, of which 5 to 6 are the join); wide tiles
 // loads and products together, 131071 rows of 8 bits for 16 users 77 (70 with the loads alone), 32749 for 64 users and their own 84.
 // One short sequence costs its two launches: 8.9.
 //
@@ -71,8 +71,6 @@ template <int CACHE> struct kind<dec_f16, CACHE> {
 template <int CACHE, int D> __device__ __forceinline__ constexpr int element_of(int kg, int c, int j) {
     return CACHE == 0 ? 32 * c + 8 * kg + j : D / 4 * kg + 8 * c + j;
 }
-
-typedef __attribute__((ext_vector_type(2))) __bf16 dbf16x2;
 
 // Eight values of codes (of 8 bits: both words, of 4: the first) under a scale byte, as bfloat16 numbers.
 template <int CACHE> __device__ __forceinline__ uint4 values_of(unsigned w0, unsigned w1, unsigned s) {
@@ -172,7 +170,7 @@ template <int ROW> __device__ __forceinline__ constexpr int key_place_of(int row
 // PAST: past the caches' lasting part, for rows that are whole lines and met once (8-bit rows: 8 x 16000, 32 heads 193 us without, 170 with, 6.3 TB/s; 32 sequences
 // of 1 to 16384, 8 heads 70 / 61.5; of 4 bits, two heads' rows to a line, 125 / 136).
 template <int CACHE, int D, bool PAST> struct Stage {
-    static constexpr int ROW = row_bytes<CACHE, D>(), LPR = ROW / 16, RPI = 64 / LPR, N = 32 / RPI, NB = D / 32;   // lanes of a row; rows of a load; loads; blocks of a row
+    static constexpr int ROW = row_bytes<CACHE, D>(), LPR = ROW / 16, RPI = 64 / LPR, N = 32 / RPI;   // lanes of a row; rows of a load; loads
     u32x4 w[N];
     // base: the lane's part of the pool's first row
     __device__ __forceinline__ void load(const char* base, const int64_t* at) {
@@ -1034,15 +1032,16 @@ __global__ __launch_bounds__(THREADS) void cached_join(const SharedArgs A) {
 
 }  // namespace
 
-// Sequences that can be long or many (keys of all KV heads, from here on) have shares of at most 512 keys, and, over codes, workgroups that
-// take four KV heads together, a wave each (or two): one fetch of scales for all, and whole lines of 4-bit codes.  Microseconds with one / two / four
+// Sequences that can be long or many (keys of all KV heads, from here on) have shares of 512 keys, where as many shares may be (below), and, over codes,
+// workgroups that take four KV heads together, a wave each (or two): one fetch of scales for all, and whole lines of 4-bit codes.  Microseconds with one / two / four
 // heads: 8 x 16000 rows, 32 heads, 4 bits 152 / 129 / 126, 8 bits 215 / 197 / 193; 131072 rows, 8 heads, 4 bits 43 / 39 / 40, 8 bits 70 / 65 / 61; 32
 // sequences of 1 to 16384 rows, 8 heads, 8 bits 73 / 71 / 70.  Fewer keys: 8 x 4000 rows of 4 bits, 8 heads 16.8 / 17.8 / 20.9, 2 x 30000 22.4 / 22.0 / 24.5.
 constexpr int64_t kManyKeys = 1 << 20;
 
 // Shares of a sequence's own rows: as many as give 1024 workgroups if all sequences are as long as they may be, of 128 to 1024 keys,
-// but no more than give 16384 workgroups, or seven; a sequence of up to 512 rows is not cut.  Shares of a prefix, of 128 keys at
-// least and no more than 256: below.
+// but no more than 16384 of all sequences and KV heads, or seven a sequence: where that is fewer, shares are longer (128 sequences of up to 131072 rows, 8 KV
+// heads: 16 of 8192, though over codes a workgroup takes four heads' shares); a sequence of up to 512 rows is not cut.  Shares of a prefix, of
+// 128 keys at least and no more than 256, go by the longest prefix there may be and the groups' average size: below.
 SharedPlan shared_plan(int B, int G, int Hq, int Hkv, int D, int64_t max_prefix, int64_t max_len) {
     SharedPlan P{};
     const int g = Hq / Hkv;
